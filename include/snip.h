@@ -337,6 +337,44 @@ snip_status snip_adamw_sensitivity(const float* m, const float* v, const void* g
 double snip_weight_divergence(double alpha, double beta1, double beta2, int64_t t, double sens_sq,
                               double err_g_sq, int64_t n, int64_t k);
 
+/* ---- RMS norm in front of a linear layer ------------------------------------------------ */
+/* What makes the X operand of the linears behind a norm, with the residual's addition in front of it:
+ *     h = bf16(x + residual)   (h = x without a residual)
+ *     rstd = 1 / sqrt(mean(h^2) + eps) of every row,   y = h * weight * rstd.
+ * The norm is that of h as it is stored, so that the backward call differentiates what was computed.  Sums
+ * and statistics are fp32; y is rounded once, from fp32, to each output asked for:
+ *   x, residual: device, bf16 [rows][ld], 16-byte aligned, ld >= cols and a multiple of 8; residual may be NULL.
+ *   weight  : device, [cols], bf16 or fp32 (weight_dtype), 16-byte aligned.
+ *   eps     : finite, >= 0.  With eps = 0 a row of zeros is 0 * infinity: NaN.
+ *   sum     : device, bf16 [rows][ld_sum], h; NULL, or with a residual only (SNIP_ERR_NULL otherwise).  May be x or residual
+ *             itself (same ld).
+ *   rstd    : device, fp32 [rows], or NULL.
+ *   y       : device, bf16 [rows][ld_y], or NULL.
+ *   out_row : y quantized in blocks along rows, as by snip_quantize(..., SNIP_AXIS_ROW, rule, ...), but from fp32; cols a
+ *             multiple of 32.  NULL if not wanted.
+ *   out_col : the same down columns, stored transposed (cols x rows), the operand of snip_gemm_wgrad; rows a multiple of 32, cols
+ *             even.  Needs rstd, and with a residual sum (SNIP_ERR_NULL otherwise).  The two formats may differ.
+ * At least one output has to be given (SNIP_ERR_NULL).  A row with an infinity or a NaN gets NaNs; blocks that hold one get scale
+ * byte 0xFF and zero codes, as in snip_quantize.  Columns >= cols of sum and y are not touched. */
+snip_status snip_rms_norm(const void* x, int64_t rows, int64_t cols, int64_t ld, const void* residual, int64_t ld_residual,
+                          const void* weight, snip_out_dtype weight_dtype, float eps, snip_scale_rule rule,
+                          void* sum, int64_t ld_sum, float* rstd, void* y, int64_t ld_y,
+                          const snip_qtensor* out_row, const snip_qtensor* out_col, void* stream);
+
+/* Its gradient.  With g = dy * weight:
+ *     dx = rstd * (g - h * rstd^2 * mean(g h)) + dsum        (of x and of the residual alike)
+ *     dweight = sum over rows of dy * h * rstd
+ *   dy, h, dsum, dx: device, bf16, rows and pitches as above; h is `sum` (or x) and rstd that of the forward call; dsum, the
+ *             gradient that reaches h past the norm, may be NULL.  dx may be dy or dsum itself.
+ *   dweight : device, fp32 [cols], or NULL.
+ *   workspace: device, needed with dweight, >= snip_rms_norm_workspace_bytes(rows, cols) bytes, 16-byte aligned.
+ * Sums are fp32 and added in a fixed order (those of workgroups in double). */
+size_t snip_rms_norm_workspace_bytes(int64_t rows, int64_t cols);
+snip_status snip_rms_norm_backward(const void* dy, int64_t rows, int64_t cols, int64_t ld_dy, const void* h, int64_t ld_h,
+                                   const void* weight, snip_out_dtype weight_dtype, const float* rstd,
+                                   const void* dsum, int64_t ld_dsum, void* dx, int64_t ld_dx, float* dweight,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- quantization-error statistics (Sec. 3.1 Step 1; row-wise form: Sec. 5.3) -------- */
 
 /* One read of a bf16 matrix; for blocks along `axis` produces the squared Frobenius norm of x

@@ -81,6 +81,30 @@ snip_status gemm(const snip_qtensor* a, int fmt_a, const snip_qtensor* b, int fm
     return launch_gemm(g, (hipStream_t)stream) == hipSuccess ? SNIP_OK : SNIP_ERR_HIP;
 }
 
+// A bf16 matrix of a norm: `rows` rows `ld` apart.
+snip_status check_rows(const void* p, int64_t rows, int64_t cols, int64_t ld)
+{
+    if (!p && rows > 0) return SNIP_ERR_NULL;
+    if (ld < cols) return SNIP_ERR_SHAPE;
+    if (!aligned16(p) || ld % 8 != 0) return SNIP_ERR_LAYOUT;
+    return SNIP_OK;
+}
+snip_status check_norm(int64_t rows, int64_t cols, const void* weight, int weight_dtype)
+{
+    if (weight_dtype != SNIP_OUT_BF16 && weight_dtype != SNIP_OUT_FP32) return SNIP_ERR_FORMAT;
+    if (rows < 0 || cols <= 0 || rows >= (int64_t)1 << 31 || cols >= (int64_t)1 << 30) return SNIP_ERR_SHAPE;
+    if (!weight) return SNIP_ERR_NULL;
+    return aligned16(weight) ? SNIP_OK : SNIP_ERR_LAYOUT;
+}
+snip_status check_out(const snip_qtensor* o, int64_t stored_rows, int64_t stored_cols)
+{
+    if (!valid_fmt(o->fmt)) return SNIP_ERR_FORMAT;
+    if (o->rows != stored_rows || o->cols != stored_cols || stored_cols % 32 != 0) return SNIP_ERR_SHAPE;
+    if ((!o->codes || !o->scales) && stored_rows > 0 && stored_cols > 0) return SNIP_ERR_NULL;
+    if (!aligned16(o->codes) || !aligned16(o->scales_g4) || (reinterpret_cast<uintptr_t>(o->scales) & 3u)) return SNIP_ERR_LAYOUT;
+    return SNIP_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -402,6 +426,74 @@ snip_status snip_quant_error_stats_both(const void* x, int64_t rows, int64_t col
     a.x = (const uint16_t*)x; a.rows = rows; a.cols = cols; a.ld = ld; a.axis = SNIP_AXIS_ROW; a.rule = rule;
     a.stats = (double*)out_row; a.per_line = nullptr; a.workspace = workspace;
     return launch_stats_both(a, (double*)out_col, (hipStream_t)stream) == hipSuccess ? SNIP_OK : SNIP_ERR_HIP;
+}
+
+snip_status snip_rms_norm(const void* x, int64_t rows, int64_t cols, int64_t ld, const void* residual, int64_t ld_residual,
+                          const void* weight, snip_out_dtype weight_dtype, float eps, snip_scale_rule rule, void* sum,
+                          int64_t ld_sum, float* rstd, void* y, int64_t ld_y, const snip_qtensor* out_row,
+                          const snip_qtensor* out_col, void* stream)
+{
+    if (rule != SNIP_SCALE_NO_OVERFLOW && rule != SNIP_SCALE_OCP_FLOOR) return SNIP_ERR_FORMAT;
+    if (!(eps >= 0.f && eps <= 3.402823466e38f)) return SNIP_ERR_FORMAT;
+    snip_status st = check_norm(rows, cols, weight, weight_dtype);
+    if (st == SNIP_OK) st = check_rows(x, rows, cols, ld);
+    if (st == SNIP_OK && residual) st = check_rows(residual, rows, cols, ld_residual);
+    if (st == SNIP_OK && sum) st = residual ? check_rows(sum, rows, cols, ld_sum) : SNIP_ERR_NULL;
+    if (st == SNIP_OK && y) st = check_rows(y, rows, cols, ld_y);
+    if (st != SNIP_OK) return st;
+    if (rows > 0 && !sum && !rstd && !y && !out_row && !out_col) return SNIP_ERR_NULL;      // (an empty vector may have no storage)
+    if (reinterpret_cast<uintptr_t>(rstd) & 3u) return SNIP_ERR_LAYOUT;
+    if (out_row && (st = check_out(out_row, rows, cols)) != SNIP_OK) return st;
+    if (out_col) {
+        if (cols % 2 != 0) return SNIP_ERR_SHAPE;
+        if ((st = check_out(out_col, cols, rows)) != SNIP_OK) return st;
+        if (rows > 0 && (!rstd || (residual && !sum))) return SNIP_ERR_NULL;
+        if ((rows + 31) / 32 * ((cols + 127) / 128) >= (int64_t)1 << 31) return SNIP_ERR_SHAPE;
+    }
+    NormArgs a = {};
+    a.x = (const uint16_t*)x; a.ldx = ld; a.r = (const uint16_t*)residual; a.ldr = ld_residual;
+    a.gain = weight; a.gain_fp32 = weight_dtype == SNIP_OUT_FP32; a.rows = (int)rows; a.cols = (int)cols; a.eps = eps;
+    a.sum = (uint16_t*)sum; a.lds = ld_sum; a.rstd = rstd; a.y = (uint16_t*)y; a.ldy = ld_y; a.rule = rule;
+    if (out_row) {
+        a.fmt_r = out_row->fmt; a.codes_r = (uint8_t*)out_row->codes; a.scales_r = out_row->scales; a.g4_r = out_row->scales_g4;
+        a.pitch_r = g4_pitch(rows);
+    }
+    if (out_col) {
+        a.fmt_c = out_col->fmt; a.codes_c = (uint8_t*)out_col->codes; a.scales_c = out_col->scales; a.g4_c = out_col->scales_g4;
+        a.pitch_c = g4_pitch(cols);
+    }
+    return launch_rms_norm(a, (hipStream_t)stream) == hipSuccess ? SNIP_OK : SNIP_ERR_HIP;
+}
+
+size_t snip_rms_norm_workspace_bytes(int64_t rows, int64_t cols)
+{
+    if (rows < 0 || cols <= 0) return 0;
+    return norm_workspace_bytes(rows, cols);
+}
+
+snip_status snip_rms_norm_backward(const void* dy, int64_t rows, int64_t cols, int64_t ld_dy, const void* h, int64_t ld_h,
+                                   const void* weight, snip_out_dtype weight_dtype, const float* rstd, const void* dsum,
+                                   int64_t ld_dsum, void* dx, int64_t ld_dx, float* dweight, void* workspace,
+                                   size_t workspace_bytes_, void* stream)
+{
+    snip_status st = check_norm(rows, cols, weight, weight_dtype);
+    if (st == SNIP_OK) st = check_rows(dy, rows, cols, ld_dy);
+    if (st == SNIP_OK) st = check_rows(h, rows, cols, ld_h);
+    if (st == SNIP_OK && dsum) st = check_rows(dsum, rows, cols, ld_dsum);
+    if (st == SNIP_OK) st = check_rows(dx, rows, cols, ld_dx);
+    if (st != SNIP_OK) return st;
+    if (!rstd && rows > 0) return SNIP_ERR_NULL;
+    if ((reinterpret_cast<uintptr_t>(rstd) | reinterpret_cast<uintptr_t>(dweight)) & 3u) return SNIP_ERR_LAYOUT;
+    if (dweight && rows > 0) {
+        if (!workspace || workspace_bytes_ < norm_workspace_bytes(rows, cols)) return SNIP_ERR_WORKSPACE;
+        if (!aligned16(workspace)) return SNIP_ERR_LAYOUT;
+    }
+    NormGradArgs a = {};
+    a.dy = (const uint16_t*)dy; a.lddy = ld_dy; a.h = (const uint16_t*)h; a.ldh = ld_h;
+    a.gain = weight; a.gain_fp32 = weight_dtype == SNIP_OUT_FP32; a.rstd = rstd;
+    a.dsum = (const uint16_t*)dsum; a.ldds = ld_dsum; a.dx = (uint16_t*)dx; a.lddx = ld_dx;
+    a.dgain = dweight; a.partials = dweight ? (float*)workspace : nullptr; a.rows = (int)rows; a.cols = (int)cols;
+    return launch_rms_norm_backward(a, (hipStream_t)stream) == hipSuccess ? SNIP_OK : SNIP_ERR_HIP;
 }
 
 size_t snip_noalloc_max_cols(void) { return (size_t)kNoallocMaxCols; }

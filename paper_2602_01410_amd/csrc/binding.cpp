@@ -22,6 +22,8 @@ decltype(&snip_gemm_paper) p_gemm_paper;
 decltype(&snip_quant_error_stats) p_stats;
 decltype(&snip_quant_error_stats_both) p_stats_both;
 decltype(&snip_adamw_sensitivity) p_adamw;
+decltype(&snip_rms_norm) p_rms_norm;
+decltype(&snip_rms_norm_backward) p_rms_norm_backward;
 
 PyObject *s_codes, *s_scales, *s_scales_g4, *s_rows, *s_cols, *s_fmt;      // interned attribute names
 
@@ -239,6 +241,54 @@ PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n)
     return call([&] { return p_adamw((const float*)m, (const float*)v, g, (snip_out_dtype)dt, cnt, (float)b1, (float)b2, (float)eps, (double*)o, ws, wn, s); });
 }
 
+// A bf16 matrix of the extents of `like`, or None: null.
+bool same_extents(PyObject* o, const Source& like, Source& s)
+{
+    s = {nullptr, 0, 0, 0};
+    if (o == Py_None) return true;
+    if (!source(o, s)) return false;
+    if (s.rows != like.rows || s.cols != like.cols) { PyErr_SetString(PyExc_ValueError, "expected a matrix with the extents of the input"); return false; }
+    return true;
+}
+// A contiguous vector of n elements on the GPU; `dtype`: which of the two it is (fp32 if only_fp32).  None: null.
+bool vector(PyObject* o, int64_t n, bool only_fp32, void*& p, snip_out_dtype& dtype)
+{
+    p = nullptr;
+    if (o == Py_None) return true;
+    const at::Tensor* t;
+    if (!tensor(o, t)) return false;
+    const bool fp32 = t->scalar_type() == at::kFloat;
+    if (!t->is_cuda() || !t->is_contiguous() || t->numel() != n || !(fp32 || (!only_fp32 && t->scalar_type() == at::kBFloat16))) {
+        PyErr_SetString(PyExc_ValueError, only_fp32 ? "expected a contiguous CUDA tensor of fp32, one element for each row (rstd) or column (weight)"
+                                                    : "expected a contiguous CUDA tensor of bf16 or fp32, one element for each column");
+        return false;
+    }
+    p = t->data_ptr();
+    dtype = fp32 ? SNIP_OUT_FP32 : SNIP_OUT_BF16;
+    return true;
+}
+// (x, weight, eps, residual, rule, sum, rstd, y, out_row, out_col, stream)
+PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Source x, r, h, y; int64_t rule; void *w, *rstd, *s; snip_out_dtype dt = SNIP_OUT_BF16, d32; snip_qtensor qr, qc;
+    if (!count(n, 11) || !source(a[0], x) || !vector(a[1], x.cols, false, w, dt)) return nullptr;
+    const double eps = PyFloat_AsDouble(a[2]);
+    if (PyErr_Occurred() || !same_extents(a[3], x, r) || !integer(a[4], rule) || !same_extents(a[5], x, h) || !vector(a[6], x.rows, true, rstd, d32) ||
+        !same_extents(a[7], x, y) || (a[8] != Py_None && !qtensor(a[8], qr)) || (a[9] != Py_None && !qtensor(a[9], qc)) || !stream(a[10], s))
+        return nullptr;
+    return call([&] { return p_rms_norm(x.p, x.rows, x.cols, x.ld, r.p, r.ld, w, dt, (float)eps, (snip_scale_rule)rule, h.p, h.ld, (float*)rstd, y.p, y.ld,
+                                        a[8] != Py_None ? &qr : nullptr, a[9] != Py_None ? &qc : nullptr, s); });
+}
+// (dy, h, weight, rstd, dsum, dx, dweight, workspace, stream)
+PyObject* rms_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Source dy, h, ds, dx; void *w, *rstd, *dw, *ws, *s; size_t wn; snip_out_dtype dt = SNIP_OUT_BF16, d32;
+    if (!count(n, 9) || !source(a[0], dy) || !same_extents(a[1], dy, h) || !vector(a[2], dy.cols, false, w, dt) || !vector(a[3], dy.rows, true, rstd, d32) ||
+        !same_extents(a[4], dy, ds) || !same_extents(a[5], dy, dx) || !vector(a[6], dy.cols, true, dw, d32) || !workspace(a[7], ws, wn) || !stream(a[8], s))
+        return nullptr;
+    return call([&] { return p_rms_norm_backward(dy.p, dy.rows, dy.cols, dy.ld, h.p, h.ld, w, dt, (const float*)rstd, ds.p, ds.ld, dx.p, dx.ld, (float*)dw, ws, wn, s); });
+}
+
 template <class F> bool find(void* lib, const char* name, F& f)
 {
     f = (F)dlsym(lib, name);
@@ -258,7 +308,8 @@ PyObject* bind(PyObject*, PyObject* arg)
         !find(lib, "snip_gemm_dgrad_norm", p_gemm_norm[1]) || !find(lib, "snip_gemm_wgrad_norm", p_gemm_norm[2]) ||
         !find(lib, "snip_quantize_paper", p_quantize_paper) || !find(lib, "snip_gemm_paper", p_gemm_paper) ||
         !find(lib, "snip_quant_error_stats", p_stats) || !find(lib, "snip_quant_error_stats_both", p_stats_both) ||
-        !find(lib, "snip_adamw_sensitivity", p_adamw))
+        !find(lib, "snip_adamw_sensitivity", p_adamw) || !find(lib, "snip_rms_norm", p_rms_norm) ||
+        !find(lib, "snip_rms_norm_backward", p_rms_norm_backward))
         return nullptr;
     Py_RETURN_NONE;
 }
@@ -277,7 +328,7 @@ PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t n)
 #define SNIP_FAST(name) {#name, (PyCFunction)(void (*)(void))guarded<name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"bind", bind, METH_O, nullptr}, SNIP_FAST(quantize), SNIP_FAST(quantize_both), SNIP_FAST(quantize_sr_fp4),
                          SNIP_FAST(gemm), SNIP_FAST(gemm_norm), SNIP_FAST(quantize_paper), SNIP_FAST(gemm_paper), SNIP_FAST(stats),
-                         SNIP_FAST(stats_both), SNIP_FAST(adamw), {nullptr, nullptr, 0, nullptr}};
+                         SNIP_FAST(stats_both), SNIP_FAST(adamw), SNIP_FAST(rms_norm), SNIP_FAST(rms_norm_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_snip_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,557 @@
+// RMS norm with the residual's addition and quantized outputs, and its gradient.
+//     h = bf16(x + r);   rstd = 1 / sqrt(mean(h^2) + eps);   y = h w rstd
+// y is rounded once: to bf16, and from fp32 to the FP8 / FP4 codes of 32-element blocks along rows (the operand of the forward
+// GEMM) or down columns (of the weight-gradient GEMM).  Bound by memory: 2 (4 with r) bytes per element read, 2 written for h,
+// 1 or 0.5 for the codes of each orientation.
+//
+// Rows: a row's elements stay in registers between the sum of squares and the outputs, so x and r are read once.  Columns need
+// the norms of 32 rows first: norm_col_kernel runs behind the row kernel and reads h again, with rstd.
+#include "snip_internal.h"
+#include "quant_common.h"
+
+namespace snip {
+namespace {
+
+// Scale byte of a block by the bits of its largest magnitude in fp32; 0xFF for Inf/NaN.
+template <int FMT>
+__device__ __forceinline__ unsigned scale_byte_f32(unsigned amax, int rule)
+{
+    int b = (int)amax + ((rule == 0 ? 0x7FFFFF - ((int)Fmt<FMT>::mmax << 16) : 0) - (Fmt<FMT>::emax << 23));
+    b = b < 0 ? 0 : b;
+    return amax >= 0x7F800000u ? 0xFFu : (unsigned)b >> 23;
+}
+
+__device__ __forceinline__ unsigned pack_bf16(float lo, float hi)
+{
+    return __builtin_bit_cast(unsigned, bf16x2{(__bf16)lo, (__bf16)hi});
+}
+__device__ __forceinline__ uint4 pack8(const float (&f)[8])
+{
+    return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+}
+__device__ __forceinline__ void unpack8(const uint4& v, float (&f)[8])
+{
+    unpack2(v.x, f[0], f[1]); unpack2(v.y, f[2], f[3]); unpack2(v.z, f[4], f[5]); unpack2(v.w, f[6], f[7]);
+}
+
+// Eight consecutive elements of a row from column `col` on, zeros from `cols` on.  RAGGED: cols is not a multiple of 8, and nothing
+// behind the row's last element is touched; otherwise col + 8 <= cols.
+template <bool RAGGED>
+__device__ __forceinline__ uint4 load8(const uint16_t* row, int64_t col, int64_t cols)
+{
+    if (!RAGGED || col + 8 <= cols) return *reinterpret_cast<const uint4*>(row + col);
+    unsigned w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (col + i < cols) w[i / 2] |= (unsigned)row[col + i] << (16 * (i & 1));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <bool RAGGED>
+__device__ __forceinline__ void store8(uint16_t* row, int64_t col, int64_t cols, const uint4& v)
+{
+    if (!RAGGED || col + 8 <= cols) { *reinterpret_cast<uint4*>(row + col) = v; return; }
+    const unsigned w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (col + i < cols) row[col + i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+}
+template <bool RAGGED>
+__device__ __forceinline__ void load_gain(const void* gain, bool fp32, int64_t col, int64_t cols, float (&f)[8])
+{
+    if (!fp32) { unpack8(load8<RAGGED>((const uint16_t*)gain, col, cols), f); return; }
+    const float* g = (const float*)gain + col;
+    if (!RAGGED || col + 8 <= cols) {
+        const float4 a = *reinterpret_cast<const float4*>(g), b = *reinterpret_cast<const float4*>(g + 4);
+        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = col + i < cols ? g[i] : 0.f;
+    }
+}
+
+// y = (h w) rstd: with bf16 gains the first product is exact.
+__device__ __forceinline__ float normed(float h, float w, float rstd) { return h * w * rstd; }
+
+// Codes of a block's quarter (eight elements of a lane, a quad owns the block); returns the scale byte.
+template <int FMT>
+__device__ __forceinline__ unsigned quant_quarter(const float (&y)[8], int rule, unsigned& c0, unsigned& c1)
+{
+    const unsigned byte = scale_byte_f32<FMT>(quad_max(__float_as_uint(max_abs<8>(y))), rule);
+    const float sc = scale_operand(byte);
+    if (FMT == kFP8) {
+        c0 = rule == 0 ? enc8x4<0>(y, sc, byte) : enc8x4<1>(y, sc, byte);
+        c1 = rule == 0 ? enc8x4<0>(y + 4, sc, byte) : enc8x4<1>(y + 4, sc, byte);
+    } else {
+        c0 = enc4x8(y, sc);
+        c1 = 0;
+    }
+    if (byte == 0xFFu) { c0 = 0; c1 = 0; }
+    return byte;
+}
+
+__device__ __forceinline__ float rstd_of(float sum_sq, int cols, float eps) { return 1.f / __fsqrt_rn(sum_sq / (float)cols + eps); }
+
+// Outputs of eight elements of row `row`.  All lanes of a wave come here (a block's maximum is exchanged between lanes); those
+// past the last column have zeros.
+template <bool RAGGED>
+__device__ __forceinline__ void norm_outputs(const NormArgs& a, int64_t row, int64_t col, const uint4& h, float rstd)
+{
+    float f[8], w[8];
+    unpack8(h, f);
+    const bool in = col < a.cols;
+    if (in) load_gain<RAGGED>(a.gain, a.gain_fp32, col, a.cols, w);
+    else
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = normed(f[i], w[i], rstd);
+    if (a.y && in) store8<RAGGED>(a.y + row * a.ldy, col, a.cols, pack8(f));
+    if (!RAGGED && a.codes_r) {                             // (its columns are a multiple of 32)
+        unsigned c0, c1;
+        const unsigned byte = a.fmt_r == kFP8 ? quant_quarter<kFP8>(f, a.rule, c0, c1) : quant_quarter<kFP4>(f, a.rule, c0, c1);
+        const int64_t at = row * a.cols + col;
+        if (in) {
+            if (a.fmt_r == kFP8) *reinterpret_cast<uint2*>(a.codes_r + at) = make_uint2(c0, c1);
+            else                 *reinterpret_cast<unsigned*>(a.codes_r + at / 2) = c0;
+            if ((threadIdx.x & 3) == 0) a.scales_r[at / kBlock] = (uint8_t)byte;
+        }
+        if (a.g4_r) {
+            // the bytes of four blocks, of this quad and the next three (zeros past the last column)
+            unsigned p = in ? byte : 0u;
+            p |= (unsigned)__builtin_amdgcn_update_dpp(0, (int)p, 0x104, 0xF, 0xF, true) << 8;        // lane + 4
+            p |= (unsigned)__builtin_amdgcn_update_dpp(0, (int)p, 0x108, 0xF, 0xF, true) << 16;       // lane + 8
+            if (in && (threadIdx.x & 15) == 0) *reinterpret_cast<unsigned*>(a.g4_r + ((col >> 7) * a.pitch_r + row) * 4) = p;
+        }
+    }
+}
+
+// One row by W waves, CH groups of eight elements per lane; cols is a multiple of 8.
+template <int W, int CH>
+__global__ __launch_bounds__(W == 1 ? 256 : W * 64) void norm_row_kernel(NormArgs a)
+{
+    constexpr int RPB = W == 1 ? 4 : 1;                     // rows a workgroup works on at a time
+    __shared__ float sums[2][W];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane_in_row = W == 1 ? threadIdx.x & 63 : threadIdx.x;
+    int turn = 0;
+    for (int64_t row = (int64_t)blockIdx.x * RPB + (W == 1 ? wave : 0); row < a.rows; row += (int64_t)gridDim.x * RPB, turn ^= 1) {
+        uint4 h[CH];
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            const int64_t col = ((int64_t)j * W * 64 + lane_in_row) * 8;
+            h[j] = col < a.cols ? load8<false>(a.x + row * a.ldx, col, a.cols) : make_uint4(0, 0, 0, 0);
+        }
+        if (a.r) {
+            uint4 r[CH];
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                const int64_t col = ((int64_t)j * W * 64 + lane_in_row) * 8;
+                r[j] = col < a.cols ? load8<false>(a.r + row * a.ldr, col, a.cols) : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                const int64_t col = ((int64_t)j * W * 64 + lane_in_row) * 8;
+                float f[8], g[8];
+                unpack8(h[j], f);
+                unpack8(r[j], g);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] += g[i];
+                h[j] = pack8(f);
+                if (a.sum && col < a.cols) store8<false>(a.sum + row * a.lds, col, a.cols, h[j]);
+            }
+        }
+        float s = 0.f;
+#pragma unroll
+        for (int j = 0; j < CH; ++j) { acc_sq(h[j].x, s); acc_sq(h[j].y, s); acc_sq(h[j].z, s); acc_sq(h[j].w, s); }
+        s = wave_sum(s);
+        if (W > 1) {
+            if ((threadIdx.x & 63) == 0) sums[turn][wave] = s;
+            __syncthreads();                                // (the other half of `sums` may still be read)
+            s = 0.f;
+#pragma unroll
+            for (int i = 0; i < W; ++i) s += sums[turn][i];
+        }
+        const float rstd = rstd_of(s, a.cols, a.eps);
+        if (a.rstd && lane_in_row == 0) a.rstd[row] = rstd;
+        if (a.y || a.codes_r)
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                if ((int64_t)j * W * 512 >= a.cols) break;
+                norm_outputs<false>(a, row, ((int64_t)j * W * 64 + lane_in_row) * 8, h[j], rstd);
+            }
+    }
+}
+
+// The same for rows of any length, by W waves: read twice, the second time as stored or added again (and out of cache unless the
+// row is very long).
+template <int W, bool RAGGED>
+__global__ __launch_bounds__(W * 64) void norm_any_row_kernel(NormArgs a)
+{
+    constexpr int STEP = W * 512;
+    __shared__ float sums[2][W];
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+        float s = 0.f;
+        auto element8 = [&](int64_t col, const uint16_t* r) {
+            uint4 h = load8<RAGGED>(a.x + row * a.ldx, col, a.cols);
+            if (r) {
+                float f[8], g[8];
+                unpack8(h, f);
+                unpack8(load8<RAGGED>(r + row * a.ldr, col, a.cols), g);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] += g[i];
+                h = pack8(f);
+            }
+            return h;
+        };
+        for (int64_t col = threadIdx.x * 8; col < a.cols; col += STEP) {
+            const uint4 h = element8(col, a.r);
+            if (a.sum) store8<RAGGED>(a.sum + row * a.lds, col, a.cols, h);
+            acc_sq(h.x, s); acc_sq(h.y, s); acc_sq(h.z, s); acc_sq(h.w, s);
+        }
+        s = wave_sum(s);
+        if ((threadIdx.x & 63) == 0) sums[turn][threadIdx.x >> 6] = s;
+        __syncthreads();
+        s = 0.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) s += sums[turn][i];
+        const float rstd = rstd_of(s, a.cols, a.eps);
+        if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
+        if (a.y || a.codes_r)
+            for (int64_t c0 = 0; c0 < a.cols; c0 += STEP) {
+                const int64_t col = c0 + threadIdx.x * 8;
+                // a lane reads back what it has stored itself
+                uint4 h = make_uint4(0, 0, 0, 0);
+                if (col < a.cols) h = a.sum ? load8<RAGGED>(a.sum + row * a.lds, col, a.cols) : element8(col, a.r);
+                norm_outputs<RAGGED>(a, row, col, h, rstd);
+            }
+    }
+}
+
+// Column blocks of y = h w rstd.  A workgroup's unit is 128 columns by one 128-byte line of every stored row (four row blocks
+// of FP8 codes, eight of FP4); a wave takes a row block at a time, a lane two columns, so that a block's maximum stays in the
+// lane.  The codes are turned through LDS and leave in whole lines.
+template <int FMT>
+__global__ __launch_bounds__(256) void norm_col_kernel(NormArgs a, const uint16_t* __restrict__ h, int64_t ldh)
+{
+    constexpr int RBU = FMT == kFP8 ? 4 : 8;                // row blocks of a unit
+    constexpr int WORDS = FMT == kFP8 ? 8 : 4;              // dwords of codes of a block
+    constexpr int CHUNKS = RBU * WORDS / 4;                 // 16-byte chunks of a stored row in the unit: 8
+    __shared__ uint4 stage[128 * CHUNKS];
+    __shared__ uint8_t bytes[RBU][128];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int cols = a.cols, ncg = (cols + 127) / 128, nrb = a.rows / kBlock;
+    const int units = ncg * ((nrb + RBU - 1) / RBU);
+    const int64_t out_row = FMT == kFP8 ? a.rows : a.rows / 2;
+    for (int u = blockIdx.x; u < units; u += gridDim.x) {
+        const int ru = u / ncg, c0 = (u - ru * ncg) * 128, c = c0 + 2 * lane;
+        const int nb = min(nrb - ru * RBU, RBU);
+        const bool in = c < cols;
+        float w0 = 0.f, w1 = 0.f;
+        if (in) {
+            if (a.gain_fp32) { w0 = ((const float*)a.gain)[c]; w1 = ((const float*)a.gain)[c + 1]; }
+            else unpack2(*((const unsigned*)a.gain + c / 2), w0, w1);
+        }
+        for (int k = wave; k < nb; k += 4) {
+            const int64_t row0 = (int64_t)(ru * RBU + k) * kBlock;
+            float y[2][32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                const unsigned v = in ? *reinterpret_cast<const unsigned*>(h + (row0 + i) * ldh + c) : 0u;
+                unpack2(v, y[0][i], y[1][i]);
+            }
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                const float rstd = a.rstd[row0 + i];
+                y[0][i] = normed(y[0][i], w0, rstd);
+                y[1][i] = normed(y[1][i], w1, rstd);
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const unsigned byte = scale_byte_f32<FMT>(__float_as_uint(max_abs<32>(y[s])), a.rule);
+                const float sc = scale_operand(byte);
+                unsigned q[WORDS];
+#pragma unroll
+                for (int i = 0; i < WORDS; ++i) {
+                    if (FMT == kFP8) q[i] = a.rule == 0 ? enc8x4<0>(y[s] + 4 * i, sc, byte) : enc8x4<1>(y[s] + 4 * i, sc, byte);
+                    else             q[i] = enc4x8(y[s] + 8 * i, sc);
+                    if (byte == 0xFFu) q[i] = 0;
+                }
+                // chunk i of stored row n lies at i ^ ((n / 2) & 7): lanes of a wave write to different banks
+                uint4* const line = stage + (2 * lane + s) * CHUNKS;
+#pragma unroll
+                for (int i = 0; i < WORDS / 4; ++i)
+                    line[(k * (WORDS / 4) + i) ^ (lane & 7)] = make_uint4(q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]);
+                bytes[k][2 * lane + s] = (uint8_t)byte;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int it = 0; it < 128 * CHUNKS / 256; ++it) {
+            const int n = it * (256 / CHUNKS) + threadIdx.x / CHUNKS, chunk = threadIdx.x % CHUNKS;
+            if (c0 + n < cols && chunk / (WORDS / 4) < nb)
+                *reinterpret_cast<uint4*>(a.codes_c + (c0 + n) * out_row + (int64_t)ru * 128 + chunk * 16) = stage[n * CHUNKS + (chunk ^ ((n >> 1) & 7))];
+        }
+        // scale bytes: a dword for four row blocks, zeros past the last one
+        const int n = threadIdx.x & 127, g = threadIdx.x >> 7;
+        if (g * 4 < nb && c0 + n < cols) {
+            unsigned d = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (g * 4 + k < nb) d |= (unsigned)bytes[(g * 4 + k) & (RBU - 1)][n] << (8 * k);
+            const int rb = ru * RBU + g * 4;
+            uint8_t* const to = a.scales_c + (int64_t)(c0 + n) * nrb + rb;
+            if ((nrb & 3) == 0) *reinterpret_cast<unsigned*>(to) = d;
+            else
+                for (int k = 0; k < 4 && rb + k < nrb; ++k) to[k] = (uint8_t)(d >> (8 * k));
+            if (a.g4_c) *reinterpret_cast<unsigned*>(a.g4_c + ((int64_t)(rb / 4) * a.pitch_c + c0 + n) * 4) = d;
+        }
+        __syncthreads();
+    }
+}
+
+template <int W, int CH> void launch_row(const NormArgs& a, hipStream_t s)
+{
+    const int64_t groups = W == 1 ? ((int64_t)a.rows + 3) / 4 : a.rows;
+    hipLaunchKernelGGL((norm_row_kernel<W, CH>), dim3((unsigned)(groups < kMostBlocks ? groups : kMostBlocks)), dim3(W == 1 ? 256 : W * 64), 0, s, a);
+}
+template <int W, bool RAGGED> void launch_any_row(const NormArgs& a, hipStream_t s)
+{
+    hipLaunchKernelGGL((norm_any_row_kernel<W, RAGGED>), dim3((unsigned)(a.rows < kMostBlocks ? a.rows : kMostBlocks)), dim3(W * 64), 0, s, a);
+}
+
+// ---- gradient ------------------------------------------------------------------------------------------------------------------
+// With g = dy w and h normed by rstd:   dx = rstd (g - h rstd^2 mean(g h)) + dsum,   dw = sum over rows of dy h rstd.
+// 6 (8 with dsum) bytes per element.  A lane owns the same columns of every row that its workgroup takes, so that the sums of dw stay
+// in registers until the workgroup's rows are done; then they go to a row of `partials`, and grad_sum_kernel adds those in a fixed
+// order.
+
+__device__ __forceinline__ void grad8(const float (&g)[8], const float (&h)[8], const uint4* dsum, float rstd, float coef, float (&dx)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dx[i] = rstd * fmaf(-coef, h[i], g[i]);
+    if (dsum) {
+        float d[8];
+        unpack8(*dsum, d);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dx[i] += d[i];
+    }
+}
+
+template <int W, int CH>
+__global__ __launch_bounds__(W == 1 ? 256 : W * 64) void norm_grad_kernel(NormGradArgs a)
+{
+    constexpr int RPB = W == 1 ? 4 : 1;
+    __shared__ float sums[2][W];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane_in_row = W == 1 ? threadIdx.x & 63 : threadIdx.x;
+    const int64_t first = (int64_t)blockIdx.x * RPB + (W == 1 ? wave : 0);
+    float w[CH][8], dw[CH][8];
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        const int64_t col = ((int64_t)j * W * 64 + lane_in_row) * 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[j][i] = dw[j][i] = 0.f;
+        if (col < a.cols) load_gain<false>(a.gain, a.gain_fp32, col, a.cols, w[j]);
+    }
+    int turn = 0;
+    for (int64_t row = first; row < a.rows; row += (int64_t)gridDim.x * RPB, turn ^= 1) {
+        const float rstd = a.rstd[row];
+        uint4 vy[CH], vh[CH], vd[CH];
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            const int64_t col = ((int64_t)j * W * 64 + lane_in_row) * 8;
+            const bool in = col < a.cols;
+            vy[j] = vh[j] = vd[j] = make_uint4(0, 0, 0, 0);
+            if (in) {
+                vy[j] = load8<false>(a.dy + row * a.lddy, col, a.cols);
+                vh[j] = load8<false>(a.h + row * a.ldh, col, a.cols);
+                if (a.dsum) vd[j] = load8<false>(a.dsum + row * a.ldds, col, a.cols);
+            }
+        }
+        float s = 0.f;
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            float y[8], h[8];
+            unpack8(vy[j], y);
+            unpack8(vh[j], h);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                s = fmaf(y[i] * w[j][i], h[i], s);
+                dw[j][i] = fmaf(y[i], h[i] * rstd, dw[j][i]);
+            }
+        }
+        s = wave_sum(s);
+        if (W > 1) {
+            if ((threadIdx.x & 63) == 0) sums[turn][wave] = s;
+            __syncthreads();
+            s = 0.f;
+#pragma unroll
+            for (int i = 0; i < W; ++i) s += sums[turn][i];
+        }
+        const float coef = s * rstd / (float)a.cols * rstd;
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            const int64_t col = ((int64_t)j * W * 64 + lane_in_row) * 8;
+            if (col >= a.cols) break;
+            float y[8], h[8], dx[8];
+            unpack8(vy[j], y);
+            unpack8(vh[j], h);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] *= w[j][i];
+            grad8(y, h, a.dsum ? &vd[j] : nullptr, rstd, coef, dx);
+            store8<false>(a.dx + row * a.lddx, col, a.cols, pack8(dx));
+        }
+    }
+    if (a.partials && first < a.rows)
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            const int64_t col = ((int64_t)j * W * 64 + lane_in_row) * 8;
+            if (col >= a.cols) break;
+            float4* const to = reinterpret_cast<float4*>(a.partials + first * a.pitch + col);
+            to[0] = make_float4(dw[j][0], dw[j][1], dw[j][2], dw[j][3]);
+            to[1] = make_float4(dw[j][4], dw[j][5], dw[j][6], dw[j][7]);
+        }
+}
+
+// Rows of any length: read twice, the sums of dw kept in the workgroup's row of `partials`.
+template <int W, bool RAGGED>
+__global__ __launch_bounds__(W * 64) void norm_grad_any_kernel(NormGradArgs a)
+{
+    __shared__ float sums[2][W];
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+        const float rstd = a.rstd[row];
+        float s = 0.f;
+        auto load_gh = [&](int64_t col, float (&y)[8], float (&h)[8], float (&w)[8]) {
+            unpack8(load8<RAGGED>(a.dy + row * a.lddy, col, a.cols), y);
+            unpack8(load8<RAGGED>(a.h + row * a.ldh, col, a.cols), h);
+            load_gain<RAGGED>(a.gain, a.gain_fp32, col, a.cols, w);
+        };
+        for (int64_t col = threadIdx.x * 8; col < a.cols; col += W * 512) {
+            float y[8], h[8], w[8];
+            load_gh(col, y, h, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s = fmaf(y[i] * w[i], h[i], s);
+        }
+        s = wave_sum(s);
+        if ((threadIdx.x & 63) == 0) sums[turn][threadIdx.x >> 6] = s;
+        __syncthreads();
+        s = 0.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) s += sums[turn][i];
+        const float coef = s * rstd / (float)a.cols * rstd;
+        for (int64_t col = threadIdx.x * 8; col < a.cols; col += W * 512) {
+            float y[8], h[8], w[8], dx[8];
+            load_gh(col, y, h, w);
+            if (a.partials) {
+                float4* const to = reinterpret_cast<float4*>(a.partials + blockIdx.x * a.pitch + col);       // (pitch is a multiple of 8)
+                float4 t0 = make_float4(0.f, 0.f, 0.f, 0.f), t1 = t0;
+                if (row != blockIdx.x) { t0 = to[0]; t1 = to[1]; }
+                to[0] = make_float4(fmaf(y[0], h[0] * rstd, t0.x), fmaf(y[1], h[1] * rstd, t0.y), fmaf(y[2], h[2] * rstd, t0.z), fmaf(y[3], h[3] * rstd, t0.w));
+                to[1] = make_float4(fmaf(y[4], h[4] * rstd, t1.x), fmaf(y[5], h[5] * rstd, t1.y), fmaf(y[6], h[6] * rstd, t1.z), fmaf(y[7], h[7] * rstd, t1.w));
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] *= w[i];
+            uint4 d;
+            if (a.dsum) d = load8<RAGGED>(a.dsum + row * a.ldds, col, a.cols);
+            grad8(y, h, a.dsum ? &d : nullptr, rstd, coef, dx);
+            store8<RAGGED>(a.dx + row * a.lddx, col, a.cols, pack8(dx));
+        }
+    }
+}
+
+// dw[c] = sum of partials[p][c] over p < n: 32 columns by 32 shares of the rows, added in a fixed order.
+__global__ __launch_bounds__(1024) void grad_sum_kernel(const float* __restrict__ partials, int n, int64_t pitch, int cols, float* __restrict__ dw)
+{
+    __shared__ float shares[32][33];
+    const int c = blockIdx.x * 32 + (threadIdx.x & 31), g = threadIdx.x >> 5;
+    float s = 0.f;
+    if (c < cols)
+#pragma unroll 4
+        for (int p = g; p < n; p += 32) s += partials[p * pitch + c];
+    shares[g][threadIdx.x & 31] = s;
+    __syncthreads();
+    if (g == 0 && c < cols) {
+        double t = 0.0;
+        for (int i = 0; i < 32; ++i) t += shares[i][threadIdx.x];
+        dw[c] = (float)t;
+    }
+}
+
+// Waves of a row (0: rows are read twice, by 4 or 16 waves) and workgroups by the number of columns.
+struct GradForm { int waves, groups, blocks; };
+inline GradForm grad_form(int64_t rows, int64_t cols)
+{
+    const int64_t groups = (cols + 7) / 8;
+    GradForm f;
+    f.groups = groups <= 64 ? 1 : groups <= 128 ? 2 : groups <= 256 ? 4 : groups <= 512 ? 2 : groups <= 1024 ? 4 : 2;
+    f.waves = cols % 8 != 0 || groups > 2048 ? 0 : groups <= 256 ? 1 : groups <= 1024 ? 4 : 16;
+    const int64_t most = groups <= 256 ? 256 : groups <= 1024 ? 512 : 256, want = f.waves == 1 ? (rows + 3) / 4 : rows;
+    f.blocks = (int)(want < most ? want : most);
+    return f;
+}
+inline int64_t grad_pitch(int64_t cols) { return (cols + 7) / 8 * 8; }
+inline int64_t grad_partials(const GradForm& f, int64_t rows) { const int64_t n = f.blocks * (int64_t)(f.waves == 1 ? 4 : 1); return n < rows ? n : rows; }
+
+}  // namespace
+
+hipError_t launch_rms_norm(const NormArgs& a, hipStream_t s)
+{
+    if (a.rows == 0) return hipSuccess;
+    const int groups = (a.cols + 7) / 8;
+    if (a.cols % 8 != 0) {
+        if (groups <= 1024) launch_any_row<4, true>(a, s);
+        else                launch_any_row<16, true>(a, s);
+    }
+    else if (groups <= 64) launch_row<1, 1>(a, s);
+    else if (groups <= 128) launch_row<1, 2>(a, s);
+    else if (groups <= 256) launch_row<1, 4>(a, s);
+    else if (groups <= 512) launch_row<4, 2>(a, s);
+    else if (groups <= 1024) launch_row<4, 4>(a, s);
+    else if (groups <= 2048) launch_row<16, 2>(a, s);
+    else if (groups <= 4096) launch_row<16, 4>(a, s);
+    else launch_any_row<16, false>(a, s);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !a.codes_c) return e;
+    const uint16_t* h = a.r ? a.sum : a.x;
+    const int64_t ldh = a.r ? a.lds : a.ldx;
+    const int rbu = a.fmt_c == kFP8 ? 4 : 8;
+    const int64_t units = (int64_t)((a.cols + 127) / 128) * ((a.rows / kBlock + rbu - 1) / rbu);
+    const dim3 grid((unsigned)(units < kMostBlocks ? units : kMostBlocks));
+    if (a.fmt_c == kFP8) hipLaunchKernelGGL(norm_col_kernel<kFP8>, grid, dim3(256), 0, s, a, h, ldh);
+    else                 hipLaunchKernelGGL(norm_col_kernel<kFP4>, grid, dim3(256), 0, s, a, h, ldh);
+    return hipGetLastError();
+}
+
+size_t norm_workspace_bytes(int64_t rows, int64_t cols)
+{
+    return (size_t)grad_partials(grad_form(rows, cols), rows) * (size_t)grad_pitch(cols) * sizeof(float);
+}
+
+hipError_t launch_rms_norm_backward(NormGradArgs a, hipStream_t s)
+{
+    const GradForm f = grad_form(a.rows, a.cols);
+    a.pitch = grad_pitch(a.cols);
+    const dim3 grid(f.blocks);
+    const bool wide = (a.cols + 7) / 8 > 1024;
+#define SNIP_GRAD(W, CH) hipLaunchKernelGGL((norm_grad_kernel<W, CH>), grid, dim3(W == 1 ? 256 : W * 64), 0, s, a)
+    if (a.rows == 0) ;
+    else if (f.waves == 0 && a.cols % 8 == 0) hipLaunchKernelGGL((norm_grad_any_kernel<16, false>), grid, dim3(1024), 0, s, a);
+    else if (f.waves == 0 && wide) hipLaunchKernelGGL((norm_grad_any_kernel<16, true>), grid, dim3(1024), 0, s, a);
+    else if (f.waves == 0) hipLaunchKernelGGL((norm_grad_any_kernel<4, true>), grid, dim3(256), 0, s, a);
+    else if (f.waves == 1 && f.groups == 1) SNIP_GRAD(1, 1);
+    else if (f.waves == 1 && f.groups == 2) SNIP_GRAD(1, 2);
+    else if (f.waves == 1) SNIP_GRAD(1, 4);
+    else if (f.waves == 4 && f.groups == 2) SNIP_GRAD(4, 2);
+    else if (f.waves == 4) SNIP_GRAD(4, 4);
+    else SNIP_GRAD(16, 2);
+#undef SNIP_GRAD
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !a.dgain) return e;
+    hipLaunchKernelGGL(grad_sum_kernel, dim3((a.cols + 31) / 32), dim3(1024), 0, s, a.partials, (int)grad_partials(f, a.rows), a.pitch, a.cols, a.dgain);
+    return hipGetLastError();
+}
+
+}  // namespace snip

@@ -121,6 +121,36 @@ struct AdamwArgs {
     void* workspace;      // room for kStreamWaves floats
 };
 
+// RMS norm (norm_kernels.hip); absent outputs are null.
+struct NormArgs {
+    const uint16_t* x; int64_t ldx;
+    const uint16_t* r; int64_t ldr;          // residual
+    const void* gain; int gain_fp32;
+    int rows, cols;
+    float eps;
+    uint16_t* sum; int64_t lds;              // may be x or r itself
+    float* rstd;
+    uint16_t* y; int64_t ldy;
+    int rule, fmt_r, fmt_c;
+    uint8_t *codes_r, *scales_r, *g4_r; int64_t pitch_r;
+    uint8_t *codes_c, *scales_c, *g4_c; int64_t pitch_c;
+};
+hipError_t launch_rms_norm(const NormArgs& a, hipStream_t s);
+struct NormGradArgs {
+    const uint16_t* dy; int64_t lddy;
+    const uint16_t* h; int64_t ldh;
+    const void* gain; int gain_fp32;
+    const float* rstd;
+    const uint16_t* dsum; int64_t ldds;      // may be null
+    uint16_t* dx; int64_t lddx;
+    float* dgain;                            // both or neither
+    float* partials;
+    int rows, cols;
+    int64_t pitch = 0;                       // of `partials`
+};
+size_t norm_workspace_bytes(int64_t rows, int64_t cols);
+hipError_t launch_rms_norm_backward(NormGradArgs a, hipStream_t s);
+
 // The paper's own recipe (real-valued scale per 1x128 tile or 128x128 block): quantize (stats == nullptr)
 // or statistics of both formats (stats != nullptr; codes / scales unused).
 struct PaperArgs {

@@ -10,7 +10,7 @@ from __future__ import annotations
 import ctypes
 import os
 from dataclasses import dataclass
-from typing import Optional, Sequence
+from typing import NamedTuple, Optional, Sequence
 
 import torch
 
@@ -30,7 +30,8 @@ EXPORTS = ("snip_qtensor_code_bytes", "snip_qtensor_scale_bytes", "snip_qtensor_
            "snip_loss_divergence", "snip_quantize_sr_fp4", "snip_quantize_both", "snip_adamw_sensitivity", "snip_weight_divergence",
            "snip_paper_scale_bytes", "snip_paper_workspace_bytes", "snip_quantize_paper",
            "snip_quant_error_stats_paper", "snip_gemm_paper", "snip_quant_error_stats_both",
-           "snip_noalloc_max_cols", "snip_quant_error_stats_noalloc")
+           "snip_noalloc_max_cols", "snip_quant_error_stats_noalloc",
+           "snip_rms_norm", "snip_rms_norm_backward", "snip_rms_norm_workspace_bytes")
 
 
 class _PTensorC(ctypes.Structure):
@@ -132,6 +133,13 @@ def _lib():
         lib.snip_noalloc_max_cols.argtypes = []
         lib.snip_quant_error_stats_noalloc.restype = ci
         lib.snip_quant_error_stats_noalloc.argtypes = [vp, i64, i64, i64, ci, ci, vp, vp, vp]
+        qp = ctypes.POINTER(_QTensorC)
+        lib.snip_rms_norm.restype = ci
+        lib.snip_rms_norm.argtypes = [vp, i64, i64, i64, vp, i64, vp, ci, cf, ci, vp, i64, vp, vp, i64, qp, qp, vp]
+        lib.snip_rms_norm_workspace_bytes.restype = sz
+        lib.snip_rms_norm_workspace_bytes.argtypes = [i64, i64]
+        lib.snip_rms_norm_backward.restype = ci
+        lib.snip_rms_norm_backward.argtypes = [vp, i64, i64, i64, vp, i64, vp, ci, vp, vp, i64, vp, i64, vp, vp, sz, vp]
         lib.snip_status_string.restype = ctypes.c_char_p
         lib.snip_status_string.argtypes = [ci]
         _handle = lib
@@ -467,3 +475,68 @@ def snip_quant_error_stats_noalloc(x: torch.Tensor, axis: int, rule: int, out: t
                                                  per_line.data_ptr() if per_line is not None else None,
                                                  _stream(stream)), "snip_quant_error_stats_noalloc")
     return out
+
+
+class RmsNorm(NamedTuple):
+    """Outputs of snip_rms_norm; None where one was not asked for."""
+    y: Optional[torch.Tensor]        # bf16 [rows, cols]
+    sum: Optional[torch.Tensor]      # bf16 [rows, cols]: x + residual
+    rstd: Optional[torch.Tensor]     # fp32 [rows]
+    row: Optional[QTensor]           # y quantized along rows
+    col: Optional[QTensor]           # y quantized down columns
+
+
+def _alloc_rows(rows: int, cols: int, device) -> torch.Tensor:
+    """bf16 matrix whose rows start on 16 bytes."""
+    return torch.empty((rows, (cols + 7) // 8 * 8), dtype=torch.bfloat16, device=device)[:, :cols]
+
+
+def snip_rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: Optional[torch.Tensor] = None,
+                  sum: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
+                  fmt_row: Optional[int] = None, fmt_col: Optional[int] = None, out_row: Optional[QTensor] = None,
+                  out_col: Optional[QTensor] = None, rule: int = NO_OVERFLOW, stream=None) -> RmsNorm:
+    """y = h * weight / sqrt(mean(h^2) + eps) with h = x + residual.  Outputs are what is passed in; fmt_row / fmt_col ask for a
+    quantized one that is allocated here, and without any of these y is.  sum (with a residual) and rstd are always delivered, allocated if
+    they are not passed; x or residual may be passed as sum."""
+    if y is None and out_row is None and out_col is None and fmt_row is None and fmt_col is None or sum is None and residual is not None \
+            or rstd is None or (fmt_row is not None and out_row is None) or (fmt_col is not None and out_col is None):
+        _, rows, cols, _ = _src(x)
+        with _alloc_on(stream):
+            if fmt_row is not None and out_row is None:
+                out_row = alloc_qtensor(rows, cols, fmt_row, x.device)
+            if fmt_col is not None and out_col is None:
+                out_col = alloc_qtensor(cols, rows, fmt_col, x.device)
+            if y is None and out_row is None and out_col is None:
+                y = _alloc_rows(rows, cols, x.device)
+            if sum is None and residual is not None:
+                sum = _alloc_rows(rows, cols, x.device)
+            if rstd is None:
+                rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
+    status = _nat().rms_norm(x, weight, eps, residual, rule, sum, rstd, y, out_row, out_col, _handle_of(stream))
+    if status:
+        raise SnipError(status, "snip_rms_norm")
+    return RmsNorm(y, sum, rstd, out_row, out_col)
+
+
+def rms_norm_workspace_bytes(rows: int, cols: int) -> int:
+    return int(_lib().snip_rms_norm_workspace_bytes(rows, cols))
+
+
+def snip_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, rstd: torch.Tensor,
+                           dsum: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
+                           dweight: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """Gradients (dx bf16, dweight fp32) of snip_rms_norm from that of y; h: the forward call's sum, or its x without a residual; dsum: the
+    gradient that reaches h past the norm.  dx may be dy or dsum."""
+    if dx is None or dweight is None or workspace is None:
+        _, rows, cols, _ = _src(dy)
+        with _alloc_on(stream):
+            if dx is None:
+                dx = _alloc_rows(rows, cols, dy.device)
+            if dweight is None:
+                dweight = torch.empty(cols, dtype=torch.float32, device=dy.device)
+            if workspace is None:
+                workspace = torch.empty(rms_norm_workspace_bytes(rows, cols), dtype=torch.uint8, device=dy.device)
+    status = _nat().rms_norm_backward(dy, h, weight, rstd, dsum, dx, dweight, workspace, _handle_of(stream))
+    if status:
+        raise SnipError(status, "snip_rms_norm_backward")
+    return dx, dweight

@@ -375,6 +375,47 @@ snip_status snip_rms_norm_backward(const void* dy, int64_t rows, int64_t cols, i
                                    const void* dsum, int64_t ld_dsum, void* dx, int64_t ld_dx, float* dweight,
                                    void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- AdamW step ------------------------------------------------------------------------- */
+/* One parameter tensor.  Arrays are contiguous and may start at any element.
+ *   param  : device, fp32 [n], the master weights, updated.
+ *   grad   : device, [n], fp32 or bf16 (grad_dtype): the dW of a wgrad call, the dweight of a norm.
+ *   m, v   : device, the moments, updated; zeros before the first step.  fp32 [n], or, where m_scale and v_scale are
+ *            given, 8 bits per element in groups of 128 (the last one may be shorter):
+ *              m       : E4M3 numbers; the moment is number * m_scale[i / 128]
+ *              v       : unsigned numbers c of 4 exponent and 4 mantissa bits, value (c >> 4 ? 2^((c >> 4) - 15) (1 + (c & 15) / 16) :
+ *                        (c & 15) 2^-18), i.e. the half-precision number of bits c << 6; the moment is (value * v_scale[i / 128])^2
+ *   copy   : device, bf16 [n], the new param rounded to nearest even, what the quantize calls read; or NULL.
+ *   m_scale, v_scale: device, fp32 [ceil(n / 128)], both or neither.
+ *   n      : 0 <= n < 2^34. */
+typedef struct {
+    float*      param;
+    const void* grad;
+    void*       m;
+    void*       v;
+    void*       copy;
+    float*      m_scale;
+    float*      v_scale;
+    int64_t     n;
+    float       weight_decay;
+    int32_t     grad_dtype;      /* snip_out_dtype */
+} snip_adamw_tensor;
+
+/* AdamW with decoupled weight decay over `count` tensors (host array), 40 of them per launch:
+ *     g = grad * *grad_scale;   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2
+ *     param = param (1 - lr weight_decay) - lr / (1 - beta1^step) m / (sqrt(v / (1 - beta2^step)) + eps)
+ * in fp32 (the coefficients formed in double), one rounding per operation.  param is updated with the moments before they are rounded to 8 bits.
+ *   step       : counts from 1.  It and lr are arguments of the launch: a captured graph repeats them.
+ *   grad_scale : device, one fp32 (a clipping coefficient, the inverse of a loss scale), or NULL for 1.
+ *   seed       : moments of 8 bits: numbers of sqrt(v) are rounded stochastically, up where the bits that are dropped and 16
+ *                random ones carry; element i of tensor k takes bits 16 (i mod 4) on of the 64 of Threefry-2x32-20 (counter = (i
+ *                div 4, k), key = seed; words and counter as for snip_quantize_sr_fp4).  Take a fresh seed for every step.  Numbers of m are
+ *                rounded to nearest even.  What is not zero keeps a number above zero.
+ * Scales are largest / 448 (m) and largest / 1.9375 (sqrt(v)), as products with the rounded reciprocals; a group whose scale would be
+ * below 2^-126 becomes zero, and one with an infinity or NaN becomes NaN altogether.
+ * beta1, beta2 in [0, 1), eps >= 0, lr and weight_decay finite, step >= 1 (SNIP_ERR_FORMAT otherwise). */
+snip_status snip_adamw_step(const snip_adamw_tensor* tensors, int32_t count, double lr, double beta1, double beta2,
+                            double eps, int64_t step, const float* grad_scale, uint64_t seed, void* stream);
+
 /* ---- quantization-error statistics (Sec. 3.1 Step 1; row-wise form: Sec. 5.3) -------- */
 
 /* One read of a bf16 matrix; for blocks along `axis` produces the squared Frobenius norm of x

@@ -496,6 +496,55 @@ snip_status snip_rms_norm_backward(const void* dy, int64_t rows, int64_t cols, i
     return launch_rms_norm_backward(a, (hipStream_t)stream) == hipSuccess ? SNIP_OK : SNIP_ERR_HIP;
 }
 
+snip_status snip_adamw_step(const snip_adamw_tensor* tensors, int32_t count, double lr, double beta1, double beta2,
+                            double eps, int64_t step, const float* grad_scale, uint64_t seed, void* stream)
+{
+    if (count < 0 || step < 1) return count < 0 ? SNIP_ERR_SHAPE : SNIP_ERR_FORMAT;
+    if (!tensors && count > 0) return SNIP_ERR_NULL;
+    if (!(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0 && eps >= 0.0) || !std::isfinite(eps) || !std::isfinite(lr)) return SNIP_ERR_FORMAT;
+    if (reinterpret_cast<uintptr_t>(grad_scale) & 3u) return SNIP_ERR_LAYOUT;
+    for (int32_t i = 0; i < count; ++i) {
+        const snip_adamw_tensor& t = tensors[i];
+        if (t.n < 0 || t.n >= (int64_t)1 << 34) return SNIP_ERR_SHAPE;
+        if (t.grad_dtype != SNIP_OUT_BF16 && t.grad_dtype != SNIP_OUT_FP32) return SNIP_ERR_FORMAT;
+        if (!std::isfinite(t.weight_decay)) return SNIP_ERR_FORMAT;
+        if (t.n == 0) continue;
+        if (!t.param || !t.grad || !t.m || !t.v || !t.m_scale != !t.v_scale) return SNIP_ERR_NULL;
+        const uintptr_t fp32 = reinterpret_cast<uintptr_t>(t.param) | reinterpret_cast<uintptr_t>(t.m_scale) | reinterpret_cast<uintptr_t>(t.v_scale) |
+                               (t.m_scale ? 0 : reinterpret_cast<uintptr_t>(t.m) | reinterpret_cast<uintptr_t>(t.v)) |
+                               (t.grad_dtype == SNIP_OUT_FP32 ? reinterpret_cast<uintptr_t>(t.grad) : 0);
+        if ((fp32 & 3u) || ((reinterpret_cast<uintptr_t>(t.copy) | reinterpret_cast<uintptr_t>(t.grad)) & 1u)) return SNIP_ERR_LAYOUT;
+    }
+    AdamwStepArgs a = {};
+    a.beta1 = (float)beta1; a.rest1 = (float)(1.0 - beta1); a.beta2 = (float)beta2; a.rest2 = (float)(1.0 - beta2);
+    a.step_size = (float)(lr / (1.0 - std::pow(beta1, (double)step)));
+    a.root_scale = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
+    a.eps = (float)eps; a.grad_scale = grad_scale; a.seed = make_uint2((unsigned)seed, (unsigned)(seed >> 32));
+    for (int small = 0; small < 2; ++small) {
+        int64_t chunks = 0;
+        a.count = 0;
+        auto launch = [&] {
+            a.chunks = (unsigned)chunks;
+            const hipError_t e = launch_adamw_step(a, small != 0, (hipStream_t)stream);
+            a.count = 0;
+            chunks = 0;
+            return e == hipSuccess;
+        };
+        for (int32_t i = 0; i < count; ++i) {
+            const snip_adamw_tensor& t = tensors[i];
+            if (t.n == 0 || (t.m_scale != nullptr) != (small != 0)) continue;
+            AdamwStepTensor& d = a.t[a.count];
+            d.p = t.param; d.g = t.grad; d.m = t.m; d.v = t.v; d.copy = (uint16_t*)t.copy; d.m_scale = t.m_scale; d.v_scale = t.v_scale; d.n = t.n;
+            d.keep = (float)(1.0 - lr * t.weight_decay); d.g_bf16 = t.grad_dtype == SNIP_OUT_BF16; d.index = (unsigned)i;
+            a.first[a.count++] = (unsigned)chunks;
+            chunks += adamw_step_chunks(t.n);
+            if (a.count == kStepTensors && !launch()) return SNIP_ERR_HIP;
+        }
+        if (a.count > 0 && !launch()) return SNIP_ERR_HIP;
+    }
+    return SNIP_OK;
+}
+
 size_t snip_noalloc_max_cols(void) { return (size_t)kNoallocMaxCols; }
 
 snip_status snip_quant_error_stats_noalloc(const void* x, int64_t rows, int64_t cols, int64_t ld, snip_axis axis,

@@ -8,6 +8,7 @@
 #include <c10/hip/HIPStream.h>
 #include <dlfcn.h>
 #include <cstring>
+#include <vector>
 #include "../../include/snip.h"
 
 namespace {
@@ -24,8 +25,10 @@ decltype(&snip_quant_error_stats_both) p_stats_both;
 decltype(&snip_adamw_sensitivity) p_adamw;
 decltype(&snip_rms_norm) p_rms_norm;
 decltype(&snip_rms_norm_backward) p_rms_norm_backward;
+decltype(&snip_adamw_step) p_adamw_step;
 
 PyObject *s_codes, *s_scales, *s_scales_g4, *s_rows, *s_cols, *s_fmt;      // interned attribute names
+PyObject *s_param, *s_grad, *s_m, *s_v, *s_copy, *s_m_scale, *s_v_scale, *s_weight_decay;
 
 // Every helper returns false (or -1) with a Python exception set when an argument is not what it should be.
 bool tensor(PyObject* o, const at::Tensor*& t)
@@ -259,7 +262,7 @@ bool vector(PyObject* o, int64_t n, bool only_fp32, void*& p, snip_out_dtype& dt
     if (!tensor(o, t)) return false;
     const bool fp32 = t->scalar_type() == at::kFloat;
     if (!t->is_cuda() || !t->is_contiguous() || t->numel() != n || !(fp32 || (!only_fp32 && t->scalar_type() == at::kBFloat16))) {
-        PyErr_SetString(PyExc_ValueError, only_fp32 ? "expected a contiguous CUDA tensor of fp32, one element for each row (rstd) or column (weight)"
+        PyErr_SetString(PyExc_ValueError, only_fp32 ? "expected a contiguous CUDA tensor of fp32, with as many elements as the call has rows, columns or scalars"
                                                     : "expected a contiguous CUDA tensor of bf16 or fp32, one element for each column");
         return false;
     }
@@ -289,6 +292,66 @@ PyObject* rms_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n)
     return call([&] { return p_rms_norm_backward(dy.p, dy.rows, dy.cols, dy.ld, h.p, h.ld, w, dt, (const float*)rstd, ds.p, ds.ld, dx.p, dx.ld, (float*)dw, ws, wn, s); });
 }
 
+// An attribute of `o`: a contiguous tensor on the GPU of n elements (n < 0: of any number, which n becomes) of one of two types, or None
+// where that may be: null.
+bool array(PyObject* o, PyObject* name, at::ScalarType type, at::ScalarType or_type, bool optional, int64_t& n, void*& p, at::ScalarType* found = nullptr)
+{
+    p = nullptr;
+    PyObject* v = PyObject_GetAttr(o, name);
+    if (!v) return false;
+    bool ok = optional && v == Py_None;
+    const at::Tensor* t;
+    if (!ok && tensor(v, t)) {
+        if (n < 0) n = t->numel();
+        ok = t->is_cuda() && t->is_contiguous() && t->numel() == n && (t->scalar_type() == type || t->scalar_type() == or_type);
+        if (ok) { p = t->data_ptr(); if (found) *found = t->scalar_type(); }
+        else PyErr_Format(PyExc_ValueError, "%U: expected a contiguous CUDA tensor of %s%s%s, %lld elements", name, c10::toString(type), type == or_type ? "" : " or ",
+                          type == or_type ? "" : c10::toString(or_type), (long long)n);
+    }
+    Py_DECREF(v);
+    return ok;
+}
+bool adamw_tensor(PyObject* o, snip_adamw_tensor& t)
+{
+    void *p, *g, *m, *v, *c, *ms, *vs;
+    at::ScalarType gt, mt;
+    t.n = -1;
+    if (!array(o, s_param, at::kFloat, at::kFloat, false, t.n, p) || !array(o, s_grad, at::kFloat, at::kBFloat16, false, t.n, g, &gt) ||
+        !array(o, s_m, at::kFloat, at::kByte, false, t.n, m, &mt) || !array(o, s_v, mt, mt, false, t.n, v) ||
+        !array(o, s_copy, at::kBFloat16, at::kBFloat16, true, t.n, c))
+        return false;
+    const bool small = mt == at::kByte;
+    int64_t groups = small ? (t.n + 127) / 128 : -1;
+    if (!array(o, s_m_scale, at::kFloat, at::kFloat, !small, groups, ms) || !array(o, s_v_scale, at::kFloat, at::kFloat, !small, groups, vs)) return false;
+    if (!small && (ms || vs)) { PyErr_SetString(PyExc_ValueError, "scales belong to moments of 8 bits"); return false; }
+    PyObject* d = PyObject_GetAttr(o, s_weight_decay);
+    if (!d) return false;
+    t.weight_decay = (float)PyFloat_AsDouble(d);
+    Py_DECREF(d);
+    t.param = (float*)p; t.grad = g; t.m = m; t.v = v; t.copy = c; t.m_scale = (float*)ms; t.v_scale = (float*)vs;
+    t.grad_dtype = gt == at::kFloat ? SNIP_OUT_FP32 : SNIP_OUT_BF16;
+    return !PyErr_Occurred();
+}
+// (tensors, lr, beta1, beta2, eps, step, grad_scale, seed, stream)
+PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (!count(n, 9)) return nullptr;
+    PyObject* seq = PySequence_Fast(a[0], "expected a sequence of tensors with their moments");
+    if (!seq) return nullptr;
+    const Py_ssize_t len = PySequence_Fast_GET_SIZE(seq);
+    std::vector<snip_adamw_tensor> ts((size_t)len);
+    bool ok = true;
+    for (Py_ssize_t i = 0; ok && i < len; ++i) ok = adamw_tensor(PySequence_Fast_GET_ITEM(seq, i), ts[(size_t)i]);
+    Py_DECREF(seq);                                 // (the caller's sequence keeps the objects)
+    if (!ok) return nullptr;
+    const double lr = PyFloat_AsDouble(a[1]), b1 = PyFloat_AsDouble(a[2]), b2 = PyFloat_AsDouble(a[3]), eps = PyFloat_AsDouble(a[4]);
+    int64_t step; void *gs, *s; snip_out_dtype d32;
+    if (PyErr_Occurred() || !integer(a[5], step) || !vector(a[6], 1, true, gs, d32)) return nullptr;
+    const unsigned long long seed = PyLong_AsUnsignedLongLong(a[7]);
+    if ((seed == (unsigned long long)-1 && PyErr_Occurred()) || !stream(a[8], s)) return nullptr;
+    return call([&] { return p_adamw_step(ts.data(), (int32_t)len, lr, b1, b2, eps, step, (const float*)gs, seed, s); });
+}
+
 template <class F> bool find(void* lib, const char* name, F& f)
 {
     f = (F)dlsym(lib, name);
@@ -309,7 +372,7 @@ PyObject* bind(PyObject*, PyObject* arg)
         !find(lib, "snip_quantize_paper", p_quantize_paper) || !find(lib, "snip_gemm_paper", p_gemm_paper) ||
         !find(lib, "snip_quant_error_stats", p_stats) || !find(lib, "snip_quant_error_stats_both", p_stats_both) ||
         !find(lib, "snip_adamw_sensitivity", p_adamw) || !find(lib, "snip_rms_norm", p_rms_norm) ||
-        !find(lib, "snip_rms_norm_backward", p_rms_norm_backward))
+        !find(lib, "snip_rms_norm_backward", p_rms_norm_backward) || !find(lib, "snip_adamw_step", p_adamw_step))
         return nullptr;
     Py_RETURN_NONE;
 }
@@ -328,7 +391,7 @@ PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t n)
 #define SNIP_FAST(name) {#name, (PyCFunction)(void (*)(void))guarded<name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"bind", bind, METH_O, nullptr}, SNIP_FAST(quantize), SNIP_FAST(quantize_both), SNIP_FAST(quantize_sr_fp4),
                          SNIP_FAST(gemm), SNIP_FAST(gemm_norm), SNIP_FAST(quantize_paper), SNIP_FAST(gemm_paper), SNIP_FAST(stats),
-                         SNIP_FAST(stats_both), SNIP_FAST(adamw), SNIP_FAST(rms_norm), SNIP_FAST(rms_norm_backward), {nullptr, nullptr, 0, nullptr}};
+                         SNIP_FAST(stats_both), SNIP_FAST(adamw), SNIP_FAST(rms_norm), SNIP_FAST(rms_norm_backward), SNIP_FAST(adamw_step), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_snip_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -341,5 +404,13 @@ PyMODINIT_FUNC PyInit__snip_binding(void)
     s_rows = PyUnicode_InternFromString("rows");
     s_cols = PyUnicode_InternFromString("cols");
     s_fmt = PyUnicode_InternFromString("fmt");
+    s_param = PyUnicode_InternFromString("param");
+    s_grad = PyUnicode_InternFromString("grad");
+    s_m = PyUnicode_InternFromString("m");
+    s_v = PyUnicode_InternFromString("v");
+    s_copy = PyUnicode_InternFromString("copy");
+    s_m_scale = PyUnicode_InternFromString("m_scale");
+    s_v_scale = PyUnicode_InternFromString("v_scale");
+    s_weight_decay = PyUnicode_InternFromString("weight_decay");
     return PyModule_Create(&module);
 }

@@ -89,7 +89,7 @@ __device__ __forceinline__ unsigned quant_quarter(const float (&y)[8], int rule,
     return byte;
 }
 
-__device__ __forceinline__ float rstd_of(float sum_sq, int cols, float eps) { return 1.f / __fsqrt_rn(sum_sq / (float)cols + eps); }
+__device__ __forceinline__ float rstd_of(float sum_sq, int cols, float eps) { return 1.f / __builtin_sqrtf(sum_sq / (float)cols + eps); }
 
 // Outputs of eight elements of row `row`.  All lanes of a wave come here (a block's maximum is exchanged between lanes); those
 // past the last column have zeros.

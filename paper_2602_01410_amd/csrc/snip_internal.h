@@ -121,6 +121,31 @@ struct AdamwArgs {
     void* workspace;      // room for kStreamWaves floats
 };
 
+// An AdamW step over tensors (optim_step.hip), all with moments of 32 bits or all with 8; the tensors of a launch travel with its arguments.
+struct AdamwStepTensor {
+    float* p; const void* g; void* m; void* v;
+    uint16_t* copy;                          // may be null
+    float *m_scale, *v_scale;                // moments of 8 bits: [ceil(n / 128)]
+    int64_t n;
+    float keep;                              // 1 - lr * decay
+    int g_bf16;
+    unsigned index;                          // in the caller's list
+};
+constexpr int kStepTensors = 40;             // (kernel arguments stay below 4 KB)
+struct AdamwStepArgs {
+    AdamwStepTensor t[kStepTensors];
+    unsigned first[kStepTensors];            // chunks before each tensor's
+    int count;
+    unsigned chunks;
+    float beta1, rest1, beta2, rest2;        // rest: 1 - beta
+    float step_size, root_scale, eps;        // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+    const float* grad_scale;                 // device, or null
+    uint2 seed;
+};
+static_assert(sizeof(AdamwStepArgs) <= 4096, "kernel arguments");
+int64_t adamw_step_chunks(int64_t n);
+hipError_t launch_adamw_step(const AdamwStepArgs& a, bool small, hipStream_t s);
+
 // RMS norm (norm_kernels.hip); absent outputs are null.
 struct NormArgs {
     const uint16_t* x; int64_t ldx;

@@ -31,7 +31,7 @@ EXPORTS = ("snip_qtensor_code_bytes", "snip_qtensor_scale_bytes", "snip_qtensor_
            "snip_paper_scale_bytes", "snip_paper_workspace_bytes", "snip_quantize_paper",
            "snip_quant_error_stats_paper", "snip_gemm_paper", "snip_quant_error_stats_both",
            "snip_noalloc_max_cols", "snip_quant_error_stats_noalloc",
-           "snip_rms_norm", "snip_rms_norm_backward", "snip_rms_norm_workspace_bytes")
+           "snip_rms_norm", "snip_rms_norm_backward", "snip_rms_norm_workspace_bytes", "snip_adamw_step")
 
 
 class _PTensorC(ctypes.Structure):
@@ -140,6 +140,8 @@ def _lib():
         lib.snip_rms_norm_workspace_bytes.argtypes = [i64, i64]
         lib.snip_rms_norm_backward.restype = ci
         lib.snip_rms_norm_backward.argtypes = [vp, i64, i64, i64, vp, i64, vp, ci, vp, vp, i64, vp, i64, vp, vp, sz, vp]
+        lib.snip_adamw_step.restype = ci
+        lib.snip_adamw_step.argtypes = [vp, ctypes.c_int32, cd, cd, cd, cd, i64, vp, ctypes.c_uint64, vp]
         lib.snip_status_string.restype = ctypes.c_char_p
         lib.snip_status_string.argtypes = [ci]
         _handle = lib
@@ -540,3 +542,35 @@ def snip_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tens
     if status:
         raise SnipError(status, "snip_rms_norm_backward")
     return dx, dweight
+
+
+@dataclass
+class AdamwTensor:
+    """A parameter tensor with its gradient and moments, all of one number of elements; see snip_adamw_tensor in the header."""
+    param: torch.Tensor                      # fp32
+    grad: torch.Tensor                       # fp32 or bf16
+    m: torch.Tensor                          # fp32, or uint8 with m_scale
+    v: torch.Tensor                          # fp32, or uint8 with v_scale
+    copy: Optional[torch.Tensor] = None      # bf16, the new param rounded
+    weight_decay: float = 0.0
+    m_scale: Optional[torch.Tensor] = None   # fp32 [ceil(n / 128)]
+    v_scale: Optional[torch.Tensor] = None
+
+
+def alloc_adamw_state(param: torch.Tensor, grad: torch.Tensor, bits: int = 32, copy: Optional[torch.Tensor] = None,
+                      weight_decay: float = 0.0) -> AdamwTensor:
+    """A tensor before its first step: moments of zero, in 32 or 8 bits."""
+    if bits not in (8, 32):
+        raise ValueError("moments have 8 or 32 bits")
+    m, v = (torch.zeros(param.shape, dtype=torch.uint8 if bits == 8 else torch.float32, device=param.device) for _ in range(2))
+    scales = [torch.zeros((param.numel() + 127) // 128, dtype=torch.float32, device=param.device) for _ in range(2)] if bits == 8 else [None, None]
+    return AdamwTensor(param, grad, m, v, copy, weight_decay, *scales)
+
+
+def snip_adamw_step(tensors: Sequence[AdamwTensor], lr: float, beta1: float, beta2: float, eps: float, step: int,
+                    grad_scale: Optional[torch.Tensor] = None, seed: int = 0, stream=None) -> None:
+    """One AdamW step over all tensors; `step` counts from 1, `grad_scale` is an fp32 tensor of one element, `seed` (64 bit, a fresh one every
+    step) selects the random numbers by which 8-bit moments are rounded."""
+    status = _nat().adamw_step(tensors, lr, beta1, beta2, eps, step, grad_scale, int(seed) & (2 ** 64 - 1), _handle_of(stream))
+    if status:
+        raise SnipError(status, "snip_adamw_step")

@@ -416,6 +416,20 @@ typedef struct {
 snip_status snip_adamw_step(const snip_adamw_tensor* tensors, int32_t count, double lr, double beta1, double beta2,
                             double eps, int64_t step, const float* grad_scale, uint64_t seed, void* stream);
 
+/* ---- few tokens against quantized weights ----------------------------------------------- */
+/* Y_i [m, n_i] = X [m, k] * W_i [n_i, k]^T for `count` weights that share X (q, k and v; gate and up), X in bf16 and not quantized: what
+ * a model generates with, a token of each sequence at a time.
+ *   x    : device, bf16 [m][ld], 16-byte aligned, ld >= k and a multiple of 8.
+ *   w    : host array; quantize(W, ROW) of every weight (FP4 or FP8, formats may differ), all with cols == k (SNIP_ERR_LAYOUT
+ *          otherwise); scales_g4 is not used.
+ *   y    : host array of device pointers; Y_i is row-major with leading dimension ld_y[i], 16-byte aligned rows as for the GEMMs
+ *          (ld_y is not read for a single token).
+ * Weights become bf16 (exactly; numbers beyond bf16's range become infinite or subnormal), products are exact and sums fp32, added in
+ * a fixed order.  A scale byte of 0xFF makes its row NaN.  Meant for up to 64 tokens (any number is served, 64 at a time, weights
+ * read anew for each); the calls above are for more. */
+snip_status snip_gemv(const void* x, int64_t m, int64_t k, int64_t ld, const snip_qtensor* w, void* const* y,
+                      const int64_t* ld_y, int32_t count, snip_out_dtype out_dtype, void* stream);
+
 /* ---- quantization-error statistics (Sec. 3.1 Step 1; row-wise form: Sec. 5.3) -------- */
 
 /* One read of a bf16 matrix; for blocks along `axis` produces the squared Frobenius norm of x

@@ -20,7 +20,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-Xclang", "-target-featu
 PRELOAD = ["-mllvm", "-amdgpu-kernarg-preload-count=16"]
 NO_PRELOAD = ("gemm_fast.hip",)
 SOURCES = ("api.hip", "quant_kernels.hip", "gemm.hip", "gemm_fast.hip", "gemm_small.hip", "optim_kernels.hip", "paper_kernels.hip", "gemm_paper.hip", "gemm_paper_wide.hip",
-           "norm_kernels.hip", "optim_step.hip")
+           "norm_kernels.hip", "optim_step.hip", "gemv.hip")
 
 
 def binding_command():

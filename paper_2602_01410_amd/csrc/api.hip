@@ -545,6 +545,37 @@ snip_status snip_adamw_step(const snip_adamw_tensor* tensors, int32_t count, dou
     return SNIP_OK;
 }
 
+snip_status snip_gemv(const void* x, int64_t m, int64_t k, int64_t ld, const snip_qtensor* w, void* const* y,
+                      const int64_t* ld_y, int32_t count, snip_out_dtype out_dtype, void* stream)
+{
+    if (out_dtype != SNIP_OUT_BF16 && out_dtype != SNIP_OUT_FP32) return SNIP_ERR_FORMAT;
+    if (m < 0 || k <= 0 || k % 32 != 0 || count < 0 || m >= (int64_t)1 << 20 || k >= (int64_t)1 << 31) return SNIP_ERR_SHAPE;
+    snip_status st = check_rows(x, m, k, ld);
+    if (st != SNIP_OK) return st;
+    if ((!w || !y || !ld_y) && count > 0) return SNIP_ERR_NULL;
+    for (int32_t i = 0; i < count; ++i) {
+        if ((st = check_qtensor(&w[i])) != SNIP_OK) return st;
+        if (w[i].cols != k) return SNIP_ERR_LAYOUT;
+        if (w[i].rows == 0) continue;
+        if (!y[i] && m > 0) return SNIP_ERR_NULL;
+        if (m > 1 && ld_y[i] < w[i].rows) return SNIP_ERR_SHAPE;                 // (a single row has no pitch)
+        if (!aligned16(y[i]) || (m > 1 && ld_y[i] % (out_dtype == SNIP_OUT_BF16 ? 8 : 4) != 0)) return SNIP_ERR_LAYOUT;
+    }
+    GemvArgs a = {};
+    a.x = (const uint16_t*)x; a.ldx = ld; a.m = (int)m; a.k = (int)k; a.out_fp32 = out_dtype == SNIP_OUT_FP32;
+    for (int32_t i = 0; i < count; ++i) {
+        if (w[i].rows > 0) {
+            GemvWeight& g = a.w[a.count++];
+            g.codes = (const uint8_t*)w[i].codes; g.scales = w[i].scales; g.y = y[i]; g.ldy = ld_y[i]; g.n = (int)w[i].rows; g.fmt = w[i].fmt;
+        }
+        if (a.count == kGemvWeights || i + 1 == count) {
+            if (launch_gemv(a, (hipStream_t)stream) != hipSuccess) return SNIP_ERR_HIP;
+            a.count = 0;
+        }
+    }
+    return SNIP_OK;
+}
+
 size_t snip_noalloc_max_cols(void) { return (size_t)kNoallocMaxCols; }
 
 snip_status snip_quant_error_stats_noalloc(const void* x, int64_t rows, int64_t cols, int64_t ld, snip_axis axis,

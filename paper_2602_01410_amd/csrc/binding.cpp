@@ -26,6 +26,7 @@ decltype(&snip_adamw_sensitivity) p_adamw;
 decltype(&snip_rms_norm) p_rms_norm;
 decltype(&snip_rms_norm_backward) p_rms_norm_backward;
 decltype(&snip_adamw_step) p_adamw_step;
+decltype(&snip_gemv) p_gemv;
 
 PyObject *s_codes, *s_scales, *s_scales_g4, *s_rows, *s_cols, *s_fmt;      // interned attribute names
 PyObject *s_param, *s_grad, *s_m, *s_v, *s_copy, *s_m_scale, *s_v_scale, *s_weight_decay;
@@ -352,6 +353,37 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t n)
     return call([&] { return p_adamw_step(ts.data(), (int32_t)len, lr, b1, b2, eps, step, (const float*)gs, seed, s); });
 }
 
+// (x, weights, outputs, out_dtype, stream): sequences of quantized tensors and of matrices
+PyObject* gemv(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Source x; int64_t dt; void* s;
+    if (!count(n, 5) || !source(a[0], x) || !integer(a[3], dt) || !stream(a[4], s)) return nullptr;
+    PyObject* ws = PySequence_Fast(a[1], "expected a sequence of quantized weights");
+    if (!ws) return nullptr;
+    PyObject* ys = PySequence_Fast(a[2], "expected a sequence of outputs");
+    if (!ys) { Py_DECREF(ws); return nullptr; }
+    const Py_ssize_t len = PySequence_Fast_GET_SIZE(ws);
+    std::vector<snip_qtensor> w((size_t)len);
+    std::vector<void*> y((size_t)len);
+    std::vector<int64_t> ld((size_t)len);
+    bool ok = PySequence_Fast_GET_SIZE(ys) == len;
+    if (!ok) PyErr_SetString(PyExc_ValueError, "expected as many outputs as weights");
+    for (Py_ssize_t i = 0; ok && i < len; ++i) {
+        const at::Tensor* t;
+        ok = qtensor(PySequence_Fast_GET_ITEM(ws, i), w[(size_t)i]) && tensor(PySequence_Fast_GET_ITEM(ys, i), t);
+        if (!ok) break;
+        ok = t->dim() == 2 && t->is_cuda() && t->size(0) == x.rows && t->size(1) == w[(size_t)i].rows && (t->stride(1) == 1 || t->size(1) <= 1) &&
+             t->scalar_type() == (dt == SNIP_OUT_FP32 ? at::kFloat : at::kBFloat16);
+        if (!ok) { PyErr_SetString(PyExc_ValueError, "expected CUDA matrices of the output type, a row for each token and a column for each row of the weight"); break; }
+        y[(size_t)i] = t->data_ptr();
+        ld[(size_t)i] = t->stride(0);
+    }
+    Py_DECREF(ws);
+    Py_DECREF(ys);
+    if (!ok) return nullptr;
+    return call([&] { return p_gemv(x.p, x.rows, x.cols, x.ld, w.data(), y.data(), ld.data(), (int32_t)len, (snip_out_dtype)dt, s); });
+}
+
 template <class F> bool find(void* lib, const char* name, F& f)
 {
     f = (F)dlsym(lib, name);
@@ -372,7 +404,8 @@ PyObject* bind(PyObject*, PyObject* arg)
         !find(lib, "snip_quantize_paper", p_quantize_paper) || !find(lib, "snip_gemm_paper", p_gemm_paper) ||
         !find(lib, "snip_quant_error_stats", p_stats) || !find(lib, "snip_quant_error_stats_both", p_stats_both) ||
         !find(lib, "snip_adamw_sensitivity", p_adamw) || !find(lib, "snip_rms_norm", p_rms_norm) ||
-        !find(lib, "snip_rms_norm_backward", p_rms_norm_backward) || !find(lib, "snip_adamw_step", p_adamw_step))
+        !find(lib, "snip_rms_norm_backward", p_rms_norm_backward) || !find(lib, "snip_adamw_step", p_adamw_step) ||
+        !find(lib, "snip_gemv", p_gemv))
         return nullptr;
     Py_RETURN_NONE;
 }
@@ -391,7 +424,7 @@ PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t n)
 #define SNIP_FAST(name) {#name, (PyCFunction)(void (*)(void))guarded<name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"bind", bind, METH_O, nullptr}, SNIP_FAST(quantize), SNIP_FAST(quantize_both), SNIP_FAST(quantize_sr_fp4),
                          SNIP_FAST(gemm), SNIP_FAST(gemm_norm), SNIP_FAST(quantize_paper), SNIP_FAST(gemm_paper), SNIP_FAST(stats),
-                         SNIP_FAST(stats_both), SNIP_FAST(adamw), SNIP_FAST(rms_norm), SNIP_FAST(rms_norm_backward), SNIP_FAST(adamw_step), {nullptr, nullptr, 0, nullptr}};
+                         SNIP_FAST(stats_both), SNIP_FAST(adamw), SNIP_FAST(rms_norm), SNIP_FAST(rms_norm_backward), SNIP_FAST(adamw_step), SNIP_FAST(gemv), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_snip_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -146,6 +146,21 @@ static_assert(sizeof(AdamwStepArgs) <= 4096, "kernel arguments");
 int64_t adamw_step_chunks(int64_t n);
 hipError_t launch_adamw_step(const AdamwStepArgs& a, bool small, hipStream_t s);
 
+// Few tokens against quantized weights that share them (gemv.hip).
+struct GemvWeight {
+    const uint8_t *codes, *scales;
+    void* y; int64_t ldy;
+    int n, fmt;
+    int first;                               // of its workgroups; set by the launcher
+};
+constexpr int kGemvWeights = 8;              // of a launch
+struct GemvArgs {
+    const uint16_t* x; int64_t ldx;
+    int m, k, out_fp32, count;
+    GemvWeight w[kGemvWeights];
+};
+hipError_t launch_gemv(GemvArgs a, hipStream_t s);
+
 // RMS norm (norm_kernels.hip); absent outputs are null.
 struct NormArgs {
     const uint16_t* x; int64_t ldx;

@@ -31,7 +31,7 @@ EXPORTS = ("snip_qtensor_code_bytes", "snip_qtensor_scale_bytes", "snip_qtensor_
            "snip_paper_scale_bytes", "snip_paper_workspace_bytes", "snip_quantize_paper",
            "snip_quant_error_stats_paper", "snip_gemm_paper", "snip_quant_error_stats_both",
            "snip_noalloc_max_cols", "snip_quant_error_stats_noalloc",
-           "snip_rms_norm", "snip_rms_norm_backward", "snip_rms_norm_workspace_bytes", "snip_adamw_step")
+           "snip_rms_norm", "snip_rms_norm_backward", "snip_rms_norm_workspace_bytes", "snip_adamw_step", "snip_gemv")
 
 
 class _PTensorC(ctypes.Structure):
@@ -142,6 +142,8 @@ def _lib():
         lib.snip_rms_norm_backward.argtypes = [vp, i64, i64, i64, vp, i64, vp, ci, vp, vp, i64, vp, i64, vp, vp, sz, vp]
         lib.snip_adamw_step.restype = ci
         lib.snip_adamw_step.argtypes = [vp, ctypes.c_int32, cd, cd, cd, cd, i64, vp, ctypes.c_uint64, vp]
+        lib.snip_gemv.restype = ci
+        lib.snip_gemv.argtypes = [vp, i64, i64, i64, qp, ctypes.POINTER(vp), ctypes.POINTER(i64), ctypes.c_int32, ci, vp]
         lib.snip_status_string.restype = ctypes.c_char_p
         lib.snip_status_string.argtypes = [ci]
         _handle = lib
@@ -573,4 +575,19 @@ def snip_adamw_step(tensors: Sequence[AdamwTensor], lr: float, beta1: float, bet
     step) selects the random numbers by which 8-bit moments are rounded."""
     status = _nat().adamw_step(tensors, lr, beta1, beta2, eps, step, grad_scale, int(seed) & (2 ** 64 - 1), _handle_of(stream))
     if status:
-        raise SnipError(status, "snip_adamw_step")
+        raise SnipError(status, "snip_adamw_step", "snip_gemv")
+
+
+def snip_gemv(x: torch.Tensor, weights: Sequence[QTensor], out: Optional[Sequence[torch.Tensor]] = None, out_dtype: int = OUT_BF16, stream=None):
+    """Products of a few tokens x (bf16 [tokens, K], not quantized) with weights quantized along their rows, which share x; returns the
+    outputs [tokens, weight.rows], those passed as `out` (their type is the output type) or new ones."""
+    if out is None:
+        t, per = (torch.bfloat16, 8) if out_dtype == OUT_BF16 else (torch.float32, 4)
+        with _alloc_on(stream):
+            out = [torch.empty((x.shape[0], (w.rows + per - 1) // per * per), dtype=t, device=x.device)[:, :w.rows] for w in weights]
+    elif len(out):
+        out_dtype = OUT_FP32 if out[0].dtype == torch.float32 else OUT_BF16
+    status = _nat().gemv(x, weights, out, out_dtype, _handle_of(stream))
+    if status:
+        raise SnipError(status, "snip_gemv")
+    return out

@@ -549,13 +549,14 @@ snip_status snip_gemv(const void* x, int64_t m, int64_t k, int64_t ld, const sni
                       const int64_t* ld_y, int32_t count, snip_out_dtype out_dtype, void* stream)
 {
     if (out_dtype != SNIP_OUT_BF16 && out_dtype != SNIP_OUT_FP32) return SNIP_ERR_FORMAT;
-    if (m < 0 || k <= 0 || k % 32 != 0 || count < 0 || m >= (int64_t)1 << 20 || k >= (int64_t)1 << 31) return SNIP_ERR_SHAPE;
+    if (m < 0 || k <= 0 || k % 32 != 0 || count < 0 || m > 65536 || k >= (int64_t)1 << 31) return SNIP_ERR_SHAPE;
     snip_status st = check_rows(x, m, k, ld);
     if (st != SNIP_OK) return st;
     if ((!w || !y || !ld_y) && count > 0) return SNIP_ERR_NULL;
     for (int32_t i = 0; i < count; ++i) {
         if ((st = check_qtensor(&w[i])) != SNIP_OK) return st;
         if (w[i].cols != k) return SNIP_ERR_LAYOUT;
+        if (w[i].rows > (int64_t)1 << 27) return SNIP_ERR_SHAPE;                 // (eight of them: workgroups of a launch)
         if (w[i].rows == 0) continue;
         if (!y[i] && m > 0) return SNIP_ERR_NULL;
         if (m > 1 && ld_y[i] < w[i].rows) return SNIP_ERR_SHAPE;                 // (a single row has no pitch)

@@ -7,7 +7,6 @@
 // memory.  A lane owns one block of 32 elements of one row (16 bytes of FP4, 32 of FP8) in each span of 128: the four lanes of a
 // row take the span's four blocks, and matrix instruction j contracts elements 8 j .. 8 j + 7 of all four, for which a lane
 // reads the same elements of x.  So a block has one lane's scale, codes come in the widest loads and nothing is exchanged.
-// The waves of a workgroup share the rows and split the spans; their sums meet in LDS and are added in wave order.
 #include "snip_internal.h"
 #include "quant_common.h"
 
@@ -16,6 +15,7 @@ namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef unsigned u4_any __attribute__((ext_vector_type(4), aligned(1)));
 
 __device__ __forceinline__ bf16x8 join(const bf16x2 (&p)[4])
 {
@@ -48,111 +48,259 @@ template <> struct Block<kFP8> {
     }
 };
 
-// The sums of this wave's spans: acc[r][t] += rows 16 r .. of the workgroup's, tokens 16 t ...
-template <int FMT, int TT, int RT>
-__device__ __forceinline__ void gemv_spans(const GemvArgs& a, const GemvWeight& w, int row0, int token0, int wave, int waves, f32x4 (&acc)[RT][TT])
+// What the workgroup's waves wrote to LDS is there; loads from memory stay under way.
+__device__ __forceinline__ void lds_barrier()
 {
-    const int lane = threadIdx.x & 63, quarter = lane >> 4;
-    const int nb = a.k / kBlock, spans = (nb + 3) / 4;
-    const uint8_t *codes[RT], *scales[RT];
-    const uint16_t* x[TT];
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+constexpr int HELD = 8;
+constexpr int64_t kLdsX = 128 * 1024;      // bytes of x in LDS
+
+// Workgroup: WR x WS waves, `per` tiles of 16 RT WR rows of one weight, one after the other.  The WR waves of a share have 16 RT rows each
+// and the share's spans in common, whose elements of x they keep in LDS: all of them, or `chunk` spans at a time (then per is 1).  A wave
+// has RT U blocks per lane under way: as soon as a span's codes are used, those of U spans later are asked for, the next tile's behind the
+// last ones.  The WS shares' sums of a tile meet in LDS and are added in order.
+template <int FMT, int TT, int RT, int U, int RING, int WR, int WS, bool ALL>
+__device__ __forceinline__ void gemv_tiles(const GemvArgs& a, const GemvWeight& w, int block, int token0, uint4* lds)
+{
+    static_assert(RING == U || !ALL, "the next tile is aimed at before this one's last codes are asked for");
     constexpr int BYTES = FMT == kFP4 ? 16 : 32;             // of a block
-    // rows and tokens past the last one repeat it; what comes of them is not stored
+    constexpr int THREADS = WR * 64;                         // of a share
+    constexpr int ROWS = 16 * RT * WR;
+    const int lane = threadIdx.x & 63, quarter = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int share = wave / WR, wr = wave % WR, tid = threadIdx.x % THREADS;
+    const int nb = a.k / kBlock, chunk = a.chunk;
+    const int chunks = ((nb + 3) / 4 + WS * chunk - 1) / (WS * chunk), begin = share * chunks * chunk;       // in spans
+    const int tokens = min(16 * TT, a.m - token0);
+    // Where codes are asked for next: rows past the last one repeat it (what comes of them is not stored), blocks past a row's last one repeat
+    // that (they meet zeros of x).
+    const uint8_t *codes, *scales;
+    unsigned row_at[RT];                                     // block 0 of a lane's row behind that of the wave's first
+    auto aim = [&](int tile) {
+        const int64_t row0 = (int64_t)tile * ROWS + wr * 16 * RT, first = row0 < w.n ? row0 : w.n - 1;
+        codes = w.codes + first * nb * BYTES;
+        scales = w.scales + first * nb;
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        const int64_t row = min(row0 + r * 16 + (lane & 15), w.n - 1);
-        codes[r] = w.codes + row * nb * BYTES;
-        scales[r] = w.scales + row * nb;
-    }
+        for (int r = 0; r < RT; ++r) row_at[r] = (unsigned)min(r * 16 + (lane & 15), (int)(w.n - 1 - first)) * nb;
+    };
+    Block<FMT> c[RT][RING];
+    auto fetch = [&](int u, int span) {
 #pragma unroll
-    for (int t = 0; t < TT; ++t) x[t] = a.x + (int64_t)min(token0 + t * 16 + (lane & 15), a.m - 1) * a.ldx;
-    for (int s = wave; s < spans; s += waves) {
-        const int b = s * 4 + quarter;
-        Block<FMT> c[RT];
-        float sc[RT];
-        bf16x8 v[TT][4];
-        if (b < nb) {
+        for (int r = 0; r < RT; ++r) c[r][u].load(codes + (uint64_t)(row_at[r] + min(span * 4 + quarter, nb - 1)) * BYTES);
+    };
+    // The scale bytes of a row come 16 at a time (byte by byte they take as long as the codes), a round of U spans ahead; lanes take theirs of
+    // the four of a span.  Where the row ends within the 16 they are read one by one.
+    constexpr int G = U / 4;
+    u4_any sc[RT][G], sc_next[RT][G];
+    const int full = nb / 16;
+    auto fetch_scales = [&](u4_any (&to)[RT][G], int span) {
 #pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                c[r].load(codes[r] + (int64_t)b * BYTES);
-                sc[r] = scale_operand(scales[r][b]);
+        for (int g = 0; g < G; ++g) {
+            const int at = min(span / 4 + g, (nb - 1) / 16);
+            if (at < full) {
+#pragma unroll
+                for (int r = 0; r < RT; ++r) to[r][g] = *reinterpret_cast<const u4_any*>(scales + row_at[r] + at * 16);
+            } else {
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        unsigned d = 0;
+                        for (int i = 0; i < 4; ++i)
+                            if (at * 16 + k * 4 + i < nb) d |= (unsigned)scales[row_at[r] + at * 16 + k * 4 + i] << (8 * i);
+                        to[r][g][k] = d;
+                    }
+            }
+        }
+    };
+    // x in LDS: 16-byte piece i of a token's 16 * chunk at i ^ (token & 15), so that 16 tokens' pieces lie in different banks
+    const int per = 16 * chunk, pieces = tokens * per;
+    uint4* const mine = lds + share * (ALL ? 1 : 2) * pieces;
+    f32x4* const sums = reinterpret_cast<f32x4*>(lds + (ALL ? 1 : 2) * WS * pieces);        // [2][share][wave in share][RT TT][lane]
+    const unsigned one_over_per = 0xFFFFFFFFu / (unsigned)per + 1;           // p / per as a product: p < 2^16
+    auto stage = [&](int ch) {
+        const int64_t k0 = (int64_t)(begin + ch * chunk) * 128;
+        for (int p0 = tid; p0 < pieces; p0 += 4 * THREADS) {
+            uint4 v[4];
+            int to[4];
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                const int p = p0 + h * THREADS, token = (int)__umulhi(p, one_over_per), i = p - token * per;
+                const int64_t k = k0 + i * 8;
+                to[h] = token * per + (i ^ (token & 15));
+                v[h] = make_uint4(0, 0, 0, 0);
+                if (p < pieces && k < a.k) v[h] = *reinterpret_cast<const uint4*>(a.x + (int64_t)(token0 + token) * a.ldx + k);
             }
 #pragma unroll
-            for (int t = 0; t < TT; ++t)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) v[t][j] = *reinterpret_cast<const bf16x8*>(x[t] + b * kBlock + j * 8);
-        } else {
-            // a span that the row does not fill: nothing of x comes in either (it may be infinite)
-#pragma unroll
-            for (int r = 0; r < RT; ++r) { c[r].clear(); sc[r] = 1.f; }
-#pragma unroll
-            for (int t = 0; t < TT; ++t)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) v[t][j] = __builtin_bit_cast(bf16x8, make_uint4(0, 0, 0, 0));
+            for (int h = 0; h < 4; ++h)
+                if (p0 + h * THREADS < pieces) mine[to[h]] = v[h];
         }
+    };
+    // Chunks: a thread holds its HELD pieces of the next one while this one is used (no condition on the loads: nothing may come between the
+    // codes' and their waits).
+    uint4 held[HELD];
+    auto hold = [&](int ch) {
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            const bf16x8 e[4] = {c[r].template elements<0>(sc[r]), c[r].template elements<1>(sc[r]), c[r].template elements<2>(sc[r]),
-                                 c[r].template elements<3>(sc[r])};
+        for (int h = 0; h < HELD; ++h) {
+            const int p = min(tid + h * THREADS, pieces - 1), token = (int)__umulhi(p, one_over_per), i = p - token * per;
+            const int k = min((begin + ch * chunk) * 128 + i * 8, a.k - 8);
+            held[h] = *reinterpret_cast<const uint4*>(a.x + (int64_t)(token0 + token) * a.ldx + k);
+        }
+    };
+    auto put = [&](int ch) {
 #pragma unroll
-            for (int t = 0; t < TT; ++t)
+        for (int h = 0; h < HELD; ++h) {
+            const int p = min(tid + h * THREADS, pieces - 1), token = (int)__umulhi(p, one_over_per), i = p - token * per;
+            if ((begin + ch * chunk) * 128 + i * 8 >= a.k) held[h] = make_uint4(0, 0, 0, 0);
+            mine[(ch & 1) * pieces + token * per + (i ^ (token & 15))] = held[h];
+        }
+    };
+    const uint4* x[TT][4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(e[j], v[t][j], acc[r][t], 0, 0, 0);
+    for (int t = 0; t < TT; ++t) {
+        const int token = min(t * 16 + (lane & 15), tokens - 1);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[t][j] = mine + token * per + ((quarter * 4 + j) ^ (token & 15));
+    }
+    f32x4 acc[RT][TT];
+    constexpr int D = TT == 1 ? 4 : TT == 2 ? 2 : 1;         // how many matrix instructions ahead elements of x are read
+    const int tiles = (w.n + ROWS - 1) / ROWS, first_tile = block * a.per, end_tile = min(first_tile + a.per, tiles);
+    aim(first_tile);
+    fetch_scales(sc, begin);
+#pragma unroll
+    for (int u = 0; u < RING; ++u) fetch(u, begin + u);
+    stage(0);
+    __syncthreads();
+    for (int tile = first_tile; tile < end_tile; ++tile) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int t = 0; t < TT; ++t) acc[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int ch = 0; ch < chunks; ++ch) {
+            if (!ALL) hold(ch + 1);
+            const int at = ALL ? 0 : (ch & 1) * pieces;
+            for (int s = 0; s < chunk; s += U) {
+                const int now = begin + ch * chunk + s;
+                int next = now + U, stride = 1;
+                if (ch + 1 == chunks && s + U >= chunk) {    // behind the tile: the next one, or, once more, blocks that have just come
+                    next = begin;
+                    if (tile + 1 < end_tile) aim(tile + 1);
+                    else { next = now; stride = 0; }
+                }
+                fetch_scales(sc_next, next);
+                bf16x8 v[D + 1][TT];
+#pragma unroll
+                for (int q = 0; q < D; ++q)
+#pragma unroll
+                    for (int t = 0; t < TT; ++t) v[q][t] = __builtin_bit_cast(bf16x8, x[t][q % 4][at + (s + q / 4) * 16]);
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int q = u * 4 + j, n = q + D;
+                        if (n < U * 4)
+#pragma unroll
+                            for (int t = 0; t < TT; ++t) v[n % (D + 1)][t] = __builtin_bit_cast(bf16x8, x[t][n % 4][at + (s + n / 4) * 16]);
+                        bf16x8 e[RT];
+#pragma unroll
+                        for (int r = 0; r < RT; ++r) {
+                            const float f = scale_operand((sc[r][u / 4][u % 4] >> (8 * quarter)) & 0xFFu);
+                            e[r] = j == 0 ? c[r][u % RING].template elements<0>(f) : j == 1 ? c[r][u % RING].template elements<1>(f)
+                                 : j == 2 ? c[r][u % RING].template elements<2>(f) : c[r][u % RING].template elements<3>(f);
+                        }
+#pragma unroll
+                        for (int r = 0; r < RT; ++r)
+#pragma unroll
+                            for (int t = 0; t < TT; ++t) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(e[r], v[q % (D + 1)][t], acc[r][t], 0, 0, 0);
+                    }
+                    // (not moved down to the next use: the loads have to be under way)
+                    __builtin_amdgcn_sched_barrier(0);
+                    fetch(u % RING, u + RING < U ? now + u + RING : next + (u + RING - U) * stride);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+#pragma unroll
+                    for (int g = 0; g < G; ++g) sc[r][g] = sc_next[r][g];
+            }
+            if (!ALL) {
+                // into the other buffer, which all have read before the last barrier; codes under way are not waited for
+                put(ch + 1);
+                lds_barrier();
+            }
+        }
+        auto store = [&](int of, int p, f32x4 s) {
+            const int row = tile * ROWS + of * 16 * RT + p / TT * 16 + quarter * 4, token = token0 + p % TT * 16 + (lane & 15);
+            if (token >= a.m || row >= w.n) return;
+            if (a.out_fp32) {
+                float* const to = (float*)w.y + token * w.ldy + row;
+                if (row + 4 <= w.n) *reinterpret_cast<f32x4*>(to) = s;
+                else
+                    for (int k = 0; k < 4 && row + k < w.n; ++k) to[k] = s[k];
+            } else {
+                uint16_t* const to = (uint16_t*)w.y + token * w.ldy + row;
+                const uint2 q = make_uint2(__builtin_bit_cast(unsigned, bf16x2{(__bf16)s[0], (__bf16)s[1]}), __builtin_bit_cast(unsigned, bf16x2{(__bf16)s[2], (__bf16)s[3]}));
+                if (row + 4 <= w.n) *reinterpret_cast<uint2*>(to) = q;
+                else
+                    for (int k = 0; k < 4 && row + k < w.n; ++k) to[k] = (uint16_t)((k < 2 ? q.x : q.y) >> (16 * (k & 1)));
+            }
+        };
+        if (WS == 1) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int t = 0; t < TT; ++t) store(wr, r * TT + t, acc[r][t]);
+        } else {
+            constexpr int PARTS = WR * RT * TT;
+            f32x4* const here = sums + (tile & 1) * WS * PARTS * 64;
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int t = 0; t < TT; ++t) here[((share * WR + wr) * RT * TT + r * TT + t) * 64 + lane] = acc[r][t];
+            lds_barrier();                                   // (the other half of `sums` may still be read)
+            for (int p = wave; p < PARTS; p += WR * WS) {
+                f32x4 s = here[p * 64 + lane];
+#pragma unroll
+                for (int k = 1; k < WS; ++k) s += here[(k * PARTS + p) * 64 + lane];
+                store(p / (RT * TT), p % (RT * TT), s);
+            }
         }
     }
 }
 
-// Workgroup: 16 RT rows of one weight by 16 TT tokens, WS waves.
-template <int TT, int RT, int WS>
-__global__ __launch_bounds__(WS * 64) void gemv_kernel(const GemvArgs a)
+template <int TT, int RT, int U, int WR, int WS, bool ALL>
+__global__ __launch_bounds__(WR * WS * 64, 2) void gemv_kernel(const GemvArgs a)
 {
-    __shared__ f32x4 sums[WS][RT * TT][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    extern __shared__ uint4 lds[];
     int i = 0;
     while (i + 1 < a.count && (int)blockIdx.x >= a.w[i + 1].first) ++i;
     const GemvWeight& w = a.w[i];
-    const int row0 = ((int)blockIdx.x - w.first) * 16 * RT, token0 = blockIdx.y * 16 * TT;
-    f32x4 acc[RT][TT];
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int t = 0; t < TT; ++t) acc[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (w.fmt == kFP4) gemv_spans<kFP4, TT, RT>(a, w, row0, token0, wave, WS, acc);
-    else               gemv_spans<kFP8, TT, RT>(a, w, row0, token0, wave, WS, acc);
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int t = 0; t < TT; ++t) sums[wave][r * TT + t][lane] = acc[r][t];
-    __syncthreads();
-    for (int p = wave; p < RT * TT; p += WS) {
-        f32x4 s = sums[0][p][lane];
-#pragma unroll
-        for (int k = 1; k < WS; ++k) s += sums[k][p][lane];
-        const int row = row0 + p / TT * 16 + (lane >> 4) * 4, token = token0 + p % TT * 16 + (lane & 15);
-        if (token >= a.m || row >= w.n) continue;
-        if (a.out_fp32) {
-            float* const to = (float*)w.y + token * w.ldy + row;
-            if (row + 4 <= w.n) *reinterpret_cast<f32x4*>(to) = s;
-            else
-                for (int k = 0; k < 4 && row + k < w.n; ++k) to[k] = s[k];
-        } else {
-            uint16_t* const to = (uint16_t*)w.y + token * w.ldy + row;
-            const uint2 q = make_uint2(__builtin_bit_cast(unsigned, bf16x2{(__bf16)s[0], (__bf16)s[1]}), __builtin_bit_cast(unsigned, bf16x2{(__bf16)s[2], (__bf16)s[3]}));
-            if (row + 4 <= w.n) *reinterpret_cast<uint2*>(to) = q;
-            else
-                for (int k = 0; k < 4 && row + k < w.n; ++k) to[k] = (uint16_t)((k < 2 ? q.x : q.y) >> (16 * (k & 1)));
-        }
-    }
+    const int block = (int)blockIdx.x - w.first, token0 = blockIdx.y * 16 * TT;
+    if (w.fmt == kFP4) gemv_tiles<kFP4, TT, RT, U, U, WR, WS, ALL>(a, w, block, token0, lds);
+    else               gemv_tiles<kFP8, TT, RT, 4, 4 / RT, WR, WS, ALL>(a, w, block, token0, lds);
 }
 
-template <int TT, int RT, int WS> hipError_t launch(GemvArgs& a, hipStream_t s)
+template <int TT, int RT, int U, int WR, int WS, bool ALL> hipError_t launch(GemvArgs& a, hipStream_t s, int most = 0)
 {
+    constexpr int ROWS = 16 * RT * WR;
+    const int tokens = a.m < 16 * TT ? a.m : 16 * TT, spans = (a.k / kBlock + 3) / 4;
+    const int own = ((spans + WS - 1) / WS + U - 1) / U * U, fit = HELD * WR * 4 / tokens / U * U;
+    a.chunk = ALL || own < fit ? own : fit;
+    if (a.chunk <= 0) return hipErrorInvalidValue;
+    int64_t tiles = 0;
+    for (int i = 0; i < a.count; ++i) tiles += (a.w[i].n + ROWS - 1) / ROWS;
+    a.per = !ALL ? 1 : (int)((tiles + most - 1) / most);
     int64_t blocks = 0;
     for (int i = 0; i < a.count; ++i) {
         a.w[i].first = (int)blocks;
-        blocks += (a.w[i].n + 16 * RT - 1) / (16 * RT);
+        blocks += ((a.w[i].n + ROWS - 1) / ROWS + a.per - 1) / a.per;
     }
-    hipLaunchKernelGGL((gemv_kernel<TT, RT, WS>), dim3((unsigned)blocks, (a.m + 16 * TT - 1) / (16 * TT)), dim3(WS * 64), 0, s, a);
+    const size_t x = (size_t)(ALL ? 1 : 2) * WS * tokens * a.chunk * 256, sums = WS > 1 ? (size_t)2 * WS * WR * RT * TT * 1024 : 0;
+    if (x + sums > 160 * 1024) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((gemv_kernel<TT, RT, U, WR, WS, ALL>), dim3((unsigned)blocks, (a.m + 16 * TT - 1) / (16 * TT)), dim3(WR * WS * 64), x + sums, s, a);
     return hipGetLastError();
 }
 
@@ -161,9 +309,31 @@ template <int TT, int RT, int WS> hipError_t launch(GemvArgs& a, hipStream_t s)
 hipError_t launch_gemv(GemvArgs a, hipStream_t s)
 {
     if (a.count == 0 || a.m == 0) return hipSuccess;
-    if (a.m <= 16) return launch<1, 1, 4>(a, s);
-    if (a.m <= 32) return launch<2, 1, 4>(a, s);
-    return launch<4, 1, 4>(a, s);
+    int64_t tiles = 0;                                       // of 16 rows
+    for (int i = 0; i < a.count; ++i) tiles += (a.w[i].n + 15) / 16;
+    const int64_t spans = (a.k / kBlock + 3) / 4;
+    auto whole = [&](int shares) { return a.m <= 16 && shares * a.m * (((spans + shares - 1) / shares + 3) / 4 * 4) * 256 <= kLdsX; };
+    if (tiles <= 512 && whole(8)) return launch<1, 1, 4, 1, 8, true>(a, s, 512);
+    if (tiles > 512 && whole(4)) {
+        if ((int64_t)a.m * a.k <= 16384) return launch<1, 1, 4, 1, 4, true>(a, s, 512);
+        return launch<1, 1, 4, 2, 4, true>(a, s, 256);
+    }
+    const int cus = gemm_compute_units();
+    int64_t most = 0;
+    int form = 0, tt = 0;                                    // rows of a workgroup's tile: 256, 128, 64, 32
+    for (int t = a.m <= 16 ? 1 : a.m <= 32 ? 2 : a.m <= 48 ? 3 : 4; t >= 1; --t)
+        for (int rows = 16; rows >= 2 * t; rows /= 2) {
+            const int64_t wgs = ((tiles + rows - 1) / rows) * ((a.m + 16 * t - 1) / (16 * t));
+            if (wgs > most && (wgs <= cus || most == 0)) { most = wgs; form = rows; tt = t; }
+            if (rows == 8 && t > 2) break;
+        }
+#define SNIP_GEMV(ROWS, TT, ...) if (form == ROWS && tt == TT) return launch<TT, __VA_ARGS__, false>(a, s)
+    SNIP_GEMV(16, 1, 2, 4, 8, 1); SNIP_GEMV(16, 2, 2, 4, 8, 1); SNIP_GEMV(16, 3, 2, 4, 8, 1); SNIP_GEMV(16, 4, 2, 4, 8, 1);
+    SNIP_GEMV(8, 1, 1, 4, 8, 1); SNIP_GEMV(8, 2, 1, 4, 8, 1); SNIP_GEMV(8, 3, 1, 4, 8, 1); SNIP_GEMV(8, 4, 1, 4, 8, 1);
+    SNIP_GEMV(4, 1, 1, 4, 4, 2); SNIP_GEMV(4, 2, 1, 4, 4, 2);
+    SNIP_GEMV(2, 1, 1, 4, 2, 4);
+#undef SNIP_GEMV
+    return hipErrorInvalidValue;
 }
 
 }  // namespace snip

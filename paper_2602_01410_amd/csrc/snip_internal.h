@@ -157,6 +157,7 @@ constexpr int kGemvWeights = 8;              // of a launch
 struct GemvArgs {
     const uint16_t* x; int64_t ldx;
     int m, k, out_fp32, count;
+    int chunk, per;                          // spans of 128 elements of x that a share of the waves keeps, tiles of a workgroup; set by the launcher
     GemvWeight w[kGemvWeights];
 };
 hipError_t launch_gemv(GemvArgs a, hipStream_t s);

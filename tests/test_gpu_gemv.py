@@ -61,6 +61,18 @@ def test_against_64_bits(m, n, k, fmt):
         assert (buf[:, n:] == 31).all()
 
 
+@pytest.mark.parametrize("m,n,k", [(15, 33, 4128), (16, 40, 4096), (16, 40, 4128), (13, 9000, 4704), (12, 9000, 5472), (3, 9000, 32), (5, 9000, 11008), (2, 32, 30016), (30, 5000, 1120),
+                                   (64, 33000, 544), (40, 18000, 96), (17, 9000, 288), (33, 1000, 4640), (64, 500, 8224)])
+def test_every_form(m, n, k):
+    """Sizes around the changes of the kernel: x whole in LDS or not, tiles of 16 to 256 rows, 16 to 64 tokens, several tiles per workgroup; both
+    formats in one call."""
+    rng = np.random.default_rng(m + n + k)
+    x, xd = tokens(rng, m, k)
+    ws = [weight(rng, n, k, snip.FP4), weight(rng, n // 3 + 1, k, snip.FP8)]
+    for (q, w), y in zip(ws, snip.snip_gemv(x, [q for q, _ in ws], out_dtype=snip.OUT_FP32)):
+        check(y, xd, w)
+
+
 @pytest.mark.parametrize("fmt", [snip.FP4, snip.FP8])
 @pytest.mark.parametrize("m,n,k", [(1, 4096, 4096), (5, 40, 96), (16, 1000, 1056), (40, 300, 512), (64, 80, 11008)])
 def test_small_integers_are_exact(m, n, k, fmt):

@@ -48,6 +48,24 @@ template <> struct Block<kFP8> {
     }
 };
 
+// Four rows of a token's output.
+__device__ __forceinline__ void store_rows(const GemvArgs& a, const GemvWeight& w, int row, int token, const f32x4& s)
+{
+    if (token >= a.m || row >= w.n) return;
+    if (a.out_fp32) {
+        float* const to = (float*)w.y + token * w.ldy + row;
+        if (row + 4 <= w.n) *reinterpret_cast<f32x4*>(to) = s;
+        else
+            for (int k = 0; k < 4 && row + k < w.n; ++k) to[k] = s[k];
+    } else {
+        uint16_t* const to = (uint16_t*)w.y + token * w.ldy + row;
+        const uint2 q = make_uint2(__builtin_bit_cast(unsigned, bf16x2{(__bf16)s[0], (__bf16)s[1]}), __builtin_bit_cast(unsigned, bf16x2{(__bf16)s[2], (__bf16)s[3]}));
+        if (row + 4 <= w.n) *reinterpret_cast<uint2*>(to) = q;
+        else
+            for (int k = 0; k < 4 && row + k < w.n; ++k) to[k] = (uint16_t)((k < 2 ? q.x : q.y) >> (16 * (k & 1)));
+    }
+}
+
 // What the workgroup's waves wrote to LDS is there; loads from memory stay under way.
 __device__ __forceinline__ void lds_barrier()
 {
@@ -121,13 +139,14 @@ __device__ __forceinline__ void gemv_tiles(const GemvArgs& a, const GemvWeight& 
     uint4* const mine = lds + share * (ALL ? 1 : 2) * pieces;
     f32x4* const sums = reinterpret_cast<f32x4*>(lds + (ALL ? 1 : 2) * WS * pieces);        // [2][share][wave in share][RT TT][lane]
     const unsigned one_over_per = 0xFFFFFFFFu / (unsigned)per + 1;           // p / per as a product: p < 2^16
+    constexpr int STAGED = 8;                                              // pieces of a thread at a time: their loads wait together
     auto stage = [&](int ch) {
         const int64_t k0 = (int64_t)(begin + ch * chunk) * 128;
-        for (int p0 = tid; p0 < pieces; p0 += 4 * THREADS) {
-            uint4 v[4];
-            int to[4];
+        for (int p0 = tid; p0 < pieces; p0 += STAGED * THREADS) {
+            uint4 v[STAGED];
+            int to[STAGED];
 #pragma unroll
-            for (int h = 0; h < 4; ++h) {
+            for (int h = 0; h < STAGED; ++h) {
                 const int p = p0 + h * THREADS, token = (int)__umulhi(p, one_over_per), i = p - token * per;
                 const int64_t k = k0 + i * 8;
                 to[h] = token * per + (i ^ (token & 15));
@@ -135,7 +154,7 @@ __device__ __forceinline__ void gemv_tiles(const GemvArgs& a, const GemvWeight& 
                 if (p < pieces && k < a.k) v[h] = *reinterpret_cast<const uint4*>(a.x + (int64_t)(token0 + token) * a.ldx + k);
             }
 #pragma unroll
-            for (int h = 0; h < 4; ++h)
+            for (int h = 0; h < STAGED; ++h)
                 if (p0 + h * THREADS < pieces) mine[to[h]] = v[h];
         }
     };
@@ -232,21 +251,8 @@ __device__ __forceinline__ void gemv_tiles(const GemvArgs& a, const GemvWeight& 
                 lds_barrier();
             }
         }
-        auto store = [&](int of, int p, f32x4 s) {
-            const int row = tile * ROWS + of * 16 * RT + p / TT * 16 + quarter * 4, token = token0 + p % TT * 16 + (lane & 15);
-            if (token >= a.m || row >= w.n) return;
-            if (a.out_fp32) {
-                float* const to = (float*)w.y + token * w.ldy + row;
-                if (row + 4 <= w.n) *reinterpret_cast<f32x4*>(to) = s;
-                else
-                    for (int k = 0; k < 4 && row + k < w.n; ++k) to[k] = s[k];
-            } else {
-                uint16_t* const to = (uint16_t*)w.y + token * w.ldy + row;
-                const uint2 q = make_uint2(__builtin_bit_cast(unsigned, bf16x2{(__bf16)s[0], (__bf16)s[1]}), __builtin_bit_cast(unsigned, bf16x2{(__bf16)s[2], (__bf16)s[3]}));
-                if (row + 4 <= w.n) *reinterpret_cast<uint2*>(to) = q;
-                else
-                    for (int k = 0; k < 4 && row + k < w.n; ++k) to[k] = (uint16_t)((k < 2 ? q.x : q.y) >> (16 * (k & 1)));
-            }
+        auto store = [&](int of, int p, const f32x4& s) {
+            store_rows(a, w, tile * ROWS + of * 16 * RT + p / TT * 16 + quarter * 4, token0 + p % TT * 16 + (lane & 15), s);
         };
         if (WS == 1) {
 #pragma unroll
@@ -283,6 +289,58 @@ __global__ __launch_bounds__(WR * WS * 64, 2) void gemv_kernel(const GemvArgs a)
     else               gemv_tiles<kFP8, TT, RT, 4, 4 / RT, WR, WS, ALL>(a, w, block, token0, lds);
 }
 
+// Small problems: 16 rows by up to 16 tokens, eight waves that take every eighth span, codes and x straight from memory.  Little code, as a
+// launch fetches it anew, and no wait but the loads' own.
+constexpr int kSmallWaves = 8;
+template <int FMT>
+__device__ __forceinline__ f32x4 small_sums(const GemvArgs& a, const GemvWeight& w, int row0, int token0, int wave, int lane)
+{
+    constexpr int BYTES = FMT == kFP4 ? 16 : 32;
+    const int nb = a.k / kBlock, quarter = lane >> 4;
+    const int64_t row = min(row0 + (lane & 15), w.n - 1);
+    const uint8_t* const codes = w.codes + row * nb * BYTES;
+    const uint8_t* const scales = w.scales + row * nb;
+    const uint16_t* const x = a.x + (int64_t)min(token0 + (lane & 15), a.m - 1) * a.ldx;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int s = wave; s * 4 < nb; s += kSmallWaves) {
+        const int b = s * 4 + quarter;
+        Block<FMT> c;
+        c.clear();
+        float sc = 1.f;
+        bf16x8 v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = __builtin_bit_cast(bf16x8, make_uint4(0, 0, 0, 0));
+        if (b < nb) {                                        // (nothing of x beyond the row: it may be infinite)
+            c.load(codes + (int64_t)b * BYTES);
+            sc = scale_operand(scales[b]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const bf16x8*>(x + b * kBlock + j * 8);
+        }
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(c.template elements<0>(sc), v[0], acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(c.template elements<1>(sc), v[1], acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(c.template elements<2>(sc), v[2], acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(c.template elements<3>(sc), v[3], acc, 0, 0, 0);
+    }
+    return acc;
+}
+__global__ __launch_bounds__(kSmallWaves * 64) void gemv_small_kernel(const GemvArgs a)
+{
+    __shared__ f32x4 sums[kSmallWaves][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int i = 0;
+    while (i + 1 < a.count && (int)blockIdx.x >= a.w[i + 1].first) ++i;
+    const GemvWeight& w = a.w[i];
+    const int row0 = ((int)blockIdx.x - w.first) * 16, token0 = blockIdx.y * 16;
+    sums[wave][lane] = w.fmt == kFP4 ? small_sums<kFP4>(a, w, row0, token0, wave, lane) : small_sums<kFP8>(a, w, row0, token0, wave, lane);
+    __syncthreads();
+    if (wave == 0) {
+        f32x4 s = sums[0][lane];
+#pragma unroll
+        for (int k = 1; k < kSmallWaves; ++k) s += sums[k][lane];
+        store_rows(a, w, row0 + (lane >> 4) * 4, token0 + (lane & 15), s);
+    }
+}
+
 template <int TT, int RT, int U, int WR, int WS, bool ALL> hipError_t launch(GemvArgs& a, hipStream_t s, int most = 0)
 {
     constexpr int ROWS = 16 * RT * WR;
@@ -312,12 +370,31 @@ hipError_t launch_gemv(GemvArgs a, hipStream_t s)
     int64_t tiles = 0;                                       // of 16 rows
     for (int i = 0; i < a.count; ++i) tiles += (a.w[i].n + 15) / 16;
     const int64_t spans = (a.k / kBlock + 3) / 4;
+    // Up to 24 spans in up to 8000 / spans workgroups: us with the small kernel / the others: 1 token [4096 x 2048] 3.5 / 4.4, [4096 x 4096] (not
+    // taken) 5.4 / 5.2, 9 tokens 2 x [1003 x 2080] 3.8 / 6.2, 3 x [4096 x 2048] (not taken) 8.9 / 7.2, 64 tokens 2 x [1003 x 2080] (not) 7.6 / 8.9.
+    const int64_t small = tiles * ((a.m + 15) / 16);
+    if (spans <= 24 && small * spans <= 8000) {
+        int blocks = 0;
+        for (int i = 0; i < a.count; ++i) {
+            a.w[i].first = blocks;
+            blocks += (a.w[i].n + 15) / 16;
+        }
+        hipLaunchKernelGGL(gemv_small_kernel, dim3(blocks, (a.m + 15) / 16), dim3(kSmallWaves * 64), 0, s, a);
+        return hipGetLastError();
+    }
+    // Up to 16 tokens whose x fits LDS as a whole: tiles of 16 rows, eight waves a tile where there are few, four where there are many (x is small) or
+    // eight that take two tiles (more tokens: the share of a wave's spans in x is read for two).  us: 1 token 3 x [4096 x 4096] 9.9 / 8.9 / 10.1, [4096 x
+    // 11008] 11.3 / 12.0 / -, 8 tokens 3 x [4096 x 4096] - / 11.4 / 10.0, 2 x [28672 x 8192], 1 token 50.5 / 50.9 / 51.3.
     auto whole = [&](int shares) { return a.m <= 16 && shares * a.m * (((spans + shares - 1) / shares + 3) / 4 * 4) * 256 <= kLdsX; };
     if (tiles <= 512 && whole(8)) return launch<1, 1, 4, 1, 8, true>(a, s, 512);
     if (tiles > 512 && whole(4)) {
         if ((int64_t)a.m * a.k <= 16384) return launch<1, 1, 4, 1, 4, true>(a, s, 512);
         return launch<1, 1, 4, 2, 4, true>(a, s, 256);
     }
+    // Otherwise x comes in chunks.  Of the tiles (256, 128, 64 or 32 rows, 16 to 64 tokens) the one with the most workgroups that still run at once, one
+    // per compute unit: us with 256 / 128 / 64 / 32 rows, 16 tokens: 2 x [28672 x 8192] 67 / 72 / 82 / -, 2 x [11008 x 4096] 26 / 16 / 23 / 25, 3 x
+    // [4096 x 4096] 26 / 16 / 12 / 18, [4096 x 11008] 66 / 38 / 26 / 20; 48 tokens 3 x [4096 x 4096] in tiles of 128 rows by 48 / 32 / 16
+    // tokens 26 / 19 / 30.
     const int cus = gemm_compute_units();
     int64_t most = 0;
     int form = 0, tt = 0;                                    // rows of a workgroup's tile: 256, 128, 64, 32

@@ -20,17 +20,28 @@ namespace snip {
 namespace {
 
 constexpr int kStepThreads = 256;
-constexpr int kStepChunk = kStepThreads * 8 * 4;       // elements of a workgroup's turn, a multiple of the scale groups' 128
+// Elements of a workgroup, a multiple of the scale groups' 128.  A workgroup for each 2048 elements: us per step of a 7B-shaped block of 202 M elements, moments of
+// 32 / 8 bits, 1114 / 607; with 8192 elements 1185 / 658, 2048 workgroups that take turns of 8192 1241 / 737, of 32768 1294 / 757.
+constexpr int kStepChunk = kStepThreads * 8;
 
 // Vectors at the elements' own alignment: tensors may start anywhere.
 typedef float f4_t __attribute__((ext_vector_type(4), aligned(4)));
 typedef unsigned u4_t __attribute__((ext_vector_type(4), aligned(2)));
 typedef unsigned u2_t __attribute__((ext_vector_type(2), aligned(1)));
 
-__device__ __forceinline__ void load8f(const float* p, int left, float (&f)[8])
+// NT: streaming.  With moments of 8 bits it pays (7B- / 1B-shaped block 607 / 187 us, plain 601 / 202), with 32 it does not (1114 / 349 us, plain
+// 1053 / 350).
+template <bool NT, class V> __device__ __forceinline__ V get(const V* p) { return NT ? __builtin_nontemporal_load(p) : *p; }
+template <bool NT, class V> __device__ __forceinline__ void put(V* p, V v)
+{
+    if (NT) __builtin_nontemporal_store(v, p);
+    else    *p = v;
+}
+
+template <bool NT> __device__ __forceinline__ void load8f(const float* p, int left, float (&f)[8])
 {
     if (left >= 8) {
-        const f4_t a = __builtin_nontemporal_load((const f4_t*)p), b = __builtin_nontemporal_load((const f4_t*)p + 1);
+        const f4_t a = get<NT>((const f4_t*)p), b = get<NT>((const f4_t*)p + 1);
 #pragma unroll
         for (int i = 0; i < 4; ++i) { f[i] = a[i]; f[4 + i] = b[i]; }
     } else {
@@ -38,21 +49,21 @@ __device__ __forceinline__ void load8f(const float* p, int left, float (&f)[8])
         for (int i = 0; i < 8; ++i) f[i] = i < left ? p[i] : 0.f;
     }
 }
-__device__ __forceinline__ void store8f(float* p, int left, const float (&f)[8])
+template <bool NT> __device__ __forceinline__ void store8f(float* p, int left, const float (&f)[8])
 {
     if (left >= 8) {
-        __builtin_nontemporal_store(f4_t{f[0], f[1], f[2], f[3]}, (f4_t*)p);
-        __builtin_nontemporal_store(f4_t{f[4], f[5], f[6], f[7]}, (f4_t*)p + 1);
+        put<NT>((f4_t*)p, f4_t{f[0], f[1], f[2], f[3]});
+        put<NT>((f4_t*)p + 1, f4_t{f[4], f[5], f[6], f[7]});
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (i < left) p[i] = f[i];
     }
 }
-__device__ __forceinline__ void load8h(const uint16_t* p, int left, float (&f)[8])
+template <bool NT> __device__ __forceinline__ void load8h(const uint16_t* p, int left, float (&f)[8])
 {
     if (left >= 8) {
-        const u4_t v = __builtin_nontemporal_load((const u4_t*)p);
+        const u4_t v = get<NT>((const u4_t*)p);
 #pragma unroll
         for (int i = 0; i < 4; ++i) unpack2(v[i], f[2 * i], f[2 * i + 1]);
     } else {
@@ -72,7 +83,7 @@ __device__ __forceinline__ void store8h(uint16_t* p, int left, const float (&f)[
 }
 __device__ __forceinline__ void load8c(const uint8_t* p, int left, unsigned& lo, unsigned& hi)
 {
-    if (left >= 8) { const u2_t v = __builtin_nontemporal_load((const u2_t*)p); lo = v[0]; hi = v[1]; return; }
+    if (left >= 8) { const u2_t v = get<true>((const u2_t*)p); lo = v[0]; hi = v[1]; return; }
     lo = hi = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -80,7 +91,7 @@ __device__ __forceinline__ void load8c(const uint8_t* p, int left, unsigned& lo,
 }
 __device__ __forceinline__ void store8c(uint8_t* p, int left, unsigned lo, unsigned hi)
 {
-    if (left >= 8) { __builtin_nontemporal_store(u2_t{lo, hi}, (u2_t*)p); return; }
+    if (left >= 8) { put<true>((u2_t*)p, u2_t{lo, hi}); return; }
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         if (i < left) p[i] = (uint8_t)((i < 4 ? lo : hi) >> (8 * (i & 3)));
@@ -127,16 +138,15 @@ __global__ __launch_bounds__(kStepThreads) void adamw_step_kernel(const AdamwSte
         const int at = 63 - __builtin_clzll(before);
         const AdamwStepTensor& t = a.t[at];
         const int64_t base = (int64_t)(chunk - a.first[at]) * kStepChunk;
-#pragma unroll 1
-        for (int64_t e = base + threadIdx.x * 8; e < base + kStepChunk; e += kStepThreads * 8) {
-            if (e - lane * 8 >= t.n) break;                                    // wave-uniform
+        const int64_t e = base + threadIdx.x * 8;
+        if (e - lane * 8 < t.n) {                                              // wave-uniform
             const int64_t rest = t.n - e;
             const int left = rest >= 8 ? 8 : rest > 0 ? (int)rest : 0;
             const int64_t at8 = left > 0 ? e : 0;
             float p[8], g[8], m[8], v[8];
-            load8f(t.p + at8, left, p);
-            if (t.g_bf16) load8h((const uint16_t*)t.g + at8, left, g);
-            else          load8f((const float*)t.g + at8, left, g);
+            load8f<SMALL>(t.p + at8, left, p);
+            if (t.g_bf16) load8h<SMALL>((const uint16_t*)t.g + at8, left, g);
+            else          load8f<SMALL>((const float*)t.g + at8, left, g);
             if (SMALL) {
                 unsigned mc[2], vc[2];
                 load8c((const uint8_t*)t.m + at8, left, mc[0], mc[1]);
@@ -155,8 +165,8 @@ __global__ __launch_bounds__(kStepThreads) void adamw_step_kernel(const AdamwSte
                     v[i] = r * r;
                 }
             } else {
-                load8f((const float*)t.m + at8, left, m);
-                load8f((const float*)t.v + at8, left, v);
+                load8f<SMALL>((const float*)t.m + at8, left, m);
+                load8f<SMALL>((const float*)t.v + at8, left, v);
             }
             float r[8];
 #pragma unroll
@@ -167,7 +177,7 @@ __global__ __launch_bounds__(kStepThreads) void adamw_step_kernel(const AdamwSte
                 r[i] = __builtin_sqrtf(v[i]);
                 p[i] = p[i] * t.keep - __fdiv_rn(a.step_size * m[i], r[i] * a.root_scale + a.eps);
             }
-            store8f(t.p + at8, left, p);
+            store8f<SMALL>(t.p + at8, left, p);
             if (t.copy) store8h(t.copy + at8, left, p);
             if (SMALL) {
 #pragma unroll
@@ -193,8 +203,8 @@ __global__ __launch_bounds__(kStepThreads) void adamw_step_kernel(const AdamwSte
                     if ((lane & 15) == 0) { t.m_scale[at8 >> 7] = ms; t.v_scale[at8 >> 7] = vs; }
                 }
             } else {
-                store8f((float*)t.m + at8, left, m);
-                store8f((float*)t.v + at8, left, v);
+                store8f<SMALL>((float*)t.m + at8, left, m);
+                store8f<SMALL>((float*)t.v + at8, left, v);
             }
         }
     }
@@ -207,8 +217,7 @@ int64_t adamw_step_chunks(int64_t n) { return (n + kStepChunk - 1) / kStepChunk;
 hipError_t launch_adamw_step(const AdamwStepArgs& a, bool small, hipStream_t s)
 {
     if (a.chunks == 0) return hipSuccess;
-    const unsigned most = 2048;
-    const dim3 grid(a.chunks < most ? a.chunks : most);
+    const dim3 grid((unsigned)(a.chunks < kMostBlocks ? a.chunks : kMostBlocks));
     if (small) hipLaunchKernelGGL(adamw_step_kernel<true>, grid, dim3(kStepThreads), 0, s, a);
     else       hipLaunchKernelGGL(adamw_step_kernel<false>, grid, dim3(kStepThreads), 0, s, a);
     return hipGetLastError();

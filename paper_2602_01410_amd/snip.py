@@ -575,7 +575,7 @@ def snip_adamw_step(tensors: Sequence[AdamwTensor], lr: float, beta1: float, bet
     step) selects the random numbers by which 8-bit moments are rounded."""
     status = _nat().adamw_step(tensors, lr, beta1, beta2, eps, step, grad_scale, int(seed) & (2 ** 64 - 1), _handle_of(stream))
     if status:
-        raise SnipError(status, "snip_adamw_step", "snip_gemv")
+        raise SnipError(status, "snip_adamw_step")
 
 
 def snip_gemv(x: torch.Tensor, weights: Sequence[QTensor], out: Optional[Sequence[torch.Tensor]] = None, out_dtype: int = OUT_BF16, stream=None):

@@ -491,9 +491,14 @@ inline GradForm grad_form(int64_t rows, int64_t cols)
 {
     const int64_t groups = (cols + 7) / 8;
     GradForm f;
-    f.groups = groups <= 64 ? 1 : groups <= 128 ? 2 : groups <= 256 ? 4 : groups <= 512 ? 2 : groups <= 1024 ? 4 : 2;
-    f.waves = cols % 8 != 0 || groups > 2048 ? 0 : groups <= 256 ? 1 : groups <= 1024 ? 4 : 16;
-    const int64_t most = groups <= 256 ? 256 : groups <= 1024 ? 512 : 256, want = f.waves == 1 ? (rows + 3) / 4 : rows;
+    f.waves = cols % 8 != 0 || groups > 2048 ? 0 : groups <= 64 ? 1 : groups <= 1024 ? 4 : 16;
+    f.groups = f.waves == 1 || groups <= 256 ? 1 : groups <= 512 ? 2 : groups <= 1024 ? 4 : 2;
+    // Each workgroup's row of partial sums is written and read again: up to 512 of them (two per compute unit; 256 of 16 waves), from 256 on only one
+    // for eight rows.  us with 256 / 512 / 1024: [4096 x 2048] 20.5 / 16.5 / 17.5, [16384 x 4096] - / 96 / 106, [1501 x 2056] 10.3 / 11.2 / 12.3.
+    // Rows that are read twice are bound by latency: [4000 x 1001] 61 / 36 / 25.
+    const int64_t all = f.waves == 0 ? (groups <= 1024 ? 1024 : 512) : f.waves == 16 ? 256 : 512;
+    const int64_t some = f.waves == 0 || rows / 8 > all ? all : rows / 8 < 256 ? 256 : rows / 8;
+    const int64_t most = some < all ? some : all, want = f.waves == 1 ? (rows + 3) / 4 : rows;
     f.blocks = (int)(want < most ? want : most);
     return f;
 }
@@ -553,9 +558,8 @@ hipError_t launch_rms_norm_backward(NormGradArgs a, hipStream_t s)
     else if (f.waves == 0 && a.cols % 8 == 0) hipLaunchKernelGGL((norm_grad_any_kernel<16, false>), grid, dim3(1024), 0, s, a);
     else if (f.waves == 0 && wide) hipLaunchKernelGGL((norm_grad_any_kernel<16, true>), grid, dim3(1024), 0, s, a);
     else if (f.waves == 0) hipLaunchKernelGGL((norm_grad_any_kernel<4, true>), grid, dim3(256), 0, s, a);
-    else if (f.waves == 1 && f.groups == 1) SNIP_GRAD(1, 1);
-    else if (f.waves == 1 && f.groups == 2) SNIP_GRAD(1, 2);
-    else if (f.waves == 1) SNIP_GRAD(1, 4);
+    else if (f.waves == 1) SNIP_GRAD(1, 1);
+    else if (f.waves == 4 && f.groups == 1) SNIP_GRAD(4, 1);
     else if (f.waves == 4 && f.groups == 2) SNIP_GRAD(4, 2);
     else if (f.waves == 4) SNIP_GRAD(4, 4);
     else SNIP_GRAD(16, 2);

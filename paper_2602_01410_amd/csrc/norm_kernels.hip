@@ -493,12 +493,10 @@ inline GradForm grad_form(int64_t rows, int64_t cols)
     GradForm f;
     f.waves = cols % 8 != 0 || groups > 2048 ? 0 : groups <= 64 ? 1 : groups <= 1024 ? 4 : 16;
     f.groups = f.waves == 1 || groups <= 256 ? 1 : groups <= 512 ? 2 : groups <= 1024 ? 4 : 2;
-    // Each workgroup's row of partial sums is written and read again: up to 512 of them (two per compute unit; 256 of 16 waves), from 256 on only one
-    // for eight rows.  us with 256 / 512 / 1024: [4096 x 2048] 20.5 / 16.5 / 17.5, [16384 x 4096] - / 96 / 106, [1501 x 2056] 10.3 / 11.2 / 12.3.
-    // Rows that are read twice are bound by latency: [4000 x 1001] 61 / 36 / 25.
-    const int64_t all = f.waves == 0 ? (groups <= 1024 ? 1024 : 512) : f.waves == 16 ? 256 : 512;
-    const int64_t some = f.waves == 0 || rows / 8 > all ? all : rows / 8 < 256 ? 256 : rows / 8;
-    const int64_t most = some < all ? some : all, want = f.waves == 1 ? (rows + 3) / 4 : rows;
+    // Each workgroup's row of partial sums is written and read again: up to 512 of them (two workgroups per compute unit), 256 of 16 waves.  us with 256 /
+    // 512 / 1024: [1501 x 2056] 12.1 / 11.2 / 12.3, [4096 x 2048] - / 16.5 / 17.5, [16384 x 4096] - / 96 / 106; [4096 x 16384], 16 waves, 104 / 113 / 126.
+    // Rows that are read twice wait for memory more often than they are limited by it: [4000 x 1001] 61 / 36 / 25.
+    const int64_t most = f.waves == 0 ? (groups <= 1024 ? 1024 : 512) : f.waves == 16 ? 256 : 512, want = f.waves == 1 ? (rows + 3) / 4 : rows;
     f.blocks = (int)(want < most ? want : most);
     return f;
 }

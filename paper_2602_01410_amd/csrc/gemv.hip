@@ -15,7 +15,8 @@ namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef unsigned u4_any __attribute__((ext_vector_type(4), aligned(1)));
+typedef unsigned u1_any __attribute__((aligned(1)));
+constexpr int kSlot = 128 + 16;            // 16-byte units of LDS through which a wave's codes and scales go to their lanes
 
 __device__ __forceinline__ bf16x8 join(const bf16x2 (&p)[4])
 {
@@ -24,24 +25,26 @@ __device__ __forceinline__ bf16x8 join(const bf16x2 (&p)[4])
 // Elements 8 j .. 8 j + 7 of a lane's block.
 template <int FMT> struct Block;
 template <> struct Block<kFP4> {
-    uint4 c;
-    __device__ __forceinline__ void load(const uint8_t* p) { c = *reinterpret_cast<const uint4*>(p); }
-    __device__ __forceinline__ void clear() { c = make_uint4(0, 0, 0, 0); }
+    v4u_t c;
+    template <class F> __device__ __forceinline__ void get(F piece) { c = piece(0); }
+    __device__ __forceinline__ void load(const uint8_t* p) { c = *reinterpret_cast<const v4u_t*>(p); }
+    __device__ __forceinline__ void clear() { c = v4u_t{0, 0, 0, 0}; }
     template <int J> __device__ __forceinline__ bf16x8 elements(float sc) const
     {
-        const unsigned w = J == 0 ? c.x : J == 1 ? c.y : J == 2 ? c.z : c.w;
+        const unsigned w = c[J];
         const bf16x2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 0), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 1),
                              __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 2), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 3)};
         return join(p);
     }
 };
 template <> struct Block<kFP8> {
-    uint4 c, d;
-    __device__ __forceinline__ void load(const uint8_t* p) { c = *reinterpret_cast<const uint4*>(p); d = *reinterpret_cast<const uint4*>(p + 16); }
-    __device__ __forceinline__ void clear() { c = d = make_uint4(0, 0, 0, 0); }
+    v4u_t c, d;
+    template <class F> __device__ __forceinline__ void get(F piece) { c = piece(0); d = piece(1); }
+    __device__ __forceinline__ void load(const uint8_t* p) { c = *reinterpret_cast<const v4u_t*>(p); d = *reinterpret_cast<const v4u_t*>(p + 16); }
+    __device__ __forceinline__ void clear() { c = d = v4u_t{0, 0, 0, 0}; }
     template <int J> __device__ __forceinline__ bf16x8 elements(float sc) const
     {
-        const unsigned lo = J == 0 ? c.x : J == 1 ? c.z : J == 2 ? d.x : d.z, hi = J == 0 ? c.y : J == 1 ? c.w : J == 2 ? d.y : d.w;
+        const unsigned lo = J < 2 ? c[2 * J & 3] : d[2 * J & 3], hi = J < 2 ? c[(2 * J + 1) & 3] : d[(2 * J + 1) & 3];
         const bf16x2 p[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, sc, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, sc, true),
                              __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, sc, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, sc, true)};
         return join(p);
@@ -75,7 +78,7 @@ __device__ __forceinline__ void lds_barrier()
 }
 
 constexpr int HELD = 8;
-constexpr int64_t kLdsX = 128 * 1024;      // bytes of x in LDS
+constexpr int64_t kLdsX = 126 * 1024;      // bytes of x in LDS, beside sums (16 KB) and slots (18 KB)
 
 // Workgroup: WR x WS waves, `per` tiles of 16 RT WR rows of one weight, one after the other.  The WR waves of a share have 16 RT rows each
 // and the share's spans in common, whose elements of x they keep in LDS: all of them, or `chunk` spans at a time (then per is 1).  A wave
@@ -102,42 +105,75 @@ __device__ __forceinline__ void gemv_tiles(const GemvArgs& a, const GemvWeight& 
         codes = w.codes + first * nb * BYTES;
         scales = w.scales + first * nb;
 #pragma unroll
-        for (int r = 0; r < RT; ++r) row_at[r] = (unsigned)min(r * 16 + (lane & 15), (int)(w.n - 1 - first)) * nb;
+        for (int r = 0; r < RT; ++r) row_at[r] = (unsigned)min(r * 16 + (lane >> 2), (int)(w.n - 1 - first)) * nb;
     };
-    Block<FMT> c[RT][RING];
+    // Codes are asked for in the order of memory, four lanes to the 64 bytes (FP8: twice) of a row's span: with a lane loading the block that
+    // it needs every lane is an access of its own to the cache, which took longer than memory.  They go to their lanes through a slot of the
+    // wave's in LDS (whose operations are done in order: no wait between a span's use of it and the next one's).
+    constexpr int PIECES = BYTES / 16;                       // loads per lane and span
+    v4u_t c[RT][RING][PIECES];
+    const int piece_of = lane & 3, row_of = lane >> 2;
     auto fetch = [&](int u, int span) {
 #pragma unroll
-        for (int r = 0; r < RT; ++r) c[r][u].load(codes + (uint64_t)(row_at[r] + min(span * 4 + quarter, nb - 1)) * BYTES);
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const int b = min(span * 4 + (i * 4 + piece_of) / PIECES, nb - 1);
+                c[r][u][i] = *reinterpret_cast<const v4u_t*>(codes + (uint64_t)(row_at[r] + b) * BYTES + (i * 4 + piece_of) % PIECES * 16);
+            }
     };
-    // The scale bytes of a row come 16 at a time (byte by byte they take as long as the codes), a round of U spans ahead; lanes take theirs of
-    // the four of a span.  Where the row ends within the 16 they are read one by one.
+    v4u_t* const slot = reinterpret_cast<v4u_t*>(lds + wave * kSlot);
+    // piece p of row n lies where 16 rows' pieces of one lane quarter lie in different banks (FP8: at most two in one)
+    auto place_of = [](int n, int p) { return PIECES == 1 ? n * 4 + (p ^ (n >> 2 & 3)) : n * 8 + (p ^ (n & 7)); };
+    auto turn = [&](int r, int u) {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) slot[place_of(row_of, i * 4 + piece_of)] = c[r][u][i];
+        __builtin_amdgcn_wave_barrier();                     // (lanes read what others wrote)
+        Block<FMT> to;
+        to.get([&](int i) { return slot[place_of(lane & 15, quarter * PIECES + i)]; });
+        __builtin_amdgcn_wave_barrier();
+        return to;
+    };
+    // The scale bytes of a row come 16 at a time, four per lane, a round of U spans ahead, and to all lanes of the row through LDS as well.  Where the
+    // row ends within the 16 they are read one by one.
     constexpr int G = U / 4;
-    u4_any sc[RT][G], sc_next[RT][G];
+    v4u_t sc[RT][G];
+    unsigned sc_next[RT][G];
     const int full = nb / 16;
-    auto fetch_scales = [&](u4_any (&to)[RT][G], int span) {
+    auto fetch_scales = [&](int span) {
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             const int at = min(span / 4 + g, (nb - 1) / 16);
             if (at < full) {
 #pragma unroll
-                for (int r = 0; r < RT; ++r) to[r][g] = *reinterpret_cast<const u4_any*>(scales + row_at[r] + at * 16);
+                for (int r = 0; r < RT; ++r) sc_next[r][g] = *reinterpret_cast<const u1_any*>(scales + row_at[r] + at * 16 + piece_of * 4);
             } else {
 #pragma unroll
-                for (int r = 0; r < RT; ++r)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        unsigned d = 0;
-                        for (int i = 0; i < 4; ++i)
-                            if (at * 16 + k * 4 + i < nb) d |= (unsigned)scales[row_at[r] + at * 16 + k * 4 + i] << (8 * i);
-                        to[r][g][k] = d;
-                    }
+                for (int r = 0; r < RT; ++r) {
+                    unsigned d = 0;
+                    for (int i = 0; i < 4; ++i)
+                        if (at * 16 + piece_of * 4 + i < nb) d |= (unsigned)scales[row_at[r] + at * 16 + piece_of * 4 + i] << (8 * i);
+                    sc_next[r][g] = d;
+                }
             }
         }
     };
+    auto turn_scales = [&] {
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                reinterpret_cast<unsigned*>(slot + 128)[lane] = sc_next[r][g];
+                __builtin_amdgcn_wave_barrier();
+                sc[r][g] = slot[128 + (lane & 15)];
+                __builtin_amdgcn_wave_barrier();
+            }
+    };
     // x in LDS: 16-byte piece i of a token's 16 * chunk at i ^ (token & 15), so that 16 tokens' pieces lie in different banks
     const int per = 16 * chunk, pieces = tokens * per;
-    uint4* const mine = lds + share * (ALL ? 1 : 2) * pieces;
-    f32x4* const sums = reinterpret_cast<f32x4*>(lds + (ALL ? 1 : 2) * WS * pieces);        // [2][share][wave in share][RT TT][lane]
+    uint4* const xs = lds + WR * WS * kSlot;
+    uint4* const mine = xs + share * (ALL ? 1 : 2) * pieces;
+    f32x4* const sums = reinterpret_cast<f32x4*>(ALL ? xs + WS * pieces : xs);       // (chunks: in their place, when all are used)        // [2][share][wave in share][RT TT][lane]
     const unsigned one_over_per = 0xFFFFFFFFu / (unsigned)per + 1;           // p / per as a product: p < 2^16
     constexpr int STAGED = 8;                                              // pieces of a thread at a time: their loads wait together
     auto stage = [&](int ch) {
@@ -188,11 +224,15 @@ __device__ __forceinline__ void gemv_tiles(const GemvArgs& a, const GemvWeight& 
     constexpr int D = TT == 1 ? 4 : TT == 2 ? 2 : 1;         // how many matrix instructions ahead elements of x are read
     const int tiles = (w.n + ROWS - 1) / ROWS, first_tile = block * a.per, end_tile = min(first_tile + a.per, tiles);
     aim(first_tile);
-    fetch_scales(sc, begin);
+    fetch_scales(begin);
 #pragma unroll
     for (int u = 0; u < RING; ++u) fetch(u, begin + u);
     stage(0);
     __syncthreads();
+    turn_scales();
+    Block<FMT> now_c[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) now_c[r] = turn(r, 0);
     for (int tile = first_tile; tile < end_tile; ++tile) {
 #pragma unroll
         for (int r = 0; r < RT; ++r)
@@ -209,14 +249,23 @@ __device__ __forceinline__ void gemv_tiles(const GemvArgs& a, const GemvWeight& 
                     if (tile + 1 < end_tile) aim(tile + 1);
                     else { next = now; stride = 0; }
                 }
-                fetch_scales(sc_next, next);
+                fetch_scales(next);
                 bf16x8 v[D + 1][TT];
 #pragma unroll
                 for (int q = 0; q < D; ++q)
 #pragma unroll
                     for (int t = 0; t < TT; ++t) v[q][t] = __builtin_bit_cast(bf16x8, x[t][q % 4][at + (s + q / 4) * 16]);
+                fetch(0, RING < U ? now + RING : next);      // span 0's codes have gone to their lanes
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
+                    // the next span's codes go to their lanes and those of RING spans behind it are asked for (not moved down to their use)
+                    Block<FMT> next_c[RT];
+                    const int n1 = u + 1, in = n1 + RING;
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) next_c[r] = turn(r, n1 % RING);
+                    if (n1 < U) fetch(n1 % RING, in < U ? now + in : next + (in - U) * stride);
+                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const int q = u * 4 + j, n = q + D;
@@ -227,23 +276,18 @@ __device__ __forceinline__ void gemv_tiles(const GemvArgs& a, const GemvWeight& 
 #pragma unroll
                         for (int r = 0; r < RT; ++r) {
                             const float f = scale_operand((sc[r][u / 4][u % 4] >> (8 * quarter)) & 0xFFu);
-                            e[r] = j == 0 ? c[r][u % RING].template elements<0>(f) : j == 1 ? c[r][u % RING].template elements<1>(f)
-                                 : j == 2 ? c[r][u % RING].template elements<2>(f) : c[r][u % RING].template elements<3>(f);
+                            e[r] = j == 0 ? now_c[r].template elements<0>(f) : j == 1 ? now_c[r].template elements<1>(f)
+                                 : j == 2 ? now_c[r].template elements<2>(f) : now_c[r].template elements<3>(f);
                         }
 #pragma unroll
                         for (int r = 0; r < RT; ++r)
 #pragma unroll
                             for (int t = 0; t < TT; ++t) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(e[r], v[q % (D + 1)][t], acc[r][t], 0, 0, 0);
                     }
-                    // (not moved down to the next use: the loads have to be under way)
-                    __builtin_amdgcn_sched_barrier(0);
-                    fetch(u % RING, u + RING < U ? now + u + RING : next + (u + RING - U) * stride);
-                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) now_c[r] = next_c[r];
                 }
-#pragma unroll
-                for (int r = 0; r < RT; ++r)
-#pragma unroll
-                    for (int g = 0; g < G; ++g) sc[r][g] = sc_next[r][g];
+                turn_scales();
             }
             if (!ALL) {
                 // into the other buffer, which all have read before the last barrier; codes under way are not waited for
@@ -261,7 +305,7 @@ __device__ __forceinline__ void gemv_tiles(const GemvArgs& a, const GemvWeight& 
                 for (int t = 0; t < TT; ++t) store(wr, r * TT + t, acc[r][t]);
         } else {
             constexpr int PARTS = WR * RT * TT;
-            f32x4* const here = sums + (tile & 1) * WS * PARTS * 64;
+            f32x4* const here = sums + (ALL ? tile & 1 : 0) * WS * PARTS * 64;
 #pragma unroll
             for (int r = 0; r < RT; ++r)
 #pragma unroll
@@ -357,8 +401,9 @@ template <int TT, int RT, int U, int WR, int WS, bool ALL> hipError_t launch(Gem
         blocks += ((a.w[i].n + ROWS - 1) / ROWS + a.per - 1) / a.per;
     }
     const size_t x = (size_t)(ALL ? 1 : 2) * WS * tokens * a.chunk * 256, sums = WS > 1 ? (size_t)2 * WS * WR * RT * TT * 1024 : 0;
-    if (x + sums > 160 * 1024) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((gemv_kernel<TT, RT, U, WR, WS, ALL>), dim3((unsigned)blocks, (a.m + 16 * TT - 1) / (16 * TT)), dim3(WR * WS * 64), x + sums, s, a);
+    const size_t lds = (size_t)WR * WS * kSlot * 16 + (ALL ? x + sums : x > sums ? x : sums);
+    if (lds > 160 * 1024) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((gemv_kernel<TT, RT, U, WR, WS, ALL>), dim3((unsigned)blocks, (a.m + 16 * TT - 1) / (16 * TT)), dim3(WR * WS * 64), lds, s, a);
     return hipGetLastError();
 }
 

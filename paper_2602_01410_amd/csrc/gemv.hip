@@ -230,9 +230,11 @@ __device__ __forceinline__ void gemv_tiles(const GemvArgs& a, const GemvWeight& 
     stage(0);
     __syncthreads();
     turn_scales();
+    constexpr bool EARLY = RT == 1;                          // (two rows' tiles leave no registers for it)
     Block<FMT> now_c[RT];
 #pragma unroll
-    for (int r = 0; r < RT; ++r) now_c[r] = turn(r, 0);
+    for (int r = 0; r < RT; ++r)
+        if (EARLY) now_c[r] = turn(r, 0);
     for (int tile = first_tile; tile < end_tile; ++tile) {
 #pragma unroll
         for (int r = 0; r < RT; ++r)
@@ -255,15 +257,16 @@ __device__ __forceinline__ void gemv_tiles(const GemvArgs& a, const GemvWeight& 
                 for (int q = 0; q < D; ++q)
 #pragma unroll
                     for (int t = 0; t < TT; ++t) v[q][t] = __builtin_bit_cast(bf16x8, x[t][q % 4][at + (s + q / 4) * 16]);
-                fetch(0, RING < U ? now + RING : next);      // span 0's codes have gone to their lanes
+                if (EARLY) fetch(0, RING < U ? now + RING : next);               // span 0's codes have gone to their lanes
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    // the next span's codes go to their lanes and those of RING spans behind it are asked for (not moved down to their use)
+                    // This span's codes, or early the next one's, go to their lanes, and those of RING spans behind are asked for (not moved down to
+                    // their use).
                     Block<FMT> next_c[RT];
-                    const int n1 = u + 1, in = n1 + RING;
+                    const int n1 = EARLY ? u + 1 : u, in = n1 + RING;
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int r = 0; r < RT; ++r) next_c[r] = turn(r, n1 % RING);
+                    for (int r = 0; r < RT; ++r) (EARLY ? next_c[r] : now_c[r]) = turn(r, n1 % RING);
                     if (n1 < U) fetch(n1 % RING, in < U ? now + in : next + (in - U) * stride);
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -285,7 +288,8 @@ __device__ __forceinline__ void gemv_tiles(const GemvArgs& a, const GemvWeight& 
                             for (int t = 0; t < TT; ++t) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(e[r], v[q % (D + 1)][t], acc[r][t], 0, 0, 0);
                     }
 #pragma unroll
-                    for (int r = 0; r < RT; ++r) now_c[r] = next_c[r];
+                    for (int r = 0; r < RT; ++r)
+                        if (EARLY) now_c[r] = next_c[r];
                 }
                 turn_scales();
             }

@@ -1,12 +1,17 @@
 // Few tokens against quantized weights: y[t][n] = sum_k x[t][k] w[n][k] with x in bf16 as it is and w = code * 2^(scale - 127), FP4 or
 // FP8 with a scale per 32 elements.  What a model answers with: every weight is read once for a handful of tokens, so the floor is
-// the weights' bytes (0.53 or 1.03 per weight) over the memory's rate.
+// the weights' bytes (0.53 or 1.03 per weight) over the memory's rate, 7.4 TB/s of reads.
 //
 // Codes become bf16 (exact: at most four significant bits, the scale is a power of two) and go to v_mfma_f32_16x16x32_bf16 with fp32
 // accumulators, 16 rows of w by 16 tokens at a time: on the vector unit four tokens would already take longer than the weights' way from
-// memory.  A lane owns one block of 32 elements of one row (16 bytes of FP4, 32 of FP8) in each span of 128: the four lanes of a
+// memory.  A lane multiplies one block of 32 elements of one row (16 bytes of FP4, 32 of FP8) in each span of 128: the four lanes of a
 // row take the span's four blocks, and matrix instruction j contracts elements 8 j .. 8 j + 7 of all four, for which a lane
-// reads the same elements of x.  So a block has one lane's scale, codes come in the widest loads and nothing is exchanged.
+// reads the same elements of x.  So a block has one lane and one scale.
+//
+// Measured (graph replays on four sets of weights), us per call and TB/s: FP4, one token 2 x [28672 x 8192] 49 (5.1), 3 x [4096 x 4096] 8.3 (3.2), [4096
+// x 11008] 9.6 (2.5), [512 x 512] 2.3; 16, 32, 48, 64 tokens 2 x [28672 x 8192] 62, 66-71, 73-75, 84 (4.0, 3.7, 3.4, 3.0); FP8, 48 tokens 118
+// (4.2).  One token is bound by memory's latency (8 waves on a compute unit, each with 4 KB under way, wait most of the time; twice as much under way is
+// no faster), 48 tokens by LDS and matrix cores taking turns on a span (two waves per SIMD), small problems by the launch.
 #include "snip_internal.h"
 #include "quant_common.h"
 
@@ -77,7 +82,7 @@ __device__ __forceinline__ void lds_barrier()
     asm volatile("" ::: "memory");
 }
 
-constexpr int HELD = 8;
+constexpr int HELD = 8;                    // 16-byte pieces of x that a thread holds on their way to LDS
 constexpr int64_t kLdsX = 126 * 1024;      // bytes of x in LDS, beside sums (16 KB) and slots (18 KB)
 
 // Workgroup: WR x WS waves, `per` tiles of 16 RT WR rows of one weight, one after the other.  The WR waves of a share have 16 RT rows each
@@ -419,8 +424,8 @@ hipError_t launch_gemv(GemvArgs a, hipStream_t s)
     int64_t tiles = 0;                                       // of 16 rows
     for (int i = 0; i < a.count; ++i) tiles += (a.w[i].n + 15) / 16;
     const int64_t spans = (a.k / kBlock + 3) / 4;
-    // Up to 24 spans in up to 8000 / spans workgroups: us with the small kernel / the others: 1 token [4096 x 2048] 3.5 / 4.4, [4096 x 4096] (not
-    // taken) 5.4 / 5.2, 9 tokens 2 x [1003 x 2080] 3.8 / 6.2, 3 x [4096 x 2048] (not taken) 8.9 / 7.2, 64 tokens 2 x [1003 x 2080] (not) 7.6 / 8.9.
+    // Up to 24 spans in up to 8000 / spans workgroups: us with the small kernel / the others: 1 token [512 x 512] 2.3 / 4.2, [4096 x 2048] 3.5 / 4.3,
+    // [4096 x 4096] (not taken) 5.6 / 5.1, 9 tokens 2 x [1003 x 2080] 3.8 / 6.3, 3 x [4096 x 2048] (not) 9.0 / 6.8, 24 tokens [4096 x 2048] (not) 6.9 / 6.1.
     const int64_t small = tiles * ((a.m + 15) / 16);
     if (spans <= 24 && small * spans <= 8000) {
         int blocks = 0;
@@ -431,19 +436,16 @@ hipError_t launch_gemv(GemvArgs a, hipStream_t s)
         hipLaunchKernelGGL(gemv_small_kernel, dim3(blocks, (a.m + 15) / 16), dim3(kSmallWaves * 64), 0, s, a);
         return hipGetLastError();
     }
-    // Up to 16 tokens whose x fits LDS as a whole: tiles of 16 rows, eight waves a tile where there are few, four where there are many (x is small) or
-    // eight that take two tiles (more tokens: the share of a wave's spans in x is read for two).  us: 1 token 3 x [4096 x 4096] 9.9 / 8.9 / 10.1, [4096 x
-    // 11008] 11.3 / 12.0 / -, 8 tokens 3 x [4096 x 4096] - / 11.4 / 10.0, 2 x [28672 x 8192], 1 token 50.5 / 50.9 / 51.3.
+    // Up to 16 tokens whose x fits LDS as a whole: eight waves on 16 rows where there are few of them, on 32 where there are many (a share's part of x is
+    // read for two tiles, and a workgroup per compute unit goes through several).  us, 16 / 32 rows: 1 token [4096 x 4096] 5.0 / 5.4, [4096 x
+    // 11008] 9.6 / 10.4, 3 x [4096 x 4096] 11.0 / 8.3, 2 x [28672 x 8192] 50.4 / 48.9, 8 tokens 3 x [4096 x 4096] 12.6 / 9.0.
     auto whole = [&](int shares) { return a.m <= 16 && shares * a.m * (((spans + shares - 1) / shares + 3) / 4 * 4) * 256 <= kLdsX; };
     if (tiles <= 512 && whole(8)) return launch<1, 1, 4, 1, 8, true>(a, s, 512);
-    if (tiles > 512 && whole(4)) {
-        if ((int64_t)a.m * a.k <= 16384) return launch<1, 1, 4, 1, 4, true>(a, s, 512);
-        return launch<1, 1, 4, 2, 4, true>(a, s, 256);
-    }
+    if (tiles > 512 && whole(4)) return launch<1, 1, 4, 2, 4, true>(a, s, 256);
     // Otherwise x comes in chunks.  Of the tiles (256, 128, 64 or 32 rows, 16 to 64 tokens) the one with the most workgroups that still run at once, one
-    // per compute unit: us with 256 / 128 / 64 / 32 rows, 16 tokens: 2 x [28672 x 8192] 67 / 72 / 82 / -, 2 x [11008 x 4096] 26 / 16 / 23 / 25, 3 x
-    // [4096 x 4096] 26 / 16 / 12 / 18, [4096 x 11008] 66 / 38 / 26 / 20; 48 tokens 3 x [4096 x 4096] in tiles of 128 rows by 48 / 32 / 16
-    // tokens 26 / 19 / 30.
+    // per compute unit: us with 256 / 128 / 64 / 32 rows, 16 tokens: 2 x [28672 x 8192] 62 / 68 / 79 / 93, 2 x [11008 x 4096] 19 / 15 / 21 / 24, 3 x
+    // [4096 x 4096] 19 / 14 / 11 / 16, [4096 x 11008] 46 / 31 / 22 / 17; 48 tokens 2 x [28672 x 8192] in tiles of 256 rows by 48 / 32 / 16
+    // tokens 73 / 104 / 137, 3 x [4096 x 4096] of 128 rows 27 / 20 / 25 (of 256 by 16 18).
     const int cus = gemm_compute_units();
     int64_t most = 0;
     int form = 0, tt = 0;                                    // rows of a workgroup's tile: 256, 128, 64, 32

@@ -355,7 +355,8 @@ double snip_weight_divergence(double alpha, double beta1, double beta2, int64_t 
  *   out_col : the same down columns, stored transposed (cols x rows), the operand of snip_gemm_wgrad; rows a multiple of 32, cols
  *             even.  Needs rstd, and with a residual sum (SNIP_ERR_NULL otherwise).  The two formats may differ.
  * At least one output has to be given (SNIP_ERR_NULL).  A row with an infinity or a NaN gets NaNs; blocks that hold one get scale
- * byte 0xFF and zero codes, as in snip_quantize.  Columns >= cols of sum and y are not touched. */
+ * byte 0xFF and zero codes, as in snip_quantize.  Columns >= cols of sum and y are not touched.  But for sum no output may overlap
+ * an input or another output. */
 snip_status snip_rms_norm(const void* x, int64_t rows, int64_t cols, int64_t ld, const void* residual, int64_t ld_residual,
                           const void* weight, snip_out_dtype weight_dtype, float eps, snip_scale_rule rule,
                           void* sum, int64_t ld_sum, float* rstd, void* y, int64_t ld_y,

@@ -6,6 +6,12 @@
 //
 // Rows: a row's elements stay in registers between the sum of squares and the outputs, so x and r are read once.  Columns need
 // the norms of 32 rows first: norm_col_kernel runs behind the row kernel and reads h again, with rstd.
+//
+// Measured (graph replays on three sets of tensors; bf16 x and residual, h stored), us and TB/s of the least bytes: [16384 x 4096] FP8 along rows 86 (5.4),
+// down columns 111, both 126 (4.3), bf16 y 95 (5.6); [4096 x 2048] 13.2 (4.5), 18, 21 (3.2); [1 x 4096] 2.6.  The row kernel is bound by memory from some
+// thousand rows on, the column kernel (40 us of the 126 for 203 MB) by h's way back from the last-level cache, as far as it is there, and from memory;
+// few rows by the launch and one chain load - sum - gain - store.  Loads that stream (past the caches) would keep h there but
+// cost small calls their residual: [4096 x 2048] 13.1 -> 16.5.
 #include "snip_internal.h"
 #include "quant_common.h"
 
@@ -328,9 +334,10 @@ template <int W, bool RAGGED> void launch_any_row(const NormArgs& a, hipStream_t
 
 // ---- gradient ------------------------------------------------------------------------------------------------------------------
 // With g = dy w and h normed by rstd:   dx = rstd (g - h rstd^2 mean(g h)) + dsum,   dw = sum over rows of dy h rstd.
-// 6 (8 with dsum) bytes per element.  A lane owns the same columns of every row that its workgroup takes, so that the sums of dw stay
-// in registers until the workgroup's rows are done; then they go to a row of `partials`, and grad_sum_kernel adds those in a fixed
-// order.
+// 6 (8 with dsum) bytes per element.  Measured with dsum, us and TB/s: [8192 x 8192] 98 (5.5), [16384 x 4096] 96 (5.6), [4096 x 2048] 16.1 (4.2);
+// without [1501 x 2056] 10.2; [1 x 4096] 4.7, two launches.  Bound by memory where there are many rows.  A lane owns the same columns of every row
+// that its workgroup takes, so that the sums of dw stay in registers until the workgroup's rows are done; then they go to a row of
+// `partials`, and grad_sum_kernel adds those in a fixed order.
 
 __device__ __forceinline__ void grad8(const float (&g)[8], const float (&h)[8], const uint4* dsum, float rstd, float coef, float (&dx)[8])
 {
@@ -491,10 +498,12 @@ inline GradForm grad_form(int64_t rows, int64_t cols)
 {
     const int64_t groups = (cols + 7) / 8;
     GradForm f;
-    f.waves = cols % 8 != 0 || groups > 2048 ? 0 : groups <= 64 ? 1 : groups <= 1024 ? 4 : 16;
-    f.groups = f.waves == 1 || groups <= 256 ? 1 : groups <= 512 ? 2 : groups <= 1024 ? 4 : 2;
+    // us with fewer / more waves: [16384 x 512] 1 / 4 19.4 / 31.4; two groups per lane of 4 waves / one of 8 [1 x 4096] 5.2 / 4.8, [1501 x 2056] 11.0 /
+    // 10.2, [16384 x 4096] 98 / 94; four of 4 / one of 16 [1 x 8192] 6.4 / 5.4, [1024 x 8192] 19.6 / 17.7, [8192 x 8192] 98 / 99.
+    f.waves = cols % 8 != 0 || groups > 2048 ? 0 : groups <= 64 ? 1 : groups <= 256 ? 4 : groups <= 512 ? 8 : 16;
+    f.groups = groups > 1024 ? 2 : 1;
     // Each workgroup's row of partial sums is written and read again: up to 512 of them (two workgroups per compute unit), 256 of 16 waves.  us with 256 /
-    // 512 / 1024: [1501 x 2056] 12.1 / 11.2 / 12.3, [4096 x 2048] - / 16.5 / 17.5, [16384 x 4096] - / 96 / 106; [4096 x 16384], 16 waves, 104 / 113 / 126.
+    // 512: [4096 x 2048] 21.0 / 16.4, [1501 x 2056] 11.0 / 10.2, [16384 x 4096] 102 / 94; [16384 x 8192], 16 waves, 184.5 / 184.6, [4096 x 16384] 104 / 113.
     // Rows that are read twice wait for memory more often than they are limited by it: [4000 x 1001] 61 / 36 / 25.
     const int64_t most = f.waves == 0 ? (groups <= 1024 ? 1024 : 512) : f.waves == 16 ? 256 : 512, want = f.waves == 1 ? (rows + 3) / 4 : rows;
     f.blocks = (int)(want < most ? want : most);
@@ -509,15 +518,24 @@ hipError_t launch_rms_norm(const NormArgs& a, hipStream_t s)
 {
     if (a.rows == 0) return hipSuccess;
     const int groups = (a.cols + 7) / 8;
+    // Waves and groups of eight per lane, by the columns and, where a row's own chain of latencies counts, by the rows.  us of row kernels with FP8
+    // codes, fewer against more waves: [16384 x 512] 1 x 1 / 4 x 1 13.0 / 21.9; 1024 columns 1 x 2 / 4 x 1 rows 1 3.0 / 2.6, 512 3.6 / 3.3, 1024 3.9 /
+    // 4.0, 16384 25.7 / 30.8; 2048 columns 1 x 4 / 4 x 1 rows 1 4.4 / 2.7, 1024 6.5 / 4.9, 16384 47.4 / 46.5; 4096 columns 4 x 2 / 8 x 1 rows 1 3.4 / 2.8, 512 5.5 /
+    // 5.1, 2048 12.9 / 13.3; 8192 columns 8 x 2 / 16 x 1 (4 x 4) rows 1 3.5 / 3.3 (5.1), 512 8.4 / 8.0, 1024 12.9 / 13.9 (13.4), 16384 165 / 173 (166).  Read
+    // twice, bf16 output, 4 / 16 waves: [1 x 4097] 5.3 / 4.0, [256 x 2049] 5.2 / 4.6, [512 x 2049] 6.1 / 7.3, [256 x 1001] 4.4 / 4.4, [4096 x 9001] 79 / 104,
+    // [4096 x 20001] 164 / 160.
+    const bool few = a.rows <= 512;
     if (a.cols % 8 != 0) {
-        if (groups <= 1024) launch_any_row<4, true>(a, s);
-        else                launch_any_row<16, true>(a, s);
+        if (groups > 2048 || (groups > 128 && a.rows <= 256)) launch_any_row<16, true>(a, s);
+        else                                                  launch_any_row<4, true>(a, s);
     }
     else if (groups <= 64) launch_row<1, 1>(a, s);
-    else if (groups <= 128) launch_row<1, 2>(a, s);
-    else if (groups <= 256) launch_row<1, 4>(a, s);
+    else if (groups <= 128 && !few) launch_row<1, 2>(a, s);
+    else if (groups <= 256) launch_row<4, 1>(a, s);
+    else if (groups <= 512 && few) launch_row<8, 1>(a, s);
     else if (groups <= 512) launch_row<4, 2>(a, s);
-    else if (groups <= 1024) launch_row<4, 4>(a, s);
+    else if (groups <= 1024 && few) launch_row<16, 1>(a, s);
+    else if (groups <= 1024) launch_row<8, 2>(a, s);
     else if (groups <= 2048) launch_row<16, 2>(a, s);
     else if (groups <= 4096) launch_row<16, 4>(a, s);
     else launch_any_row<16, false>(a, s);
@@ -557,9 +575,9 @@ hipError_t launch_rms_norm_backward(NormGradArgs a, hipStream_t s)
     else if (f.waves == 0 && wide) hipLaunchKernelGGL((norm_grad_any_kernel<16, true>), grid, dim3(1024), 0, s, a);
     else if (f.waves == 0) hipLaunchKernelGGL((norm_grad_any_kernel<4, true>), grid, dim3(256), 0, s, a);
     else if (f.waves == 1) SNIP_GRAD(1, 1);
-    else if (f.waves == 4 && f.groups == 1) SNIP_GRAD(4, 1);
-    else if (f.waves == 4 && f.groups == 2) SNIP_GRAD(4, 2);
-    else if (f.waves == 4) SNIP_GRAD(4, 4);
+    else if (f.waves == 4) SNIP_GRAD(4, 1);
+    else if (f.waves == 8) SNIP_GRAD(8, 1);
+    else if (f.groups == 1) SNIP_GRAD(16, 1);
     else SNIP_GRAD(16, 2);
 #undef SNIP_GRAD
     hipError_t e = hipGetLastError();

@@ -161,6 +161,24 @@ def test_codes(rows, cols, fr, fc, rule):
         check_codes(got.col, np.ascontiguousarray(ref.T), rule)
 
 
+@pytest.mark.parametrize("rows,cols", [(544, 544), (544, 1024), (512, 1024), (544, 2080), (544, 4096), (513, 4104), (520, 8192), (257, 1033), (257, 2049), (256, 1033), (100, 1033)])
+def test_many_rows(rows, cols):
+    """A row's waves depend on the number of rows too."""
+    rng = np.random.default_rng(rows * 7 + cols)
+    x, r, w = rows_of(rng, rows, cols), rows_of(rng, rows, cols), gain_of(rng, cols, False)
+    out = snip.snip_rms_norm(x, w, 1e-5, residual=r, y=empty_rows(rows, cols), fmt_row=snip.FP8 if cols % 32 == 0 else None,
+                             fmt_col=snip.FP4 if rows % 32 == 0 and cols % 2 == 0 else None)
+    h = f64(out.sum)
+    assert (h == f64(bf16(x.float() + r.float()))).all()
+    rstd, y = reference(h, f64(w), 1e-5)
+    assert (np.abs(f64(out.rstd) / rstd - 1) <= DELTA).all()
+    between(f64(out.y), y)
+    if out.row is not None:
+        check_codes(out.row, y, snip.NO_OVERFLOW)
+    if out.col is not None:
+        check_codes(out.col, y.T, snip.NO_OVERFLOW)
+
+
 @pytest.mark.parametrize("rows", [1, 3, 50])
 def test_row_codes_of_any_number_of_rows(rows):
     rng = np.random.default_rng(rows)

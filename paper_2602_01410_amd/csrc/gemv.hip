@@ -8,9 +8,9 @@
 // row take the span's four blocks, and matrix instruction j contracts elements 8 j .. 8 j + 7 of all four, for which a lane
 // reads the same elements of x.  So a block has one lane and one scale.
 //
-// Measured (graph replays on four sets of weights), us per call and TB/s: FP4, one token 2 x [28672 x 8192] 49 (5.1), 3 x [4096 x 4096] 8.3 (3.2), [4096
-// x 11008] 9.6 (2.5), [512 x 512] 2.3; 16, 32, 48, 64 tokens 2 x [28672 x 8192] 62, 66-71, 73-75, 84 (4.0, 3.7, 3.4, 3.0); FP8, 48 tokens 118
-// (4.2).  One token is bound by memory's latency (8 waves on a compute unit, each with 4 KB under way, wait most of the time; twice as much under way is
+// Measured (graph replays on four sets of weights), us per call and TB/s: FP4, one token 2 x [28672 x 8192] 50 (5.0), 3 x [4096 x 4096] 8.4 (3.2), [4096
+// x 11008] 9.6 (2.5), [512 x 512] 2.3; 16, 32, 48, 64 tokens 2 x [28672 x 8192] 63, 63, 73, 82 (4.0, 4.0, 3.5, 3.1); FP8, one token 85 (5.7), 48 tokens 109
+// (4.5).  One token is bound by memory's latency (8 waves on a compute unit, each with 4 KB under way, wait most of the time; twice as much under way is
 // no faster), 48 tokens by LDS and matrix cores taking turns on a span (two waves per SIMD), small problems by the launch.
 #include "snip_internal.h"
 #include "quant_common.h"

@@ -416,15 +416,35 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void norm_grad_kernel(NormGr
             store8<false>(a.dx + row * a.lddx, col, a.cols, pack8(dx));
         }
     }
-    if (a.partials && first < a.rows)
+    if (!a.partials) return;
+    if (W == 1) {
+        // the four rows' sums become one, in the order of the waves (those without a row have zeros); with a row of partial sums per wave [2048 x 512] took 11.4 us
+        // and [16384 x 512] 19.5, now 6.5 and 15.3
+        __shared__ float4 joined[W == 1 ? 3 : 1][CH][2][64];
+        if (wave > 0)
 #pragma unroll
-        for (int j = 0; j < CH; ++j) {
-            const int64_t col = ((int64_t)j * W * 64 + lane_in_row) * 8;
-            if (col >= a.cols) break;
-            float4* const to = reinterpret_cast<float4*>(a.partials + first * a.pitch + col);
-            to[0] = make_float4(dw[j][0], dw[j][1], dw[j][2], dw[j][3]);
-            to[1] = make_float4(dw[j][4], dw[j][5], dw[j][6], dw[j][7]);
-        }
+            for (int j = 0; j < CH; ++j) {
+                joined[wave - 1][j][0][lane_in_row] = make_float4(dw[j][0], dw[j][1], dw[j][2], dw[j][3]);
+                joined[wave - 1][j][1][lane_in_row] = make_float4(dw[j][4], dw[j][5], dw[j][6], dw[j][7]);
+            }
+        __syncthreads();
+        if (wave > 0) return;
+        for (int k = 0; k < 3; ++k)
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                const float4 p = joined[k][j][0][lane_in_row], q = joined[k][j][1][lane_in_row];
+                dw[j][0] += p.x; dw[j][1] += p.y; dw[j][2] += p.z; dw[j][3] += p.w;
+                dw[j][4] += q.x; dw[j][5] += q.y; dw[j][6] += q.z; dw[j][7] += q.w;
+            }
+    }
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+        const int64_t col = ((int64_t)j * W * 64 + lane_in_row) * 8;
+        if (col >= a.cols) break;
+        float4* const to = reinterpret_cast<float4*>(a.partials + blockIdx.x * a.pitch + col);
+        to[0] = make_float4(dw[j][0], dw[j][1], dw[j][2], dw[j][3]);
+        to[1] = make_float4(dw[j][4], dw[j][5], dw[j][6], dw[j][7]);
+    }
 }
 
 // Rows of any length: read twice, the sums of dw kept in the workgroup's row of `partials`.
@@ -498,7 +518,7 @@ inline GradForm grad_form(int64_t rows, int64_t cols)
 {
     const int64_t groups = (cols + 7) / 8;
     GradForm f;
-    // us with fewer / more waves: [16384 x 512] 1 / 4 19.4 / 31.4; two groups per lane of 4 waves / one of 8 [1 x 4096] 5.2 / 4.8, [1501 x 2056] 11.0 /
+    // us with fewer / more waves: 512 columns 1 / 4 rows 1024 5.3 / 6.7, 16384 15.3 / 31.0; two groups per lane of 4 waves / one of 8 [1 x 4096] 5.2 / 4.8, [1501 x 2056] 11.0 /
     // 10.2, [16384 x 4096] 98 / 94; four of 4 / one of 16 [1 x 8192] 6.4 / 5.4, [1024 x 8192] 19.6 / 17.7, [8192 x 8192] 98 / 99.
     f.waves = cols % 8 != 0 || groups > 2048 ? 0 : groups <= 64 ? 1 : groups <= 256 ? 4 : groups <= 512 ? 8 : 16;
     f.groups = groups > 1024 ? 2 : 1;
@@ -510,7 +530,6 @@ inline GradForm grad_form(int64_t rows, int64_t cols)
     return f;
 }
 inline int64_t grad_pitch(int64_t cols) { return (cols + 7) / 8 * 8; }
-inline int64_t grad_partials(const GradForm& f, int64_t rows) { const int64_t n = f.blocks * (int64_t)(f.waves == 1 ? 4 : 1); return n < rows ? n : rows; }
 
 }  // namespace
 
@@ -553,7 +572,7 @@ hipError_t launch_rms_norm(const NormArgs& a, hipStream_t s)
 
 size_t norm_workspace_bytes(int64_t rows, int64_t cols)
 {
-    return (size_t)grad_partials(grad_form(rows, cols), rows) * (size_t)grad_pitch(cols) * sizeof(float);
+    return (size_t)grad_form(rows, cols).blocks * (size_t)grad_pitch(cols) * sizeof(float);
 }
 
 hipError_t launch_rms_norm_backward(NormGradArgs a, hipStream_t s)
@@ -582,7 +601,7 @@ hipError_t launch_rms_norm_backward(NormGradArgs a, hipStream_t s)
 #undef SNIP_GRAD
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.dgain) return e;
-    hipLaunchKernelGGL(grad_sum_kernel, dim3((a.cols + 31) / 32), dim3(1024), 0, s, a.partials, (int)grad_partials(f, a.rows), a.pitch, a.cols, a.dgain);
+    hipLaunchKernelGGL(grad_sum_kernel, dim3((a.cols + 31) / 32), dim3(1024), 0, s, a.partials, f.blocks, a.pitch, a.cols, a.dgain);
     return hipGetLastError();
 }
 

@@ -518,10 +518,11 @@ inline GradForm grad_form(int64_t rows, int64_t cols)
 {
     const int64_t groups = (cols + 7) / 8;
     GradForm f;
-    // us with fewer / more waves: 512 columns 1 / 4 rows 1024 5.3 / 6.7, 16384 15.3 / 31.0; two groups per lane of 4 waves / one of 8 [1 x 4096] 5.2 / 4.8, [1501 x 2056] 11.0 /
+    // us with fewer / more waves: 512 columns 1 / 4 rows 1024 5.3 / 6.7, 16384 15.3 / 31.0; 1024 columns 1 / 4 rows 64 5.2 / 4.9, 512 5.6 / 6.6, 16384 29.8 / 43.4;
+    // 2048 columns 1 / 4 rows 64 6.4 / 5.2, 1024 9.7 / 9.1, 16384 54.8 / 53.6; two groups per lane of 4 waves / one of 8 [1 x 4096] 5.2 / 4.8, [1501 x 2056] 11.0 /
     // 10.2, [16384 x 4096] 98 / 94; four of 4 / one of 16 [1 x 8192] 6.4 / 5.4, [1024 x 8192] 19.6 / 17.7, [8192 x 8192] 98 / 99.
-    f.waves = cols % 8 != 0 || groups > 2048 ? 0 : groups <= 64 ? 1 : groups <= 256 ? 4 : groups <= 512 ? 8 : 16;
-    f.groups = groups > 1024 ? 2 : 1;
+    f.waves = cols % 8 != 0 || groups > 2048 ? 0 : groups <= 64 || (groups <= 128 && rows > 256) ? 1 : groups <= 256 ? 4 : groups <= 512 ? 8 : 16;
+    f.groups = groups > 1024 || (f.waves == 1 && groups > 64) ? 2 : 1;
     // Each workgroup's row of partial sums is written and read again: up to 512 of them (two workgroups per compute unit), 256 of 16 waves.  us with 256 /
     // 512: [4096 x 2048] 21.0 / 16.4, [1501 x 2056] 11.0 / 10.2, [16384 x 4096] 102 / 94; [16384 x 8192], 16 waves, 184.5 / 184.6, [4096 x 16384] 104 / 113.
     // Rows that are read twice wait for memory more often than they are limited by it: [4000 x 1001] 61 / 36 / 25.
@@ -593,7 +594,8 @@ hipError_t launch_rms_norm_backward(NormGradArgs a, hipStream_t s)
     else if (f.waves == 0 && a.cols % 8 == 0) hipLaunchKernelGGL((norm_grad_any_kernel<16, false>), grid, dim3(1024), 0, s, a);
     else if (f.waves == 0 && wide) hipLaunchKernelGGL((norm_grad_any_kernel<16, true>), grid, dim3(1024), 0, s, a);
     else if (f.waves == 0) hipLaunchKernelGGL((norm_grad_any_kernel<4, true>), grid, dim3(256), 0, s, a);
-    else if (f.waves == 1) SNIP_GRAD(1, 1);
+    else if (f.waves == 1 && f.groups == 1) SNIP_GRAD(1, 1);
+    else if (f.waves == 1) SNIP_GRAD(1, 2);
     else if (f.waves == 4) SNIP_GRAD(4, 1);
     else if (f.waves == 8) SNIP_GRAD(8, 1);
     else if (f.groups == 1) SNIP_GRAD(16, 1);

@@ -276,6 +276,12 @@ def test_gradient(rows, cols, dsum):
     assert torch.equal(ds if dsum else dy, was)
 
 
+@pytest.mark.parametrize("rows,cols", [(256, 1024), (257, 520), (301, 1024), (2050, 1016), (1501, 2056), (260, 16384)])
+def test_gradient_of_many_rows(rows, cols):
+    """A row's waves depend on the number of rows too; bounds as above."""
+    test_gradient(rows, cols, True)
+
+
 def test_gradient_against_differences():
     """Central differences of sum(dy y) in 64 bits; their own error is of the order of step^2."""
     rng = np.random.default_rng(11)

@@ -140,7 +140,8 @@ __device__ __forceinline__ void gemv_tiles(const GemvArgs& a, const GemvWeight& 
         return to;
     };
     // The scale bytes of a row come 16 at a time, four per lane, a round of U spans ahead, and to all lanes of the row through LDS as well.  Where the
-    // row ends within the 16 they are read one by one.
+    // row ends within the 16 or before them they are read one by one, and bytes past its last block are zero: the codes that repeat the last block
+    // there are then small, where the scale of another block could make them infinite (times x's zeros: NaN).
     constexpr int G = U / 4;
     v4u_t sc[RT][G];
     unsigned sc_next[RT][G];
@@ -148,7 +149,7 @@ __device__ __forceinline__ void gemv_tiles(const GemvArgs& a, const GemvWeight& 
     auto fetch_scales = [&](int span) {
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            const int at = min(span / 4 + g, (nb - 1) / 16);
+            const int at = span / 4 + g;
             if (at < full) {
 #pragma unroll
                 for (int r = 0; r < RT; ++r) sc_next[r][g] = *reinterpret_cast<const u1_any*>(scales + row_at[r] + at * 16 + piece_of * 4);

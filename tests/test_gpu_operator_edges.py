@@ -1,0 +1,34 @@
+"""Corners of the norm, optimizer and few-token calls: rows that end inside a round of loads, scales at the ends of their range, dtypes,
+what holds the tensors of a call, calls without the gains' gradient, large tensors' forms."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2602_01410_amd import snip
+
+pytestmark = pytest.mark.gpu
+
+# tokens, rows, columns whose last spans lie behind the row's end, in each form of the few-token kernel; the last one in the small one
+BEHIND = [(1, 40, 3328), (1, 9000, 3328), (3, 40, 5120), (16, 40, 11008), (16, 5000, 14336), (20, 300, 5120), (33, 1000, 4640), (48, 300, 11008), (64, 40, 3328),
+          (64, 9000, 3328), (5, 40, 224)]
+
+
+@pytest.mark.parametrize("fmt", [snip.FP4, snip.FP8])
+@pytest.mark.parametrize("m,n,k", BEHIND)
+def test_large_scales_beside_large_codes_in_the_last_block(m, n, k, fmt):
+    """Small codes under scales close to the largest (2^125 and 2^120 each) and, in the last block, the largest code under a scale of 2^-7: all weights
+    are finite, and so are the outputs; the last block is below a unit in the last place of them.  k equal positive products are within k 2^-24 of their sum.
+    Row 1 has an infinite weight in its last block, row 2 a scale byte that is no number."""
+    small, large, byte, per = (0x11, 0x77, 253, 16) if fmt == snip.FP4 else (0x38, 0x7E, 247, 32)
+    codes = torch.full((n, k // 32 * per), small, dtype=torch.uint8, device="cuda")
+    scales = torch.full((n, k // 32), byte, dtype=torch.uint8, device="cuda")
+    codes[:, -per:] = large
+    scales[:, -1] = 120
+    scales[1, -1] = 254
+    scales[2, 0] = 255
+    x = (torch.arange(m, device="cuda").float() + 1).mul(2.0 ** -20)[:, None].expand(m, k).bfloat16().contiguous()
+    y = snip.snip_gemv(x, [snip.QTensor(codes, scales, n, k, fmt)], out_dtype=snip.OUT_FP32)[0].double().cpu().numpy()
+    want = x[:, 0].double().cpu().numpy() * (k - 32) * 2.0 ** (125 if fmt == snip.FP4 else 120)
+    assert (y[:, 1] == np.inf).all() and np.isnan(y[:, 2]).all()
+    rest = np.delete(y, (1, 2), 1)
+    assert (np.abs(rest / want[:, None] - 1) <= k * 2.0 ** -24).all()

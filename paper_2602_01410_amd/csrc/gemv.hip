@@ -14,6 +14,7 @@
 // no faster), 48 tokens by LDS and matrix cores taking turns on a span (two waves per SIMD), small problems by the launch.
 #include "snip_internal.h"
 #include "quant_common.h"
+#include "x_pieces.h"
 
 namespace snip {
 namespace {
@@ -207,15 +208,15 @@ __device__ __forceinline__ void gemv_tiles(const GemvArgs& a, const GemvWeight& 
 #pragma unroll
         for (int h = 0; h < HELD; ++h) {
             const int p = min(tid + h * THREADS, pieces - 1), token = (int)__umulhi(p, one_over_per), i = p - token * per;
-            const int k = min((begin + ch * chunk) * 128 + i * 8, a.k - 8);
-            held[h] = *reinterpret_cast<const uint4*>(a.x + (int64_t)(token0 + token) * a.ldx + k);
+            const int at = min(x_piece(begin, ch, chunk, i), x_pieces(a.k) - 1);
+            held[h] = *reinterpret_cast<const uint4*>(a.x + (int64_t)(token0 + token) * a.ldx + piece_element(at));
         }
     };
     auto put = [&](int ch) {
 #pragma unroll
         for (int h = 0; h < HELD; ++h) {
             const int p = min(tid + h * THREADS, pieces - 1), token = (int)__umulhi(p, one_over_per), i = p - token * per;
-            if ((begin + ch * chunk) * 128 + i * 8 >= a.k) held[h] = make_uint4(0, 0, 0, 0);
+            if (x_piece(begin, ch, chunk, i) >= x_pieces(a.k)) held[h] = make_uint4(0, 0, 0, 0);
             mine[(ch & 1) * pieces + token * per + (i ^ (token & 15))] = held[h];
         }
     };

@@ -32,3 +32,17 @@ def test_large_scales_beside_large_codes_in_the_last_block(m, n, k, fmt):
     assert (y[:, 1] == np.inf).all() and np.isnan(y[:, 2]).all()
     rest = np.delete(y, (1, 2), 1)
     assert (np.abs(rest / want[:, None] - 1) <= k * 2.0 ** -24).all()
+
+
+def test_longest_rows():
+    """k = 2^31 - 32: x is 4 GB, its last chunk ends 32 elements before 2^31.  Few elements of x are not zero, so that the sums are exact."""
+    n, k = 2, (1 << 31) - 32
+    codes = torch.full((n, k // 2), 0x11, dtype=torch.uint8, device="cuda")              # 0.5
+    codes[1] = 0xA2                                                                      # 1 and -1 in turn
+    scales = torch.full((n, k // 32), 127, dtype=torch.uint8, device="cuda")
+    x = torch.zeros((1, k), dtype=torch.bfloat16, device="cuda")
+    at = [0, 5, 4097, k // 2, k - 32768, k - 33, k - 1]
+    for i, c in enumerate(at):
+        x[0, c] = 2.0 ** i
+    y = snip.snip_gemv(x, [snip.QTensor(codes, scales, n, k, snip.FP4)], out_dtype=snip.OUT_FP32)[0].cpu().tolist()
+    assert y == [[sum(2.0 ** i for i in range(len(at))) / 2, sum((-1.0) ** (c % 2) * 2.0 ** i for i, c in enumerate(at))]]

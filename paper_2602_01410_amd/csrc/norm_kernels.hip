@@ -325,11 +325,12 @@ __global__ __launch_bounds__(256) void norm_col_kernel(NormArgs a, const uint16_
 template <int W, int CH> void launch_row(const NormArgs& a, hipStream_t s)
 {
     const int64_t groups = W == 1 ? ((int64_t)a.rows + 3) / 4 : a.rows;
-    hipLaunchKernelGGL((norm_row_kernel<W, CH>), dim3((unsigned)(groups < kMostBlocks ? groups : kMostBlocks)), dim3(W == 1 ? 256 : W * 64), 0, s, a);
+    constexpr int threads = W == 1 ? 256 : W * 64;
+    hipLaunchKernelGGL((norm_row_kernel<W, CH>), dim3((unsigned)(groups < most_blocks(threads) ? groups : most_blocks(threads))), dim3(threads), 0, s, a);
 }
 template <int W, bool RAGGED> void launch_any_row(const NormArgs& a, hipStream_t s)
 {
-    hipLaunchKernelGGL((norm_any_row_kernel<W, RAGGED>), dim3((unsigned)(a.rows < kMostBlocks ? a.rows : kMostBlocks)), dim3(W * 64), 0, s, a);
+    hipLaunchKernelGGL((norm_any_row_kernel<W, RAGGED>), dim3((unsigned)(a.rows < most_blocks(W * 64) ? a.rows : most_blocks(W * 64))), dim3(W * 64), 0, s, a);
 }
 
 // ---- gradient ------------------------------------------------------------------------------------------------------------------
@@ -498,17 +499,21 @@ __global__ __launch_bounds__(W * 64) void norm_grad_any_kernel(NormGradArgs a)
 __global__ __launch_bounds__(1024) void grad_sum_kernel(const float* __restrict__ partials, int n, int64_t pitch, int cols, float* __restrict__ dw)
 {
     __shared__ float shares[32][33];
-    const int c = blockIdx.x * 32 + (threadIdx.x & 31), g = threadIdx.x >> 5;
-    float s = 0.f;
-    if (c < cols)
+    const int g = threadIdx.x >> 5;
+    for (int c0 = blockIdx.x * 32; c0 < cols; c0 += gridDim.x * 32) {
+        const int c = c0 + (threadIdx.x & 31);
+        float s = 0.f;
+        if (c < cols)
 #pragma unroll 4
-        for (int p = g; p < n; p += 32) s += partials[p * pitch + c];
-    shares[g][threadIdx.x & 31] = s;
-    __syncthreads();
-    if (g == 0 && c < cols) {
-        double t = 0.0;
-        for (int i = 0; i < 32; ++i) t += shares[i][threadIdx.x];
-        dw[c] = (float)t;
+            for (int p = g; p < n; p += 32) s += partials[p * pitch + c];
+        shares[g][threadIdx.x & 31] = s;
+        __syncthreads();
+        if (g == 0 && c < cols) {
+            double t = 0.0;
+            for (int i = 0; i < 32; ++i) t += shares[i][threadIdx.x];
+            dw[c] = (float)t;
+        }
+        __syncthreads();
     }
 }
 
@@ -603,7 +608,8 @@ hipError_t launch_rms_norm_backward(NormGradArgs a, hipStream_t s)
 #undef SNIP_GRAD
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.dgain) return e;
-    hipLaunchKernelGGL(grad_sum_kernel, dim3((a.cols + 31) / 32), dim3(1024), 0, s, a.partials, f.blocks, a.pitch, a.cols, a.dgain);
+    const int groups = (a.cols + 31) / 32, most = (int)most_blocks(1024);
+    hipLaunchKernelGGL(grad_sum_kernel, dim3(groups < most ? groups : most), dim3(1024), 0, s, a.partials, f.blocks, a.pitch, a.cols, a.dgain);
     return hipGetLastError();
 }
 

@@ -184,4 +184,8 @@ constexpr bool qb_streams(long long rows, long long cols, bool fp8_rows, bool fp
     return rows * row + cols * column >= (fp8_rows || fp8_columns ? 128ll << 20 : 256ll << 20);
 }
 
+// ---- workgroups of a launch whose kernel takes turns where there are more units ----
+// A launch counts its threads in 32 bits: 2^31 of them at most, with up to 512 in a workgroup 2^22 workgroups.
+constexpr long long most_blocks(int threads) { return (1ll << 31) / (threads < 512 ? 512 : threads); }
+
 }  // namespace snip

@@ -18,7 +18,7 @@ constexpr int kBlock = 32;  // elements per scale
 constexpr int kStreamBlocks = 2048;
 constexpr int kWavesPerBlock = 4;
 constexpr int kStreamWaves = kStreamBlocks * kWavesPerBlock;
-constexpr int64_t kMostBlocks = (int64_t)1 << 22;    // workgroups of a launch that needs no slot per workgroup (threads are counted in 32 bits)
+constexpr int64_t kMostBlocks = most_blocks(512);    // workgroups of up to 512 threads of a launch that needs no slot per workgroup
 constexpr int kMaxColSplits = 64;    // row splits of the column-statistics kernel
 // Workspace of the streaming kernels: partial sums, for one block direction [kStreamWaves][3] fp32 of waves, for both at most
 // [kStreamBlocks][6] fp64 of workgroups; then [kMaxColSplits][cols][3] fp32 per-column partials for the per-line column

@@ -46,3 +46,35 @@ def test_longest_rows():
         x[0, c] = 2.0 ** i
     y = snip.snip_gemv(x, [snip.QTensor(codes, scales, n, k, snip.FP4)], out_dtype=snip.OUT_FP32)[0].cpu().tolist()
     assert y == [[sum(2.0 ** i for i in range(len(at))) / 2, sum((-1.0) ** (c % 2) * 2.0 ** i for i, c in enumerate(at))]]
+
+
+def test_more_rows_than_workgroups():
+    """2^22 + 3 rows of 16 waves each (69 GB) are 2^32 threads and more; the rows of a second turn have their own norms."""
+    rows, cols = (1 << 22) + 3, 8200
+    x = torch.zeros((rows, cols), dtype=torch.bfloat16, device="cuda")
+    at = torch.tensor([0, 1, (1 << 21) - 1, 1 << 21, (1 << 21) + 1, (1 << 22) - 1, 1 << 22, rows - 1], device="cuda")
+    x[at] = (torch.arange(len(at), device="cuda") + 1).bfloat16()[:, None]
+    rstd = torch.full((rows,), -1.0, device="cuda")
+    w = torch.ones(cols, device="cuda")
+    # no output but rstd: through the C call, since the binding's always delivers y or codes
+    assert snip._lib().snip_rms_norm(x.data_ptr(), rows, cols, cols, None, 0, w.data_ptr(), 1, 1.0, 0, None, 0, rstd.data_ptr(), None, 0, None, None, None) == 0
+    torch.cuda.synchronize()
+    want = 1 / np.sqrt(1 + (np.arange(len(at)) + 1.0) ** 2)
+    assert (np.abs(rstd[at].double().cpu().numpy() / want - 1) <= 3e-6).all()
+    rstd[at] = 1.0
+    assert bool((rstd == 1).all())
+    del x
+    torch.cuda.empty_cache()
+
+
+def test_more_columns_than_a_launch_sums():
+    """Gains' gradients of 2^27 + 8 columns, 32 a workgroup of 1024 threads: more than 2^32 threads."""
+    cols = (1 << 27) + 8
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    dy, h = (torch.randint(-8, 9, (2, cols), generator=gen, device="cuda").bfloat16() for _ in range(2))
+    w = torch.ones(cols, dtype=torch.bfloat16, device="cuda")
+    _, dw = snip.snip_rms_norm_backward(dy, h, w, torch.tensor([1.0, 0.5], device="cuda"))
+    want = dy[0].float() * h[0].float() + dy[1].float() * h[1].float() * 0.5                    # (few bits: exact)
+    assert torch.equal(dw, want)
+    del dy, h, dw, want
+    torch.cuda.empty_cache()

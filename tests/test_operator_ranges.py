@@ -62,3 +62,19 @@ def test_places_in_elements_are_noticed(tmp_path):
     (tmp_path / "x_pieces.h").write_text(wrong)
     res = run(tmp_path, PIECES, tmp_path)
     assert res.returncode == 1 and "element -" in res.stdout, res.stdout
+
+
+def test_threads_of_a_launch(tmp_path):
+    """A launch counts its threads in 32 bits."""
+    program = r"""
+#include <cstdio>
+#include "picks.h"
+int main()
+{
+    for (int threads = 64; threads <= 1024; threads += 64)
+        if (snip::most_blocks(threads) * threads >= 1ll << 32 || snip::most_blocks(threads) < 1 << 21) { std::printf("%d\n", threads); return 1; }
+    return 0;
+}
+"""
+    res = run(tmp_path, program)
+    assert res.returncode == 0, res.stdout

@@ -368,7 +368,8 @@ snip_status snip_rms_norm(const void* x, int64_t rows, int64_t cols, int64_t ld,
  *   dy, h, dsum, dx: device, bf16, rows and pitches as above; h is `sum` (or x) and rstd that of the forward call; dsum, the
  *             gradient that reaches h past the norm, may be NULL.  dx may be dy or dsum itself.
  *   dweight : device, fp32 [cols], or NULL.
- *   workspace: device, needed with dweight, >= snip_rms_norm_workspace_bytes(rows, cols) bytes, 16-byte aligned.
+ *   workspace: device, needed with dweight, >= snip_rms_norm_workspace_bytes(rows, cols) bytes, 16-byte aligned.  The size never falls as
+ *             rows or cols grow: a workspace for the largest matrix serves all that are no larger in either extent.
  * Sums are fp32 and added in a fixed order (those of workgroups in double). */
 size_t snip_rms_norm_workspace_bytes(int64_t rows, int64_t cols);
 snip_status snip_rms_norm_backward(const void* dy, int64_t rows, int64_t cols, int64_t ld_dy, const void* h, int64_t ld_h,

@@ -485,7 +485,7 @@ snip_status snip_rms_norm_backward(const void* dy, int64_t rows, int64_t cols, i
     if (!rstd && rows > 0) return SNIP_ERR_NULL;
     if ((reinterpret_cast<uintptr_t>(rstd) | reinterpret_cast<uintptr_t>(dweight)) & 3u) return SNIP_ERR_LAYOUT;
     if (dweight && rows > 0) {
-        if (!workspace || workspace_bytes_ < norm_workspace_bytes(rows, cols)) return SNIP_ERR_WORKSPACE;
+        if (!workspace || workspace_bytes_ < norm_workspace_needed(rows, cols)) return SNIP_ERR_WORKSPACE;
         if (!aligned16(workspace)) return SNIP_ERR_LAYOUT;
     }
     NormGradArgs a = {};

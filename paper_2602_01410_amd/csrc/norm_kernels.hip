@@ -576,9 +576,15 @@ hipError_t launch_rms_norm(const NormArgs& a, hipStream_t s)
     return hipGetLastError();
 }
 
-size_t norm_workspace_bytes(int64_t rows, int64_t cols)
+size_t norm_workspace_needed(int64_t rows, int64_t cols)
 {
     return (size_t)grad_form(rows, cols).blocks * (size_t)grad_pitch(cols) * sizeof(float);
+}
+// The most that any call of at most these extents needs: 1024 workgroups up to 8192 columns (rows that are read twice), 512 beyond.
+size_t norm_workspace_bytes(int64_t rows, int64_t cols)
+{
+    const int64_t narrow = (rows < 1024 ? rows : 1024) * (cols < 8192 ? grad_pitch(cols) : 8192), wide = (rows < 512 ? rows : 512) * grad_pitch(cols);
+    return (size_t)(narrow > wide ? narrow : wide) * sizeof(float);
 }
 
 hipError_t launch_rms_norm_backward(NormGradArgs a, hipStream_t s)

@@ -189,7 +189,8 @@ struct NormGradArgs {
     int rows, cols;
     int64_t pitch = 0;                       // of `partials`
 };
-size_t norm_workspace_bytes(int64_t rows, int64_t cols);
+size_t norm_workspace_needed(int64_t rows, int64_t cols);      // by a call of these extents
+size_t norm_workspace_bytes(int64_t rows, int64_t cols);       // by any call of at most these extents
 hipError_t launch_rms_norm_backward(NormGradArgs a, hipStream_t s);
 
 // The paper's own recipe (real-valued scale per 1x128 tile or 128x128 block): quantize (stats == nullptr)

@@ -78,3 +78,13 @@ def test_more_columns_than_a_launch_sums():
     assert torch.equal(dw, want)
     del dy, h, dw, want
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("rows,cols,smaller", [(512, 1024, [(256, 1024), (200, 1024), (257, 1017), (512, 520)]), (4096, 8192, [(4096, 8191), (1500, 4097), (700, 1001)]),
+                                               (1100, 16384, [(1100, 8191), (1024, 4095), (513, 16377)])])
+def test_workspace_of_the_largest_matrix_serves_the_others(rows, cols, smaller):
+    workspace = torch.empty(snip.rms_norm_workspace_bytes(rows, cols), dtype=torch.uint8, device="cuda")
+    for r, c in smaller:
+        dy, h = (torch.ones((r, (c + 7) // 8 * 8), dtype=torch.bfloat16, device="cuda")[:, :c] for _ in range(2))
+        _, dw = snip.snip_rms_norm_backward(dy, h, torch.ones(c, device="cuda"), torch.ones(r, device="cuda"), workspace=workspace)
+        assert bool((dw == r).all())

@@ -78,3 +78,19 @@ int main()
 """
     res = run(tmp_path, program)
     assert res.returncode == 0, res.stdout
+
+
+def test_workspace_of_the_gradient_grows_with_the_matrix():
+    """A workspace sized for a program's largest matrix serves the smaller ones: over the changes of the kernel's form, the size falls neither
+    with the rows nor with the columns."""
+    from paper_2602_01410_amd import snip
+    rows = [0, 1, 2, 3, 4, 5, 8, 63, 64, 65, 200, 255, 256, 257, 260, 300, 511, 512, 513, 1023, 1024, 1025, 2047, 2048, 2049, 4096, 16384, 1 << 20, (1 << 31) - 1]
+    cols = [1, 7, 8, 9, 505, 511, 512, 513, 520, 1016, 1023, 1024, 1025, 1032, 2047, 2048, 2049, 2056, 4095, 4096, 4097, 4104, 8184, 8191, 8192, 8193, 8200, 16383, 16384,
+            16385, 16392, 40001, 1 << 20]
+    size = snip.rms_norm_workspace_bytes
+    for a, b in zip(rows, rows[1:]):
+        for c in cols:
+            assert size(a, c) <= size(b, c), (a, b, c)
+    for a, b in zip(cols, cols[1:]):
+        for r in rows:
+            assert size(r, a) <= size(r, b), (r, a, b)

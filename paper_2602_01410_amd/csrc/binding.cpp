@@ -54,7 +54,8 @@ bool source(PyObject* o, Source& s)
 {
     const at::Tensor* t;
     if (!tensor(o, t)) return false;
-    if (t->dim() != 2 || t->element_size() != 2 || !t->is_cuda()) {
+    const at::ScalarType type = t->scalar_type();
+    if (t->dim() != 2 || (type != at::kBFloat16 && type != at::kShort && type != at::kUInt16) || !t->is_cuda()) {
         PyErr_SetString(PyExc_ValueError, "expected a 2-D CUDA tensor of bf16 (or its uint16/int16 bit patterns)");
         return false;
     }

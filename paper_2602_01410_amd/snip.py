@@ -237,8 +237,11 @@ def make_plan(entry: Sequence[int]) -> _PlanC:
     return _PlanC(*[int(v) for v in entry])
 
 
+_BF16_BITS = (torch.bfloat16, torch.int16, torch.uint16)
+
+
 def _src(x: torch.Tensor):
-    if x.dim() != 2 or x.element_size() != 2 or not x.is_cuda:
+    if x.dim() != 2 or x.dtype not in _BF16_BITS or not x.is_cuda:
         raise ValueError("expected a 2-D CUDA tensor of bf16 (or its uint16/int16 bit patterns)")
     if x.stride(1) != 1:
         raise ValueError("rows must be contiguous")

@@ -88,3 +88,23 @@ def test_workspace_of_the_largest_matrix_serves_the_others(rows, cols, smaller):
         dy, h = (torch.ones((r, (c + 7) // 8 * 8), dtype=torch.bfloat16, device="cuda")[:, :c] for _ in range(2))
         _, dw = snip.snip_rms_norm_backward(dy, h, torch.ones(c, device="cuda"), torch.ones(r, device="cuda"), workspace=workspace)
         assert bool((dw == r).all())
+
+
+def test_half_precision_is_not_bf16():
+    """fp16 has bf16's size; its bits mean other numbers.  Bit patterns in 16-bit integers are taken as bf16's, as before."""
+    x = torch.randn(32, 64, device="cuda")
+    h, b, w, rstd = x.half(), x.bfloat16(), torch.ones(64, device="cuda"), torch.ones(32, device="cuda")
+    q = snip.alloc_qtensor(32, 64, snip.FP8)
+    weight = snip.snip_quantize(b, snip.FP8, snip.ROW)
+    stats = torch.zeros(3, dtype=torch.float64, device="cuda")
+    ws = snip.alloc_workspace(32, 64, x.device)
+    for bad in (lambda: snip.snip_rms_norm(h, w, 1e-5), lambda: snip.snip_rms_norm(b, w, 1e-5, residual=h), lambda: snip.snip_rms_norm(b, w, 1e-5, residual=b, sum=h),
+                lambda: snip.snip_rms_norm(b, w, 1e-5, y=h), lambda: snip.snip_rms_norm_backward(h, b, w, rstd), lambda: snip.snip_rms_norm_backward(b, h, w, rstd),
+                lambda: snip.snip_rms_norm_backward(b, b, w, rstd, dsum=h), lambda: snip.snip_rms_norm_backward(b, b, w, rstd, dx=h), lambda: snip.snip_gemv(h, [weight]),
+                lambda: snip.snip_quantize(h, snip.FP8), lambda: snip.snip_quantize(h, snip.FP8, out=q), lambda: snip.snip_quantize_both(h, snip.FP8, snip.FP4),
+                lambda: snip.snip_quant_error_stats(h, snip.ROW, snip.NO_OVERFLOW, stats, workspace=ws)):
+        with pytest.raises(ValueError):
+            bad()
+    for bits in (torch.int16, torch.uint16):
+        assert torch.equal(snip.snip_rms_norm(b.view(bits), w, 1e-5).y, snip.snip_rms_norm(b, w, 1e-5).y)
+        assert torch.equal(snip.snip_quantize(b.view(bits), snip.FP8).codes, snip.snip_quantize(b, snip.FP8).codes)

@@ -334,18 +334,26 @@ bool adamw_tensor(PyObject* o, snip_adamw_tensor& t)
     t.grad_dtype = gt == at::kFloat ? SNIP_OUT_FP32 : SNIP_OUT_BF16;
     return !PyErr_Occurred();
 }
+// The objects of a sequence until the end of the call: an iterable's are held by nobody else, and their memory is the caller's only as long as they are.
+struct Items {
+    PyObject* seq;
+    Items(PyObject* o, const char* message) : seq(PySequence_Fast(o, message)) {}
+    ~Items() { Py_XDECREF(seq); }
+    Items(const Items&) = delete;
+    Items& operator=(const Items&) = delete;
+    Py_ssize_t size() const { return PySequence_Fast_GET_SIZE(seq); }
+    PyObject* operator[](Py_ssize_t i) const { return PySequence_Fast_GET_ITEM(seq, i); }
+};
 // (tensors, lr, beta1, beta2, eps, step, grad_scale, seed, stream)
 PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
     if (!count(n, 9)) return nullptr;
-    PyObject* seq = PySequence_Fast(a[0], "expected a sequence of tensors with their moments");
-    if (!seq) return nullptr;
-    const Py_ssize_t len = PySequence_Fast_GET_SIZE(seq);
+    const Items items(a[0], "expected a sequence of tensors with their moments");
+    if (!items.seq) return nullptr;
+    const Py_ssize_t len = items.size();
     std::vector<snip_adamw_tensor> ts((size_t)len);
-    bool ok = true;
-    for (Py_ssize_t i = 0; ok && i < len; ++i) ok = adamw_tensor(PySequence_Fast_GET_ITEM(seq, i), ts[(size_t)i]);
-    Py_DECREF(seq);                                 // (the caller's sequence keeps the objects)
-    if (!ok) return nullptr;
+    for (Py_ssize_t i = 0; i < len; ++i)
+        if (!adamw_tensor(items[i], ts[(size_t)i])) return nullptr;
     const double lr = PyFloat_AsDouble(a[1]), b1 = PyFloat_AsDouble(a[2]), b2 = PyFloat_AsDouble(a[3]), eps = PyFloat_AsDouble(a[4]);
     int64_t step; void *gs, *s; snip_out_dtype d32;
     if (PyErr_Occurred() || !integer(a[5], step) || !vector(a[6], 1, true, gs, d32)) return nullptr;
@@ -359,29 +367,26 @@ PyObject* gemv(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
     Source x; int64_t dt; void* s;
     if (!count(n, 5) || !source(a[0], x) || !integer(a[3], dt) || !stream(a[4], s)) return nullptr;
-    PyObject* ws = PySequence_Fast(a[1], "expected a sequence of quantized weights");
-    if (!ws) return nullptr;
-    PyObject* ys = PySequence_Fast(a[2], "expected a sequence of outputs");
-    if (!ys) { Py_DECREF(ws); return nullptr; }
-    const Py_ssize_t len = PySequence_Fast_GET_SIZE(ws);
+    const Items ws(a[1], "expected a sequence of quantized weights");
+    if (!ws.seq) return nullptr;
+    const Items ys(a[2], "expected a sequence of outputs");
+    if (!ys.seq) return nullptr;
+    const Py_ssize_t len = ws.size();
     std::vector<snip_qtensor> w((size_t)len);
     std::vector<void*> y((size_t)len);
     std::vector<int64_t> ld((size_t)len);
-    bool ok = PySequence_Fast_GET_SIZE(ys) == len;
-    if (!ok) PyErr_SetString(PyExc_ValueError, "expected as many outputs as weights");
-    for (Py_ssize_t i = 0; ok && i < len; ++i) {
+    if (ys.size() != len) { PyErr_SetString(PyExc_ValueError, "expected as many outputs as weights"); return nullptr; }
+    for (Py_ssize_t i = 0; i < len; ++i) {
         const at::Tensor* t;
-        ok = qtensor(PySequence_Fast_GET_ITEM(ws, i), w[(size_t)i]) && tensor(PySequence_Fast_GET_ITEM(ys, i), t);
-        if (!ok) break;
-        ok = t->dim() == 2 && t->is_cuda() && t->size(0) == x.rows && t->size(1) == w[(size_t)i].rows && (t->stride(1) == 1 || t->size(1) <= 1) &&
-             t->scalar_type() == (dt == SNIP_OUT_FP32 ? at::kFloat : at::kBFloat16);
-        if (!ok) { PyErr_SetString(PyExc_ValueError, "expected CUDA matrices of the output type, a row for each token and a column for each row of the weight"); break; }
+        if (!qtensor(ws[i], w[(size_t)i]) || !tensor(ys[i], t)) return nullptr;
+        if (t->dim() != 2 || !t->is_cuda() || t->size(0) != x.rows || t->size(1) != w[(size_t)i].rows || (t->stride(1) != 1 && t->size(1) > 1) ||
+            t->scalar_type() != (dt == SNIP_OUT_FP32 ? at::kFloat : at::kBFloat16)) {
+            PyErr_SetString(PyExc_ValueError, "expected CUDA matrices of the output type, a row for each token and a column for each row of the weight");
+            return nullptr;
+        }
         y[(size_t)i] = t->data_ptr();
         ld[(size_t)i] = t->stride(0);
     }
-    Py_DECREF(ws);
-    Py_DECREF(ys);
-    if (!ok) return nullptr;
     return call([&] { return p_gemv(x.p, x.rows, x.cols, x.ld, w.data(), y.data(), ld.data(), (int32_t)len, (snip_out_dtype)dt, s); });
 }
 

@@ -108,3 +108,38 @@ def test_half_precision_is_not_bf16():
     for bits in (torch.int16, torch.uint16):
         assert torch.equal(snip.snip_rms_norm(b.view(bits), w, 1e-5).y, snip.snip_rms_norm(b, w, 1e-5).y)
         assert torch.equal(snip.snip_quantize(b.view(bits), snip.FP8).codes, snip.snip_quantize(b, snip.FP8).codes)
+
+
+def test_tensors_of_an_iterable_are_held_until_the_call_is_launched():
+    """Nobody but the iterable has them; what the end of the last reference does (here: it zeroes an input, on the same stream) comes after the
+    launch."""
+    class Param(snip.AdamwTensor):
+        def __del__(self):
+            self.grad.zero_()
+
+    class Weight(snip.QTensor):
+        def __del__(self):
+            self.codes.zero_()
+
+    n, params = 5000, []
+
+    def tensors():
+        for _ in range(3):
+            t = Param(*(torch.full((n,), v, device="cuda") for v in (1.0, 1.0, 0.0, 0.0)))
+            params.append((t.param, t.m, t.grad))
+            yield t
+            del t
+
+    snip.snip_adamw_step(tensors(), 1e-2, 0.75, 0.75, 1e-8, 1)
+    for p, m, g in params:
+        assert bool((g == 0).all()) and bool((m == 0.25).all()) and bool(((p - 0.99).abs() < 1e-5).all())
+
+    def weights(codes):
+        for c in codes:
+            yield Weight(c, torch.full((40, 2), 127, dtype=torch.uint8, device="cuda"), 40, 64, snip.FP4)
+
+    codes = [torch.full((40, 32), 0x22, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    outs = [torch.zeros((4, 40), device="cuda") for _ in codes]
+    x = torch.ones((4, 64), device="cuda").bfloat16()
+    snip.snip_gemv(x, weights(codes), outs)
+    assert all(bool((c == 0).all()) for c in codes) and all(bool((y == 64).all()) for y in outs)

@@ -531,17 +531,21 @@ def rms_norm_workspace_bytes(rows: int, cols: int) -> int:
 
 def snip_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, rstd: torch.Tensor,
                            dsum: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
-                           dweight: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+                           dweight: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None, gains: bool = True):
     """Gradients (dx bf16, dweight fp32) of snip_rms_norm from that of y; h: the forward call's sum, or its x without a residual; dsum: the
-    gradient that reaches h past the norm.  dx may be dy or dsum."""
-    if dx is None or dweight is None or workspace is None:
+    gradient that reaches h past the norm.  dx may be dy or dsum.  gains=False (frozen gains): dx alone, dweight is None."""
+    if not gains:
+        if dweight is not None:
+            raise ValueError("dweight without the gains' gradient")
+        workspace = None
+    if dx is None or (gains and (dweight is None or workspace is None)):
         _, rows, cols, _ = _src(dy)
         with _alloc_on(stream):
             if dx is None:
                 dx = _alloc_rows(rows, cols, dy.device)
-            if dweight is None:
+            if gains and dweight is None:
                 dweight = torch.empty(cols, dtype=torch.float32, device=dy.device)
-            if workspace is None:
+            if gains and workspace is None:
                 workspace = torch.empty(rms_norm_workspace_bytes(rows, cols), dtype=torch.uint8, device=dy.device)
     status = _nat().rms_norm_backward(dy, h, weight, rstd, dsum, dx, dweight, workspace, _handle_of(stream))
     if status:

@@ -143,3 +143,16 @@ def test_tensors_of_an_iterable_are_held_until_the_call_is_launched():
     x = torch.ones((4, 64), device="cuda").bfloat16()
     snip.snip_gemv(x, weights(codes), outs)
     assert all(bool((c == 0).all()) for c in codes) and all(bool((y == 64).all()) for y in outs)
+
+
+@pytest.mark.parametrize("rows,cols", [(0, 64), (3, 13), (512, 512), (700, 1024), (96, 2048), (96, 4096), (40, 8192), (20, 16384), (7, 16391), (5, 32768)])
+def test_gradient_without_that_of_the_gains(rows, cols):
+    """In every form: dx has the bytes of the call that delivers both."""
+    gen = torch.Generator(device="cuda").manual_seed(rows + cols)
+    dy, h, ds = (torch.randn((rows, (cols + 7) // 8 * 8), generator=gen, device="cuda").bfloat16()[:, :cols] for _ in range(3))
+    w, rstd = torch.randn(cols, generator=gen, device="cuda"), torch.rand(rows, generator=gen, device="cuda")
+    both, dw = snip.snip_rms_norm_backward(dy, h, w, rstd, dsum=ds)
+    dx, none = snip.snip_rms_norm_backward(dy, h, w, rstd, dsum=ds, gains=False)
+    assert none is None and dw.shape == (cols,) and torch.equal(dx, both)
+    with pytest.raises(ValueError):
+        snip.snip_rms_norm_backward(dy, h, w, rstd, dweight=dw, gains=False)

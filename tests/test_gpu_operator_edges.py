@@ -156,3 +156,34 @@ def test_gradient_without_that_of_the_gains(rows, cols):
     assert none is None and dw.shape == (cols,) and torch.equal(dx, both)
     with pytest.raises(ValueError):
         snip.snip_rms_norm_backward(dy, h, w, rstd, dweight=dw, gains=False)
+
+
+@pytest.mark.parametrize("dsum", [False, True])
+@pytest.mark.parametrize("cols", [504, 512, 1016, 1024, 2040, 2048, 4088, 4096, 8184, 8192, 16376, 16384])
+def test_gradient_of_tensors_beyond_the_last_level_cache(cols, dsum):
+    """The smallest calls whose tensors exceed 256 MB, which read past the caches, in every number of waves; all rows and all columns.  dx as in
+    test_gpu_rms_norm.py: its parts are off by 2 DELTA at most before the rounding to bf16.  dweight: a term is added at most rows / 256 times in a lane, three times between
+    waves and 16 between workgroups, a factor and a product are rounded before and the sum behind the doubles after that."""
+    delta = 3e-6
+    rows = (256 << 20) // (cols * (8 if dsum else 6)) + 1
+    gen = torch.Generator(device="cuda").manual_seed(cols + dsum)
+    dy, h, ds = (torch.randn((rows, cols), generator=gen, device="cuda").bfloat16() for _ in range(3))
+    h[rows // 3] = 0
+    w, rstd = 1 + 0.2 * torch.randn(cols, generator=gen, device="cuda"), 0.5 + torch.rand(rows, generator=gen, device="cuda")
+    dx, dw = snip.snip_rms_norm_backward(dy, h, w, rstd, dsum=ds if dsum else None)
+    total, magnitude = torch.zeros(cols, dtype=torch.float64, device="cuda"), torch.zeros(cols, dtype=torch.float64, device="cuda")
+    step = (4 << 20) // cols
+    for i in range(0, rows, step):
+        d, x, r = dy[i:i + step].double(), h[i:i + step].double(), rstd[i:i + step].double()[:, None]
+        g = d * w.double()
+        ref = r * (g - x * r * r * (g * x).mean(1, keepdim=True))
+        parts = r * (g.abs() + x.abs() * r * r * (g * x).abs().mean(1, keepdim=True))
+        if dsum:
+            ref, parts = ref + ds[i:i + step].double(), parts + ds[i:i + step].double().abs()
+        got = dx[i:i + step].double()
+        lo, hi = ((ref + e * parts).float().bfloat16().double() for e in (-2 * delta, 2 * delta))
+        assert bool(((got >= lo) & (got <= hi)).all()), i
+        t = d * x * r
+        total += t.sum(0)
+        magnitude += t.abs().sum(0)
+    assert bool(((dw.double() - total).abs() <= (rows / 256 + 24) * 2.0 ** -24 * magnitude).all())

@@ -426,8 +426,8 @@ snip_status snip_adamw_step(const snip_adamw_tensor* tensors, int32_t count, dou
  *          otherwise); scales_g4 is not used.
  *   y    : host array of device pointers; Y_i is row-major with leading dimension ld_y[i], 16-byte aligned rows as for the GEMMs
  *          (ld_y is not read for a single token).
- * Weights become bf16 (exactly; numbers beyond bf16's range become infinite or subnormal), products are exact and sums fp32, added in
- * a fixed order.  A scale byte of 0xFF makes its row NaN.  Meant for up to 64 tokens (m <= 65536 are served, 64 at a time, weights
+ * Weights become bf16: exactly within its normal numbers, below them (2^-126) to its nearest subnormal one, 2^-134 off at most (FP4, and FP8 under scale bytes
+ * from 3 on, exactly there too), beyond them infinite.  Products are exact and sums fp32, added in a fixed order.  A scale byte of 0xFF makes its row NaN.  Meant for up to 64 tokens (m <= 65536 are served, 64 at a time, weights
  * read anew for each); the calls above are for more.  n_i <= 2^27. */
 snip_status snip_gemv(const void* x, int64_t m, int64_t k, int64_t ld, const snip_qtensor* w, void* const* y,
                       const int64_t* ld_y, int32_t count, snip_out_dtype out_dtype, void* stream);

@@ -2,7 +2,7 @@
 // FP8 with a scale per 32 elements.  What a model answers with: every weight is read once for a handful of tokens, so the floor is
 // the weights' bytes (0.53 or 1.03 per weight) over the memory's rate, 7.4 TB/s of reads.
 //
-// Codes become bf16 (exact: at most four significant bits, the scale is a power of two) and go to v_mfma_f32_16x16x32_bf16 with fp32
+// Codes become bf16 (exact down to 2^-126: at most four significant bits, the scale is a power of two) and go to v_mfma_f32_16x16x32_bf16 with fp32
 // accumulators, 16 rows of w by 16 tokens at a time: on the vector unit four tokens would already take longer than the weights' way from
 // memory.  A lane multiplies one block of 32 elements of one row (16 bytes of FP4, 32 of FP8) in each span of 128: the four lanes of a
 // row take the span's four blocks, and matrix instruction j contracts elements 8 j .. 8 j + 7 of all four, for which a lane

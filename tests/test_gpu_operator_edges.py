@@ -187,3 +187,20 @@ def test_gradient_of_tensors_beyond_the_last_level_cache(cols, dsum):
         total += t.sum(0)
         magnitude += t.abs().sum(0)
     assert bool(((dw.double() - total).abs() <= (rows / 256 + 24) * 2.0 ** -24 * magnitude).all())
+
+
+@pytest.mark.parametrize("fmt", [snip.FP4, snip.FP8])
+@pytest.mark.parametrize("end", ["lowest", "highest"])
+@pytest.mark.parametrize("m,n,k", [(5, 40, 224), (1, 50, 3328), (16, 9000, 3328), (16, 40, 11008), (40, 300, 4640), (64, 500, 4128)])
+def test_values_at_the_ends_of_the_scales(m, n, k, end, fmt):
+    """Weights below bf16's normal numbers (scale bytes 0 to 3: code 2^-127 ...) are rounded to its nearest subnormal one, 2^-134 off at most (FP4's, and
+    FP8's from byte 3 on, are exact); those under the highest scales that keep all codes finite are exact.  x is scaled so that products and sums are normal."""
+    from test_gpu_gemv import weight
+    rng = np.random.default_rng(m * n + k)
+    top = 253 if fmt == snip.FP4 else 247                        # from here on the largest code is infinite
+    q, w = weight(rng, n, k, fmt, *((0, 4) if end == "lowest" else (top - 4, top)))
+    x = torch.from_numpy(rng.standard_normal((m, k)).astype(np.float32) * np.float32(2.0 ** (60 if end == "lowest" else -60))).bfloat16()
+    y = snip.snip_gemv(x.cuda(), [q], out_dtype=snip.OUT_FP32)[0].double().cpu().numpy()
+    xd = x.double().numpy()
+    room = k * 2.0 ** -24 * (np.abs(xd) @ np.abs(w.T)) + (np.abs(xd).sum(1)[:, None] * 2.0 ** -134 if end == "lowest" else 0)
+    assert (np.abs(y - xd @ w.T) <= room).all()

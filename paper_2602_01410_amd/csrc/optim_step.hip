@@ -6,7 +6,8 @@
 //
 // Moments of 8 bits, in groups of 128 elements with an fp32 scale each:
 //   m        E4M3 numbers, rounded to nearest; the scale takes the largest to 448.  A scale that is no power of two lets a whole group
-//            decay without a change of its codes.
+//            decay without a change of its codes.  A step moves a number only where (1 - b1) |g - m| exceeds half its distance to the next one, |m| / 16
+//            at most: noise in the gradients does (1 - b1 is 0.1), but m can stop 0.63 |m| from a gradient that no longer changes.
 //   sqrt(v)  unsigned numbers of 4 exponent and 4 mantissa bits with gradual underflow (bits 13 to 6 of a half); the scale takes
 //            the largest to 1.9375.  The root halves the range in the exponent, so that 2^-15.. of the largest root is 2^-30.. of v.  Rounded
 //            stochastically: b2 changes v by a small part of a code's distance per step, which rounding to nearest would undo at every

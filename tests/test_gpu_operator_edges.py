@@ -204,3 +204,23 @@ def test_values_at_the_ends_of_the_scales(m, n, k, end, fmt):
     xd = x.double().numpy()
     room = k * 2.0 ** -24 * (np.abs(xd) @ np.abs(w.T)) + (np.abs(xd).sum(1)[:, None] * 2.0 ** -134 if end == "lowest" else 0)
     assert (np.abs(y - xd @ w.T) <= room).all()
+
+
+@pytest.mark.parametrize("beta1", [0.5, 0.9, 0.99])
+def test_8_bit_moments_stop_where_the_header_says(beta1):
+    """Moments of 1, gradients from then on between -1 and 1 that do not change, one of 1 in each group, which keeps the scale: m comes as close as half
+    the distance of its numbers, |m| / 16 or 2^-10 of the scale, over 1 - beta1.  Moments of 32 bits get there."""
+    n = 128 * 64
+    g = torch.linspace(-1, 1, n, device="cuda")
+    g[::128] = 1.0
+    small, exact = (snip.alloc_adamw_state(torch.zeros(n, device="cuda"), g, bits) for bits in (8, 32))
+    small.m.fill_(0x7E)
+    small.m_scale.fill_(1 / 448)
+    exact.m.fill_(1.0)
+    for step in range(1, 2001):
+        snip.snip_adamw_step([small, exact], 0.0, beta1, 0.95, 1e-8, step, seed=step)
+    scale = small.m_scale.repeat_interleave(128)
+    m = small.m.view(torch.float8_e4m3fn).float() * scale
+    assert bool((scale * 448 - 1 < 1e-5).all())
+    assert bool(((g - m).abs() <= torch.maximum(m.abs() / 16, scale * 2.0 ** -10) / (1 - beta1) * 1.001).all())
+    assert bool(((g - exact.m).abs() < 1e-5).all())

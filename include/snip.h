@@ -354,9 +354,10 @@ double snip_weight_divergence(double alpha, double beta1, double beta2, int64_t 
  *             multiple of 32.  NULL if not wanted.
  *   out_col : the same down columns, stored transposed (cols x rows), the operand of snip_gemm_wgrad; rows a multiple of 32, cols
  *             even.  Needs rstd, and with a residual sum (SNIP_ERR_NULL otherwise).  The two formats may differ.
- * At least one output has to be given (SNIP_ERR_NULL).  A row with an infinity or a NaN gets NaNs; blocks that hold one get scale
- * byte 0xFF and zero codes, as in snip_quantize.  Columns >= cols of sum and y are not touched.  But for sum no output may overlap
- * an input or another output. */
+ * At least one output has to be given (SNIP_ERR_NULL).  A row with a NaN gets NaNs.  Where a row's squares add up to more than fp32
+ * holds (3.4e38: an infinity, or numbers from 1.8e19 on) rstd is 0: finite elements become 0, infinite ones NaN, and no error is
+ * raised; squares below fp32's normal numbers may count as zero.  Blocks that hold an infinity or a NaN get scale byte 0xFF and zero
+ * codes, as in snip_quantize.  Columns >= cols of sum and y are not touched.  But for sum no output may overlap an input or another output. */
 snip_status snip_rms_norm(const void* x, int64_t rows, int64_t cols, int64_t ld, const void* residual, int64_t ld_residual,
                           const void* weight, snip_out_dtype weight_dtype, float eps, snip_scale_rule rule,
                           void* sum, int64_t ld_sum, float* rstd, void* y, int64_t ld_y,
@@ -370,7 +371,7 @@ snip_status snip_rms_norm(const void* x, int64_t rows, int64_t cols, int64_t ld,
  *   dweight : device, fp32 [cols], or NULL.
  *   workspace: device, needed with dweight, >= snip_rms_norm_workspace_bytes(rows, cols) bytes, 16-byte aligned.  The size never falls as
  *             rows or cols grow: a workspace for the largest matrix serves all that are no larger in either extent.
- * Sums are fp32 and added in a fixed order (those of workgroups in double). */
+ * Sums are fp32 and added in a fixed order (the last 32 of each column in double). */
 size_t snip_rms_norm_workspace_bytes(int64_t rows, int64_t cols);
 snip_status snip_rms_norm_backward(const void* dy, int64_t rows, int64_t cols, int64_t ld_dy, const void* h, int64_t ld_h,
                                    const void* weight, snip_out_dtype weight_dtype, const float* rstd,
@@ -412,11 +413,12 @@ typedef struct {
  *                random ones carry; element i of tensor k takes bits 16 (i mod 4) on of the 64 of Threefry-2x32-20 (counter = (i
  *                div 4, k), key = seed; words and counter as for snip_quantize_sr_fp4).  Take a fresh seed for every step.  Numbers of m are
  *                rounded to nearest even.  What is not zero keeps a number of sqrt(v) above zero.
- * What 8 bits do over steps: m keeps its number while (1 - beta1) |g - m| is below half the distance to the next one, up to |m| / 16 (2^-10 m_scale below 2^-6
- * m_scale).  Under gradients that do not change it can stop up to |m| / (16 (1 - beta1)) from them: 0.63 |m| for beta1 = 0.9, and from 0.9375 on a moment
- * whose gradients have become zero may stay for good.  Gradients that vary from step to step move it all the same; where that cannot be relied on, and for beta1 above 0.9,
- * take moments of 32 bits.  sqrt(v) is rounded without bias, v is thus too large in the mean: 0.1 % under gradients that do not change, 0.9 % (beta2 = 0.95) to 2.1 %
- * (0.999) under normally distributed ones.
+ * What 8 bits do over steps: m keeps its number while (1 - beta1) |g - m| is below half the distance to the next one, up to |m| / 16
+ * (2^-10 m_scale below 2^-6 m_scale).  Under gradients that do not change it can stop up to |m| / (16 (1 - beta1)) from them: 0.63 |m|
+ * for beta1 = 0.9, and from 0.9375 on a moment whose gradients have become zero may stay for good.  Gradients that vary from step to
+ * step move it all the same; where that cannot be relied on, and for beta1 above 0.9, take moments of 32 bits.  sqrt(v) is rounded without
+ * bias, v is thus too large in the mean: 0.1 % under gradients that do not change, 0.9 % (beta2 = 0.95) to 2.1 % (0.999) under normally
+ * distributed ones.
  * Scales are largest / 448 (m) and largest / 1.9375 (sqrt(v)), as products with the rounded reciprocals; a group whose scale would be
  * below 2^-126 becomes zero, and one with an infinity or NaN becomes NaN altogether.
  * beta1, beta2 in [0, 1), eps >= 0, lr and weight_decay finite, step >= 1 (SNIP_ERR_FORMAT otherwise). */
@@ -431,8 +433,8 @@ snip_status snip_adamw_step(const snip_adamw_tensor* tensors, int32_t count, dou
  *          otherwise); scales_g4 is not used.
  *   y    : host array of device pointers; Y_i is row-major with leading dimension ld_y[i], 16-byte aligned rows as for the GEMMs
  *          (ld_y is not read for a single token).
- * Weights become bf16: exactly within its normal numbers, below them (2^-126) to its nearest subnormal one, 2^-134 off at most (FP4, and FP8 under scale bytes
- * from 3 on, exactly there too), beyond them infinite.  Products are exact and sums fp32, added in a fixed order.  A scale byte of 0xFF makes its row NaN.  Meant for up to 64 tokens (m <= 65536 are served, 64 at a time, weights
+ * Weights become bf16: exactly within its normal numbers, below them (2^-126) to its nearest subnormal one, 2^-134 off at most (FP4, and
+ * FP8 under scale bytes from 3 on, exactly there too), beyond them infinite.  Products are exact and sums fp32, added in a fixed order.  A scale byte of 0xFF makes its row NaN.  Meant for up to 64 tokens (m <= 65536 are served, 64 at a time, weights
  * read anew for each); the calls above are for more.  n_i <= 2^27. */
 snip_status snip_gemv(const void* x, int64_t m, int64_t k, int64_t ld, const snip_qtensor* w, void* const* y,
                       const int64_t* ld_y, int32_t count, snip_out_dtype out_dtype, void* stream);

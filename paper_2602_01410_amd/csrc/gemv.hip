@@ -9,9 +9,10 @@
 // reads the same elements of x.  So a block has one lane and one scale.
 //
 // Measured (graph replays on four sets of weights), us per call and TB/s: FP4, one token 2 x [28672 x 8192] 50 (5.0), 3 x [4096 x 4096] 8.4 (3.2), [4096
-// x 11008] 9.6 (2.5), [512 x 512] 2.3; 16, 32, 48, 64 tokens 2 x [28672 x 8192] 63, 63, 73, 82 (4.0, 4.0, 3.5, 3.1); FP8, one token 85 (5.7), 48 tokens 109
-// (4.5).  One token is bound by memory's latency (8 waves on a compute unit, each with 4 KB under way, wait most of the time; twice as much under way is
-// no faster), 48 tokens by LDS and matrix cores taking turns on a span (two waves per SIMD), small problems by the launch.
+// x 11008] 8.1 (3.0), [512 x 512] 2.3; 16, 32, 48, 64 tokens 2 x [28672 x 8192] 63, 63, 73, 82 (4.0, 4.0, 3.5, 3.1; on other machines 59 to 80 and 86); FP8, one token
+// 85 (5.7), 48 tokens 109 (4.5).  One token is bound by memory's latency (8 waves on a compute unit, each with 4 KB under way, wait most of the time; twice as much under way is
+// no faster), 48 tokens by LDS and matrix cores taking turns on a span (two waves per SIMD; every wave reads x of all tokens for its two row tiles, 96 KB per
+// span and workgroup), small problems by the launch.
 #include "snip_internal.h"
 #include "quant_common.h"
 #include "x_pieces.h"
@@ -439,15 +440,18 @@ hipError_t launch_gemv(GemvArgs a, hipStream_t s)
         return hipGetLastError();
     }
     // Up to 16 tokens whose x fits LDS as a whole: eight waves on 16 rows where there are few of them, on 32 where there are many (a share's part of x is
-    // read for two tiles, and a workgroup per compute unit goes through several).  us, 16 / 32 rows: 1 token [4096 x 4096] 5.0 / 5.4, [4096 x
-    // 11008] 9.6 / 10.4, 3 x [4096 x 4096] 11.0 / 8.3, 2 x [28672 x 8192] 50.4 / 48.9, 8 tokens 3 x [4096 x 4096] 12.6 / 9.0.
+    // read for two tiles, and a workgroup per compute unit goes through several).  us, 16 / 32 rows: 1 token [4096 x 4096] 4.8 / 5.3, [4096 x
+    // 11008] 8.1 / 9.7, 3 x [4096 x 4096] 11.0 / 8.3, 2 x [28672 x 8192] 50.4 / 48.9, 8 tokens 3 x [4096 x 4096] 12.6 / 9.0.
     auto whole = [&](int shares) { return a.m <= 16 && shares * a.m * (((spans + shares - 1) / shares + 3) / 4 * 4) * 256 <= kLdsX; };
     if (tiles <= 512 && whole(8)) return launch<1, 1, 4, 1, 8, true>(a, s, 512);
     if (tiles > 512 && whole(4)) return launch<1, 1, 4, 2, 4, true>(a, s, 256);
     // Otherwise x comes in chunks.  Of the tiles (256, 128, 64 or 32 rows, 16 to 64 tokens) the one with the most workgroups that still run at once, one
     // per compute unit: us with 256 / 128 / 64 / 32 rows, 16 tokens: 2 x [28672 x 8192] 62 / 68 / 79 / 93, 2 x [11008 x 4096] 19 / 15 / 21 / 24, 3 x
-    // [4096 x 4096] 19 / 14 / 11 / 16, [4096 x 11008] 46 / 31 / 22 / 17; 48 tokens 2 x [28672 x 8192] in tiles of 256 rows by 48 / 32 / 16
-    // tokens 73 / 104 / 137, 3 x [4096 x 4096] of 128 rows 27 / 20 / 25 (of 256 by 16 18).
+    // [4096 x 4096] 18 / 14 / 11 / 16, [4096 x 11008] 46 / 31 / 21 / 16; 48 tokens 2 x [28672 x 8192] in tiles of 256 rows by 48 / 32 / 16
+    // tokens 77 / 109 / 134, 3 x [4096 x 4096] of 128 rows 27 / 19.4 / 25, [4096 x 11008] of 64 rows by 16 21.
+    // It is not the best form everywhere: a tile whose tokens are not all there counts like a full one, and rereading the weights can cost less than idle compute
+    // units or fewer rows.  Taken / best of them: 48 tokens 3 x [4096 x 4096] 19.4 / 18.3 (256 rows by 16), 2 x [11008 x 4096] 28.5 (128 by 48) / 26.0 (256 by 32), 64 tokens
+    // 3 x [4096 x 4096] 27.6 (128 by 48) / 18.5 (256 by 16), 2 x [11008 x 4096] 32.6 (128 by 64) / 26.1 (256 by 32).
     const int cus = gemm_compute_units();
     int64_t most = 0;
     int form = 0, tt = 0;                                    // rows of a workgroup's tile: 256, 128, 64, 32

@@ -8,10 +8,11 @@
 // the norms of 32 rows first: norm_col_kernel runs behind the row kernel and reads h again, with rstd.
 //
 // Measured (graph replays on three sets of tensors; bf16 x and residual, h stored), us and TB/s of the least bytes: [16384 x 4096] FP8 along rows 86 (5.4),
-// down columns 111, both 126 (4.3), bf16 y 95 (5.6); [4096 x 2048] 13.2 (4.5), 18, 21 (3.2); [1 x 4096] 2.6.  The row kernel is bound by memory from some
-// thousand rows on, the column kernel (40 us of the 126 for 203 MB) by h's way back from the last-level cache, as far as it is there, and from memory;
-// few rows by the launch and one chain load - sum - gain - store.  Loads that stream (past the caches) would keep h there but
-// cost small calls their residual: [4096 x 2048] 13.1 -> 16.5.
+// down columns 111, both 126 (4.3), bf16 y 95 (5.6); [4096 x 2048] 13.2 (4.5), 18, 21 (3.2); [1 x 4096] 2.6; FP4 down columns 97 and 18, with
+// FP8 along rows 116 and 20.6.  The row kernel is bound by memory from some thousand rows on, the column kernel (40 us of the 126 for 203 MB, FP4 34) by h's
+// way back from the last-level cache, as far as it is there, and from memory; few rows by the launch and one chain load - sum - gain - store.  Widths
+// off a multiple of 8 are read twice, the second time from cache, at two to three times the floor ([4096 x 9001] 79 us).  Loads that stream (past
+// the caches) would keep h there but cost small calls their residual: [4096 x 2048] 13.1 -> 16.5.
 #include "snip_internal.h"
 #include "quant_common.h"
 
@@ -336,7 +337,8 @@ template <int W, bool RAGGED> void launch_any_row(const NormArgs& a, hipStream_t
 // ---- gradient ------------------------------------------------------------------------------------------------------------------
 // With g = dy w and h normed by rstd:   dx = rstd (g - h rstd^2 mean(g h)) + dsum,   dw = sum over rows of dy h rstd.
 // 6 (8 with dsum) bytes per element.  Measured with dsum, us and TB/s: [8192 x 8192] 98 (5.5), [16384 x 4096] 96 (5.6), [4096 x 2048] 16.1 (4.2);
-// without [1501 x 2056] 10.2; [1 x 4096] 4.7, two launches.  Bound by memory where there are many rows.  A lane owns the same columns of every row
+// without [1501 x 2056] 10.2; [1 x 4096] 4.7, two launches; dx alone, without dsum, [1501 x 2056] 5.7 (with
+// dw 10.1), [4096 x 2048] 10.3 (13.9).  Bound by memory where there are many rows.  A lane owns the same columns of every row
 // that its workgroup takes, so that the sums of dw stay in registers until the workgroup's rows are done; then they go to a row of
 // `partials`, and grad_sum_kernel adds those in a fixed order.
 
@@ -495,7 +497,7 @@ __global__ __launch_bounds__(W * 64) void norm_grad_any_kernel(NormGradArgs a)
     }
 }
 
-// dw[c] = sum of partials[p][c] over p < n: 32 columns by 32 shares of the rows, added in a fixed order.
+// dw[c] = sum of partials[p][c] over p < n: 32 columns by 32 shares of the rows, added in a fixed order, the shares in double.
 __global__ __launch_bounds__(1024) void grad_sum_kernel(const float* __restrict__ partials, int n, int64_t pitch, int cols, float* __restrict__ dw)
 {
     __shared__ float shares[32][33];
@@ -517,7 +519,7 @@ __global__ __launch_bounds__(1024) void grad_sum_kernel(const float* __restrict_
     }
 }
 
-// Waves of a row (0: rows are read twice, by 4 or 16 waves) and workgroups by the number of columns.
+// Waves of a row (0: rows are read twice, by 4 or 16 waves) and workgroups, by the numbers of columns and rows.
 struct GradForm { int waves, groups, blocks; };
 inline GradForm grad_form(int64_t rows, int64_t cols)
 {

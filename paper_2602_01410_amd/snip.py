@@ -568,7 +568,7 @@ class AdamwTensor:
 
 def alloc_adamw_state(param: torch.Tensor, grad: torch.Tensor, bits: int = 32, copy: Optional[torch.Tensor] = None,
                       weight_decay: float = 0.0) -> AdamwTensor:
-    """A tensor before its first step: moments of zero, in 32 or 8 bits."""
+    """A tensor before its first step: moments of zero, in 32 or 8 bits (see the header for what 8 bits do over steps)."""
     if bits not in (8, 32):
         raise ValueError("moments have 8 or 32 bits")
     m, v = (torch.zeros(param.shape, dtype=torch.uint8 if bits == 8 else torch.float32, device=param.device) for _ in range(2))

@@ -439,6 +439,83 @@ snip_status snip_adamw_step(const snip_adamw_tensor* tensors, int32_t count, dou
 snip_status snip_gemv(const void* x, int64_t m, int64_t k, int64_t ld, const snip_qtensor* w, void* const* y,
                       const int64_t* ld_y, int32_t count, snip_out_dtype out_dtype, void* stream);
 
+/* ---- both ends of a language model -------------------------------------------------------- */
+/* What comes in front of the first layer and behind the last one: rows of the embedding, and the loss over the vocabulary with its
+ * gradients, for the head's weights in bf16 and without keeping the logits.
+ * Token numbers (`ids`, `targets`, `indices`) are 32- or 64-bit integers on the device, aligned to their size.  A number outside
+ * [0, vocab) is no token: it has no row, no loss and no gradient (padding; a target of -100). */
+typedef enum { SNIP_INDEX_I32 = 0, SNIP_INDEX_I64 = 1 } snip_index_dtype;
+
+/* y[t] = scale * w[ids[t]], rounded once; zeros where ids[t] is no token.
+ *   w    : device, bf16 or fp32 (w_dtype) [vocab][ld_w], 16-byte aligned; cols < 2^20 and ld_w >= cols multiples of 8; 0 < vocab < 2^31.
+ *   scale: finite.
+ *   y    : device, bf16 [tokens][ld_y], 16-byte aligned, ld_y >= cols, a multiple of 8.  Columns >= cols are not touched. */
+snip_status snip_embed(const void* w, snip_out_dtype w_dtype, int64_t vocab, int64_t cols, int64_t ld_w, const void* ids,
+                       snip_index_dtype id_dtype, int64_t tokens, float scale, void* y, int64_t ld_y, void* stream);
+
+/* Its gradient: dw[v] = scale * (sum of dy[t] over the t with ids[t] == v), or, with `accumulate`, that added to what dw holds (a second
+ * micro-batch; a table that is the head's weight too).
+ *   dy  : device, bf16 [tokens][ld_dy], 16-byte aligned, ld_dy >= cols, a multiple of 8; tokens < 2^30.
+ *   dw  : device, bf16 or fp32 (dw_dtype) [vocab][ld_dw], 16-byte aligned, ld_dw a multiple of 8.  Rows that no token names become
+ *         zero, or with `accumulate` are not touched.
+ *   workspace: device, >= snip_embed_workspace_bytes(tokens, cols, vocab) bytes, 16-byte aligned.  The size never falls as an extent grows.
+ * Sums are fp32, of the tokens in their order (64 at a time where a row has more), and rounded once: results are the same from run to run. */
+size_t snip_embed_workspace_bytes(int64_t tokens, int64_t cols, int64_t vocab);
+snip_status snip_embed_backward(const void* dy, int64_t tokens, int64_t cols, int64_t ld_dy, const void* ids,
+                                snip_index_dtype id_dtype, int64_t vocab, float scale, void* dw, snip_out_dtype dw_dtype,
+                                int64_t ld_dw, int32_t accumulate, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Softmax cross entropy of x [tokens][cols] against the head's weight w [vocab][cols], z = x w^T never being stored:
+ *     lse[t] = log(sum over v of exp(z[t][v])),   loss[t] = lse[t] - z[t][targets[t]],   0 where targets[t] is no token.
+ *   x, w   : device, bf16 [rows][ld], 16-byte aligned; cols and both ld >= cols multiples of 8; cols < 2^20, ld < 2^22; up to 2^21 tokens;
+ *            0 < vocab < 2^31.
+ *   targets: device, [tokens].
+ *   loss, lse: device, fp32 [tokens]; lse is what the backward call needs.  Either may be NULL.
+ *   workspace: device, >= snip_vocab_loss_workspace_bytes(tokens, cols, vocab, 1) bytes, 16-byte aligned.  The size never falls as an extent grows;
+ *            calls that overlap in time must not share it.
+ * Products are exact, sums, exponentials and logarithms fp32, in a fixed order. */
+size_t snip_vocab_loss_workspace_bytes(int64_t tokens, int64_t cols, int64_t vocab, int64_t k);
+snip_status snip_cross_entropy(const void* x, int64_t tokens, int64_t cols, int64_t ld_x, const void* w, int64_t vocab, int64_t ld_w,
+                               const void* targets, snip_index_dtype index_dtype, float* loss, float* lse, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
+/* Its gradients, from the same x, w and targets and the forward call's lse.  The logits are formed anew, a piece of the vocabulary at a time:
+ *     dz[t][v] = dloss[t] * (exp(z[t][v] - lse[t]) - [v == targets[t]]),   dx = dz w,   dw = dz^T x.
+ *   dloss: device, fp32 [tokens], the loss's gradient of every token (1 / count for a mean), or NULL for 1.  A token without a target, or
+ *          whose dloss is zero, takes no part, whatever its x holds: its dx is zero and dw has nothing of it.
+ *   dx   : device, bf16 [tokens][ld_dx], 16-byte aligned, ld_dx a multiple of 8, or NULL.
+ *   dw   : device, bf16 or fp32 (dw_dtype) [vocab][ld_dw], 16-byte aligned, ld_dw a multiple of 8, or NULL (a frozen head); with
+ *          `accumulate` the gradient is added to what dw holds.
+ *   workspace: as above, >= snip_vocab_loss_backward_workspace_bytes(tokens, cols, vocab, 1) bytes.
+ * dz is rounded to bf16 once, before the products with w and x (relative 2^-8 of each, also of an fp32 dw); sums are fp32, in a fixed order. */
+size_t snip_vocab_loss_backward_workspace_bytes(int64_t tokens, int64_t cols, int64_t vocab, int64_t k);
+snip_status snip_cross_entropy_backward(const void* x, int64_t tokens, int64_t cols, int64_t ld_x, const void* w, int64_t vocab,
+                                        int64_t ld_w, const void* targets, snip_index_dtype index_dtype, const float* lse,
+                                        const float* dloss, void* dx, int64_t ld_dx, void* dw, snip_out_dtype dw_dtype, int64_t ld_dw,
+                                        int32_t accumulate, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Distillation from the k largest logits of a teacher for every token.  With s = z / temperature and q[t] = softmax(teacher[t] /
+ * temperature) over the entries whose index is a token:
+ *     lse[t] = log(sum over v of exp(s[t][v])),
+ *     loss[t] = temperature^2 * sum over j of q[t][j] * (log q[t][j] - s[t][indices[t][j]] + lse[t]),
+ * the Kullback-Leibler divergence of the student, over the whole vocabulary, from the teacher's k; 0 where no index is a token.
+ *   indices: device, [tokens][k], contiguous.  An index may come twice: both entries count.
+ *   teacher: device, fp32 or bf16 (teacher_dtype) [tokens][k], contiguous.  An entry of minus infinity has q = 0; a row of nothing else is
+ *            one without a token.
+ *   k      : 1 to 1024, tokens * k < 2^31.   temperature: finite, > 0, as is its inverse.
+ * Other arguments as for snip_cross_entropy; workspace for this k. */
+snip_status snip_distill(const void* x, int64_t tokens, int64_t cols, int64_t ld_x, const void* w, int64_t vocab, int64_t ld_w,
+                         const void* indices, snip_index_dtype index_dtype, const void* teacher, snip_out_dtype teacher_dtype, int64_t k,
+                         float temperature, float* loss, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Its gradients, as for snip_cross_entropy_backward with
+ *     dz[t][v] = dloss[t] * temperature * (exp(s[t][v] - lse[t]) - sum of q[t][j] over the j with indices[t][j] == v). */
+snip_status snip_distill_backward(const void* x, int64_t tokens, int64_t cols, int64_t ld_x, const void* w, int64_t vocab, int64_t ld_w,
+                                  const void* indices, snip_index_dtype index_dtype, const void* teacher, snip_out_dtype teacher_dtype,
+                                  int64_t k, float temperature, const float* lse, const float* dloss, void* dx, int64_t ld_dx, void* dw,
+                                  snip_out_dtype dw_dtype, int64_t ld_dw, int32_t accumulate, void* workspace, size_t workspace_bytes,
+                                  void* stream);
+
 /* ---- quantization-error statistics (Sec. 3.1 Step 1; row-wise form: Sec. 5.3) -------- */
 
 /* One read of a bf16 matrix; for blocks along `axis` produces the squared Frobenius norm of x

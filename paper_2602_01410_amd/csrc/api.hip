@@ -105,6 +105,61 @@ snip_status check_out(const snip_qtensor* o, int64_t stored_rows, int64_t stored
     return SNIP_OK;
 }
 
+// Operands of the calls at both ends of a model: rows of a table or of tokens, whole pieces of 16 bytes.
+constexpr int64_t kMostTokens = 1 << 21, kMostLd = 1 << 22, kMostVocab = (int64_t)1 << 31, kMostWidth = 1 << 20;
+bool valid_type(int t) { return t == SNIP_OUT_BF16 || t == SNIP_OUT_FP32; }
+snip_status check_index(const void* p, int type, int64_t n)
+{
+    if (type != SNIP_INDEX_I32 && type != SNIP_INDEX_I64) return SNIP_ERR_FORMAT;
+    if (!p && n > 0) return SNIP_ERR_NULL;
+    return reinterpret_cast<uintptr_t>(p) & (type == SNIP_INDEX_I64 ? 7u : 3u) ? SNIP_ERR_LAYOUT : SNIP_OK;
+}
+snip_status check_vocab_loss(const VocabLossArgs& a, int index_type)
+{
+    if (a.tokens < 0 || a.tokens > kMostTokens || a.vocab <= 0 || a.vocab >= kMostVocab || a.cols <= 0 || a.cols >= kMostWidth || a.cols % 8 != 0) return SNIP_ERR_SHAPE;
+    if (a.ldx >= kMostLd || a.ldw >= kMostLd) return SNIP_ERR_SHAPE;
+    if (a.k < 1 || a.k > 1024 || a.tokens * a.k >= (int64_t)1 << 31) return SNIP_ERR_SHAPE;
+    if (!std::isfinite(a.tau) || !(a.tau > 0.f) || !std::isfinite(1.f / a.tau)) return SNIP_ERR_FORMAT;
+    snip_status st = check_rows(a.x, a.tokens, a.cols, a.ldx);
+    if (st == SNIP_OK) st = check_rows(a.w, a.vocab, a.cols, a.ldw);
+    if (st == SNIP_OK) st = check_index(a.indices, index_type, a.tokens);
+    if (st == SNIP_OK && ((reinterpret_cast<uintptr_t>(a.loss) | reinterpret_cast<uintptr_t>(a.lse) | reinterpret_cast<uintptr_t>(a.lse_in) | reinterpret_cast<uintptr_t>(a.dloss)) & 3u))
+        st = SNIP_ERR_LAYOUT;
+    return st;
+}
+snip_status check_teacher(const void* teacher, int type, int64_t tokens)
+{
+    if (!valid_type(type)) return SNIP_ERR_FORMAT;
+    if (!teacher && tokens > 0) return SNIP_ERR_NULL;
+    return reinterpret_cast<uintptr_t>(teacher) & (type == SNIP_OUT_FP32 ? 3u : 1u) ? SNIP_ERR_LAYOUT : SNIP_OK;
+}
+snip_status check_workspace(const void* p, size_t bytes, size_t needed)
+{
+    if (!p || bytes < needed) return SNIP_ERR_WORKSPACE;
+    return aligned16(p) ? SNIP_OK : SNIP_ERR_LAYOUT;
+}
+snip_status vocab_loss(const VocabLossArgs& a, int index_type, size_t workspace_bytes_, void* stream)
+{
+    snip_status st = check_vocab_loss(a, index_type);
+    if (st != SNIP_OK) return st;
+    if (a.tokens == 0) return SNIP_OK;
+    if (!a.loss && !a.lse) return SNIP_ERR_NULL;
+    if ((st = check_workspace(a.workspace, workspace_bytes_, vocab_loss_needed(a))) != SNIP_OK) return st;
+    return launch_vocab_loss(a, (hipStream_t)stream) == hipSuccess ? SNIP_OK : SNIP_ERR_HIP;
+}
+snip_status vocab_loss_backward(const VocabLossArgs& a, int index_type, int dw_type, size_t workspace_bytes_, void* stream)
+{
+    snip_status st = check_vocab_loss(a, index_type);
+    if (st != SNIP_OK) return st;
+    if (!valid_type(dw_type)) return SNIP_ERR_FORMAT;
+    if (!a.lse_in && a.tokens > 0) return SNIP_ERR_NULL;
+    if (!a.dx && !a.dw && a.tokens > 0) return SNIP_ERR_NULL;
+    if (a.dx && (st = check_rows(a.dx, a.tokens, a.cols, a.lddx)) != SNIP_OK) return st;
+    if (a.dw && (st = check_rows(a.dw, a.vocab, a.cols, a.lddw)) != SNIP_OK) return st;
+    if (a.tokens > 0 && (st = check_workspace(a.workspace, workspace_bytes_, vocab_loss_backward_needed(a))) != SNIP_OK) return st;
+    return launch_vocab_loss_backward(a, (hipStream_t)stream) == hipSuccess ? SNIP_OK : SNIP_ERR_HIP;
+}
+
 }  // namespace
 
 extern "C" {
@@ -575,6 +630,107 @@ snip_status snip_gemv(const void* x, int64_t m, int64_t k, int64_t ld, const sni
         }
     }
     return SNIP_OK;
+}
+
+snip_status snip_embed(const void* w, snip_out_dtype w_dtype, int64_t vocab, int64_t cols, int64_t ld_w, const void* ids,
+                       snip_index_dtype id_dtype, int64_t tokens, float scale, void* y, int64_t ld_y, void* stream)
+{
+    if (!valid_type(w_dtype) || !std::isfinite(scale)) return SNIP_ERR_FORMAT;
+    if (tokens < 0 || vocab <= 0 || vocab >= kMostVocab || cols <= 0 || cols >= kMostWidth || cols % 8 != 0) return SNIP_ERR_SHAPE;
+    snip_status st = check_rows(w, vocab, cols, ld_w);
+    if (st == SNIP_OK) st = check_rows(y, tokens, cols, ld_y);
+    if (st == SNIP_OK) st = check_index(ids, id_dtype, tokens);
+    if (st != SNIP_OK) return st;
+    EmbedArgs a = {};
+    a.w = w; a.w_fp32 = w_dtype == SNIP_OUT_FP32; a.vocab = vocab; a.ldw = ld_w; a.ids = ids; a.ids64 = id_dtype == SNIP_INDEX_I64;
+    a.tokens = tokens; a.cols = (int)cols; a.scale = scale; a.y = (uint16_t*)y; a.ldy = ld_y;
+    return launch_embed(a, (hipStream_t)stream) == hipSuccess ? SNIP_OK : SNIP_ERR_HIP;
+}
+
+size_t snip_embed_workspace_bytes(int64_t tokens, int64_t cols, int64_t vocab)
+{
+    return tokens < 0 || cols <= 0 || vocab <= 0 ? 0 : embed_workspace_bytes(tokens, cols, vocab);
+}
+
+snip_status snip_embed_backward(const void* dy, int64_t tokens, int64_t cols, int64_t ld_dy, const void* ids,
+                                snip_index_dtype id_dtype, int64_t vocab, float scale, void* dw, snip_out_dtype dw_dtype,
+                                int64_t ld_dw, int32_t accumulate, void* workspace, size_t workspace_bytes_, void* stream)
+{
+    if (!valid_type(dw_dtype) || !std::isfinite(scale)) return SNIP_ERR_FORMAT;
+    if (tokens < 0 || tokens >= (int64_t)1 << 30 || vocab <= 0 || vocab >= kMostVocab || cols <= 0 || cols >= kMostWidth || cols % 8 != 0) return SNIP_ERR_SHAPE;
+    snip_status st = check_rows(dy, tokens, cols, ld_dy);
+    if (st == SNIP_OK) st = check_rows(dw, vocab, cols, ld_dw);
+    if (st == SNIP_OK) st = check_index(ids, id_dtype, tokens);
+    if (st == SNIP_OK) st = check_workspace(workspace, workspace_bytes_, embed_workspace_bytes(tokens, cols, vocab));
+    if (st != SNIP_OK) return st;
+    EmbedGradArgs a = {};
+    a.dy = (const uint16_t*)dy; a.ld = ld_dy; a.ids = ids; a.ids64 = id_dtype == SNIP_INDEX_I64; a.tokens = tokens; a.vocab = vocab; a.cols = (int)cols;
+    a.scale = scale; a.dw = dw; a.dw_fp32 = dw_dtype == SNIP_OUT_FP32; a.lddw = ld_dw; a.add = accumulate != 0; a.workspace = workspace;
+    return launch_embed_backward(a, (hipStream_t)stream) == hipSuccess ? SNIP_OK : SNIP_ERR_HIP;
+}
+
+static bool vocab_extents(int64_t tokens, int64_t cols, int64_t vocab, int64_t k) { return tokens >= 0 && cols > 0 && vocab > 0 && k > 0; }
+size_t snip_vocab_loss_workspace_bytes(int64_t tokens, int64_t cols, int64_t vocab, int64_t k)
+{
+    return vocab_extents(tokens, cols, vocab, k) ? vocab_loss_bytes(tokens, vocab, k) : 0;
+}
+size_t snip_vocab_loss_backward_workspace_bytes(int64_t tokens, int64_t cols, int64_t vocab, int64_t k)
+{
+    return vocab_extents(tokens, cols, vocab, k) ? vocab_loss_backward_bytes(tokens, cols, vocab, k) : 0;
+}
+
+static VocabLossArgs loss_args(const void* x, int64_t tokens, int64_t cols, int64_t ld_x, const void* w, int64_t vocab, int64_t ld_w, const void* indices,
+                               int index_dtype, const void* teacher, int teacher_dtype, int64_t k, float tau, void* workspace)
+{
+    VocabLossArgs a = {};
+    a.x = (const uint16_t*)x; a.tokens = tokens; a.cols = cols; a.ldx = ld_x; a.w = (const uint16_t*)w; a.vocab = vocab; a.ldw = ld_w;
+    a.indices = indices; a.index64 = index_dtype == SNIP_INDEX_I64; a.teacher = teacher; a.teacher_fp32 = teacher_dtype == SNIP_OUT_FP32;
+    a.k = k; a.tau = tau; a.workspace = workspace;
+    return a;
+}
+static void grad_args(VocabLossArgs& a, const float* lse, const float* dloss, void* dx, int64_t ld_dx, void* dw, int dw_dtype, int64_t ld_dw, int32_t accumulate)
+{
+    a.lse_in = lse; a.dloss = dloss; a.dx = (uint16_t*)dx; a.lddx = ld_dx; a.dw = dw; a.dw_fp32 = dw_dtype == SNIP_OUT_FP32; a.lddw = ld_dw; a.add = accumulate != 0;
+}
+
+snip_status snip_cross_entropy(const void* x, int64_t tokens, int64_t cols, int64_t ld_x, const void* w, int64_t vocab, int64_t ld_w,
+                               const void* targets, snip_index_dtype index_dtype, float* loss, float* lse, void* workspace,
+                               size_t workspace_bytes_, void* stream)
+{
+    VocabLossArgs a = loss_args(x, tokens, cols, ld_x, w, vocab, ld_w, targets, index_dtype, nullptr, SNIP_OUT_BF16, 1, 1.f, workspace);
+    a.loss = loss; a.lse = lse;
+    return vocab_loss(a, index_dtype, workspace_bytes_, stream);
+}
+snip_status snip_cross_entropy_backward(const void* x, int64_t tokens, int64_t cols, int64_t ld_x, const void* w, int64_t vocab,
+                                        int64_t ld_w, const void* targets, snip_index_dtype index_dtype, const float* lse,
+                                        const float* dloss, void* dx, int64_t ld_dx, void* dw, snip_out_dtype dw_dtype, int64_t ld_dw,
+                                        int32_t accumulate, void* workspace, size_t workspace_bytes_, void* stream)
+{
+    VocabLossArgs a = loss_args(x, tokens, cols, ld_x, w, vocab, ld_w, targets, index_dtype, nullptr, SNIP_OUT_BF16, 1, 1.f, workspace);
+    grad_args(a, lse, dloss, dx, ld_dx, dw, dw_dtype, ld_dw, accumulate);
+    return vocab_loss_backward(a, index_dtype, dw_dtype, workspace_bytes_, stream);
+}
+snip_status snip_distill(const void* x, int64_t tokens, int64_t cols, int64_t ld_x, const void* w, int64_t vocab, int64_t ld_w,
+                         const void* indices, snip_index_dtype index_dtype, const void* teacher, snip_out_dtype teacher_dtype, int64_t k,
+                         float temperature, float* loss, float* lse, void* workspace, size_t workspace_bytes_, void* stream)
+{
+    const snip_status st = check_teacher(teacher, teacher_dtype, tokens);
+    if (st != SNIP_OK) return st;
+    VocabLossArgs a = loss_args(x, tokens, cols, ld_x, w, vocab, ld_w, indices, index_dtype, teacher, teacher_dtype, k, temperature, workspace);
+    a.loss = loss; a.lse = lse;
+    return vocab_loss(a, index_dtype, workspace_bytes_, stream);
+}
+snip_status snip_distill_backward(const void* x, int64_t tokens, int64_t cols, int64_t ld_x, const void* w, int64_t vocab, int64_t ld_w,
+                                  const void* indices, snip_index_dtype index_dtype, const void* teacher, snip_out_dtype teacher_dtype,
+                                  int64_t k, float temperature, const float* lse, const float* dloss, void* dx, int64_t ld_dx, void* dw,
+                                  snip_out_dtype dw_dtype, int64_t ld_dw, int32_t accumulate, void* workspace, size_t workspace_bytes_,
+                                  void* stream)
+{
+    const snip_status st = check_teacher(teacher, teacher_dtype, tokens);
+    if (st != SNIP_OK) return st;
+    VocabLossArgs a = loss_args(x, tokens, cols, ld_x, w, vocab, ld_w, indices, index_dtype, teacher, teacher_dtype, k, temperature, workspace);
+    grad_args(a, lse, dloss, dx, ld_dx, dw, dw_dtype, ld_dw, accumulate);
+    return vocab_loss_backward(a, index_dtype, dw_dtype, workspace_bytes_, stream);
 }
 
 size_t snip_noalloc_max_cols(void) { return (size_t)kNoallocMaxCols; }

@@ -27,6 +27,12 @@ decltype(&snip_rms_norm) p_rms_norm;
 decltype(&snip_rms_norm_backward) p_rms_norm_backward;
 decltype(&snip_adamw_step) p_adamw_step;
 decltype(&snip_gemv) p_gemv;
+decltype(&snip_embed) p_embed;
+decltype(&snip_embed_backward) p_embed_backward;
+decltype(&snip_cross_entropy) p_cross_entropy;
+decltype(&snip_cross_entropy_backward) p_cross_entropy_backward;
+decltype(&snip_distill) p_distill;
+decltype(&snip_distill_backward) p_distill_backward;
 
 PyObject *s_codes, *s_scales, *s_scales_g4, *s_rows, *s_cols, *s_fmt;      // interned attribute names
 PyObject *s_param, *s_grad, *s_m, *s_v, *s_copy, *s_m_scale, *s_v_scale, *s_weight_decay;
@@ -390,6 +396,131 @@ PyObject* gemv(PyObject*, PyObject* const* a, Py_ssize_t n)
     return call([&] { return p_gemv(x.p, x.rows, x.cols, x.ld, w.data(), y.data(), ld.data(), (int32_t)len, (snip_out_dtype)dt, s); });
 }
 
+// The calls at both ends of a model: tensors of one call are on one device, the current one.
+bool refuse(const char* message) { PyErr_SetString(PyExc_ValueError, message); return false; }
+bool here(const at::Tensor& t)
+{
+    if (!t.is_cuda()) return refuse("expected a CUDA tensor");
+    if (t.get_device() != c10::hip::getCurrentHIPStream().device_index()) return refuse("expected a tensor on the current device");
+    return true;
+}
+struct Table { void* p; int64_t rows, cols, ld; snip_out_dtype dtype; };
+// A matrix of bf16 or, where that may be, fp32.  None, where that may be: null.
+bool table(PyObject* o, bool may_be_fp32, bool optional, Table& m)
+{
+    m = {nullptr, 0, 0, 0, SNIP_OUT_BF16};
+    if (optional && o == Py_None) return true;
+    const at::Tensor* t;
+    if (!tensor(o, t) || !here(*t)) return false;
+    const bool fp32 = t->scalar_type() == at::kFloat;
+    if (t->dim() != 2 || !(t->scalar_type() == at::kBFloat16 || (fp32 && may_be_fp32)))
+        return refuse(may_be_fp32 ? "expected a 2-D tensor of bf16 or fp32" : "expected a 2-D tensor of bf16");
+    if (t->stride(1) != 1 && t->size(1) > 1) return refuse("rows must be contiguous");
+    m = {t->data_ptr(), t->size(0), t->size(1), t->stride(0), fp32 ? SNIP_OUT_FP32 : SNIP_OUT_BF16};
+    return true;
+}
+bool extents(const Table& m, int64_t rows, int64_t cols)
+{
+    return !m.p || (m.rows == rows && m.cols == cols) || refuse("expected matrices of the same extents");
+}
+// Token numbers: `tokens` of them, or (any_k) a matrix with that many rows.
+struct Numbers { void* p; int64_t n, k; snip_index_dtype dtype; };
+bool numbers(PyObject* o, bool any_k, Numbers& i)
+{
+    const at::Tensor* t;
+    if (!tensor(o, t) || !here(*t)) return false;
+    if ((t->scalar_type() != at::kInt && t->scalar_type() != at::kLong) || !t->is_contiguous() || t->dim() != (any_k ? 2 : 1))
+        return refuse(any_k ? "expected a contiguous matrix of 32- or 64-bit integers" : "expected a contiguous vector of 32- or 64-bit integers");
+    i = {t->data_ptr(), t->size(0), any_k ? t->size(1) : 1, t->scalar_type() == at::kLong ? SNIP_INDEX_I64 : SNIP_INDEX_I32};
+    return true;
+}
+bool scalars(PyObject* o, int64_t n, bool optional, void*& p)        // contiguous fp32 [n], or None where that may be
+{
+    p = nullptr;
+    if (optional && o == Py_None) return true;
+    const at::Tensor* t;
+    if (!tensor(o, t) || !here(*t)) return false;
+    if (t->scalar_type() != at::kFloat || !t->is_contiguous() || t->numel() != n) return refuse("expected a contiguous tensor of fp32, one element for each token");
+    p = t->data_ptr();
+    return true;
+}
+// Scratch memory: contiguous bytes.
+bool scratch(PyObject* o, void*& p, size_t& n)
+{
+    const at::Tensor* t;
+    p = nullptr; n = 0;
+    if (o == Py_None) return true;
+    if (!tensor(o, t) || !here(*t)) return false;
+    if (!t->is_contiguous()) return refuse("a workspace is contiguous");
+    p = t->data_ptr(); n = t->nbytes();
+    return true;
+}
+// (w, ids, scale, y, stream)
+PyObject* embed(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Table w, y; Numbers ids; void* s;
+    if (!count(n, 5) || !table(a[0], true, false, w) || !numbers(a[1], false, ids)) return nullptr;
+    const double scale = PyFloat_AsDouble(a[2]);
+    if (PyErr_Occurred() || !table(a[3], false, false, y) || !stream(a[4], s)) return nullptr;
+    if (y.rows != ids.n || y.cols != w.cols) { refuse("expected a row of output for each token, as wide as the table"); return nullptr; }
+    return call([&] { return p_embed(w.p, w.dtype, w.rows, w.cols, w.ld, ids.p, ids.dtype, ids.n, (float)scale, y.p, y.ld, s); });
+}
+// (dy, ids, scale, dw, accumulate, workspace, stream)
+PyObject* embed_backward(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Table dy, dw; Numbers ids; int64_t add; void *ws, *s; size_t wn;
+    if (!count(n, 7) || !table(a[0], false, false, dy) || !numbers(a[1], false, ids)) return nullptr;
+    const double scale = PyFloat_AsDouble(a[2]);
+    if (PyErr_Occurred() || !table(a[3], true, false, dw) || !integer(a[4], add) || !scratch(a[5], ws, wn) || !stream(a[6], s)) return nullptr;
+    if (dy.rows != ids.n || dy.cols != dw.cols) { refuse("expected a row of dy for each token, as wide as the table"); return nullptr; }
+    return call([&] { return p_embed_backward(dy.p, dy.rows, dy.cols, dy.ld, ids.p, ids.dtype, dw.rows, (float)scale, dw.p, dw.dtype, dw.ld, (int32_t)add, ws, wn, s); });
+}
+// What both directions of a loss have: (x, w, indices, teacher or None, temperature).  Without a teacher the indices are targets.
+struct LossInput { Table x, w; Numbers at; void* teacher; snip_out_dtype teacher_dtype; double temperature; };
+bool loss_input(PyObject* const* a, LossInput& i)
+{
+    const bool distill = a[3] != Py_None;
+    i.teacher = nullptr; i.teacher_dtype = SNIP_OUT_BF16;
+    if (!table(a[0], false, false, i.x) || !table(a[1], false, false, i.w) || !numbers(a[2], distill, i.at)) return false;
+    if (i.x.cols != i.w.cols) return refuse("x and w differ in their width");
+    if (i.at.n != i.x.rows) return refuse("expected targets or indices for each token");
+    if (distill) {
+        Table t;
+        if (!table(a[3], true, false, t) || !extents(t, i.at.n, i.at.k)) return false;
+        if (t.ld != t.cols && t.rows > 1) return refuse("the teacher's logits must be contiguous");
+        i.teacher = t.p; i.teacher_dtype = t.dtype;
+    }
+    i.temperature = PyFloat_AsDouble(a[4]);
+    return !PyErr_Occurred();
+}
+// (x, w, indices, teacher, temperature, loss, lse, workspace, stream)
+PyObject* vocab_loss(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    LossInput i; void *loss, *lse, *ws, *s; size_t wn;
+    if (!count(n, 9) || !loss_input(a, i) || !scalars(a[5], i.x.rows, true, loss) || !scalars(a[6], i.x.rows, true, lse) || !scratch(a[7], ws, wn) || !stream(a[8], s)) return nullptr;
+    return call([&] {
+        return a[3] == Py_None
+                   ? p_cross_entropy(i.x.p, i.x.rows, i.x.cols, i.x.ld, i.w.p, i.w.rows, i.w.ld, i.at.p, i.at.dtype, (float*)loss, (float*)lse, ws, wn, s)
+                   : p_distill(i.x.p, i.x.rows, i.x.cols, i.x.ld, i.w.p, i.w.rows, i.w.ld, i.at.p, i.at.dtype, i.teacher, i.teacher_dtype, i.at.k, (float)i.temperature,
+                               (float*)loss, (float*)lse, ws, wn, s);
+    });
+}
+// (x, w, indices, teacher, temperature, lse, dloss, dx, dw, accumulate, workspace, stream)
+PyObject* vocab_loss_backward(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    LossInput i; Table dx, dw; int64_t add; void *lse, *dloss, *ws, *s; size_t wn;
+    if (!count(n, 12) || !loss_input(a, i) || !scalars(a[5], i.x.rows, false, lse) || !scalars(a[6], i.x.rows, true, dloss) || !table(a[7], false, true, dx) ||
+        !extents(dx, i.x.rows, i.x.cols) || !table(a[8], true, true, dw) || !extents(dw, i.w.rows, i.w.cols) || !integer(a[9], add) || !scratch(a[10], ws, wn) || !stream(a[11], s))
+        return nullptr;
+    return call([&] {
+        return a[3] == Py_None
+                   ? p_cross_entropy_backward(i.x.p, i.x.rows, i.x.cols, i.x.ld, i.w.p, i.w.rows, i.w.ld, i.at.p, i.at.dtype, (const float*)lse, (const float*)dloss, dx.p, dx.ld,
+                                              dw.p, dw.dtype, dw.ld, (int32_t)add, ws, wn, s)
+                   : p_distill_backward(i.x.p, i.x.rows, i.x.cols, i.x.ld, i.w.p, i.w.rows, i.w.ld, i.at.p, i.at.dtype, i.teacher, i.teacher_dtype, i.at.k, (float)i.temperature,
+                                        (const float*)lse, (const float*)dloss, dx.p, dx.ld, dw.p, dw.dtype, dw.ld, (int32_t)add, ws, wn, s);
+    });
+}
+
 template <class F> bool find(void* lib, const char* name, F& f)
 {
     f = (F)dlsym(lib, name);
@@ -411,7 +542,9 @@ PyObject* bind(PyObject*, PyObject* arg)
         !find(lib, "snip_quant_error_stats", p_stats) || !find(lib, "snip_quant_error_stats_both", p_stats_both) ||
         !find(lib, "snip_adamw_sensitivity", p_adamw) || !find(lib, "snip_rms_norm", p_rms_norm) ||
         !find(lib, "snip_rms_norm_backward", p_rms_norm_backward) || !find(lib, "snip_adamw_step", p_adamw_step) ||
-        !find(lib, "snip_gemv", p_gemv))
+        !find(lib, "snip_gemv", p_gemv) || !find(lib, "snip_embed", p_embed) || !find(lib, "snip_embed_backward", p_embed_backward) ||
+        !find(lib, "snip_cross_entropy", p_cross_entropy) || !find(lib, "snip_cross_entropy_backward", p_cross_entropy_backward) ||
+        !find(lib, "snip_distill", p_distill) || !find(lib, "snip_distill_backward", p_distill_backward))
         return nullptr;
     Py_RETURN_NONE;
 }
@@ -430,7 +563,8 @@ PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t n)
 #define SNIP_FAST(name) {#name, (PyCFunction)(void (*)(void))guarded<name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"bind", bind, METH_O, nullptr}, SNIP_FAST(quantize), SNIP_FAST(quantize_both), SNIP_FAST(quantize_sr_fp4),
                          SNIP_FAST(gemm), SNIP_FAST(gemm_norm), SNIP_FAST(quantize_paper), SNIP_FAST(gemm_paper), SNIP_FAST(stats),
-                         SNIP_FAST(stats_both), SNIP_FAST(adamw), SNIP_FAST(rms_norm), SNIP_FAST(rms_norm_backward), SNIP_FAST(adamw_step), SNIP_FAST(gemv), {nullptr, nullptr, 0, nullptr}};
+                         SNIP_FAST(stats_both), SNIP_FAST(adamw), SNIP_FAST(rms_norm), SNIP_FAST(rms_norm_backward), SNIP_FAST(adamw_step), SNIP_FAST(gemv),
+                         SNIP_FAST(embed), SNIP_FAST(embed_backward), SNIP_FAST(vocab_loss), SNIP_FAST(vocab_loss_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_snip_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,269 @@
+// Rows of an embedding, and their gradient summed over the tokens in sorted order.
+//     y[t] = scale w[ids[t]]            dw[v] = scale sum over t with ids[t] = v of dy[t]   (+ what dw holds)
+// Both move bytes and do nothing else: T rows read and written; T rows of dy read and the table's gradient written.
+//
+// The gradient takes three launches without atomics on memory, so that its sums have one order:
+//   sort      a workgroup for each range of token numbers looks through all of ids twice: it counts its numbers (and those below its
+//             range, which gives its place in the order), then puts the places of its tokens in order.  A wave takes a stretch of ids, so
+//             tokens of one number stay in their order.  T * ranges reads, from L2: 16384 ids of 8 bytes and 250 ranges are 65 MB.
+//   partials  rows with more than kLong tokens (the most frequent words, a tenth of a text each) are summed kLong tokens at a time
+//             by as many workgroups; for most blocks there is nothing to do.
+//   rows      a wave for each 512 columns of a row of the table: zeros, or the sum of its tokens, or of its partial sums.
+#include "snip_internal.h"
+#include "quant_common.h"
+
+namespace snip {
+namespace {
+
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
+constexpr int kMostRange = 512;          // token numbers of a workgroup of the sort
+constexpr int kLong = 64;                // tokens of a row from which on it is summed in parts, and the tokens of a part
+constexpr int kSegment = 512;            // columns of a wave: 8 per lane
+
+template <bool I64> __device__ __forceinline__ int token(const void* ids, int64_t t, int vocab)      // -1: none
+{
+    if (I64) {
+        const int64_t v = ((const int64_t*)ids)[t];
+        return v >= 0 && v < vocab ? (int)v : -1;
+    }
+    const int v = ((const int*)ids)[t];
+    return v >= 0 && v < vocab ? v : -1;
+}
+
+__device__ __forceinline__ void load8(const float* p, float (&f)[8])
+{
+    const float4 a = ((const float4*)p)[0], b = ((const float4*)p)[1];
+    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+}
+__device__ __forceinline__ void load8(const uint16_t* p, float (&f)[8])
+{
+    const uint4 v = *(const uint4*)p;
+    unpack2(v.x, f[0], f[1]); unpack2(v.y, f[2], f[3]); unpack2(v.z, f[4], f[5]); unpack2(v.w, f[6], f[7]);
+}
+__device__ __forceinline__ void store8(float* p, const float (&f)[8])
+{
+    ((float4*)p)[0] = make_float4(f[0], f[1], f[2], f[3]);
+    ((float4*)p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+}
+__device__ __forceinline__ unsigned pack2(float a, float b) { return __builtin_bit_cast(unsigned, bf16x2{(__bf16)a, (__bf16)b}); }
+__device__ __forceinline__ void store8(uint16_t* p, const float (&f)[8])
+{
+    *(uint4*)p = make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
+}
+
+// `lanes` (64 or 256) threads share a row.
+template <class T, bool I64>
+__global__ __launch_bounds__(256) void embed_kernel(const T* __restrict__ w, int vocab, int cols, int64_t ldw, const void* __restrict__ ids,
+                                                    int64_t tokens, float scale, uint16_t* __restrict__ y, int64_t ldy, int lanes)
+{
+    const int per = 256 / lanes, me = threadIdx.x % lanes;
+    for (int64_t t = (int64_t)blockIdx.x * per + threadIdx.x / lanes; t < tokens; t += (int64_t)gridDim.x * per) {
+        const int v = token<I64>(ids, t, vocab);
+        const T* row = w + (int64_t)(v < 0 ? 0 : v) * ldw;
+#pragma unroll 4
+        for (int c = me * 8; c < cols; c += lanes * 8) {
+            float f[8];
+            load8(row + c, f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = v < 0 ? 0.f : f[i] * scale;
+            store8(y + t * ldy + c, f);
+        }
+    }
+}
+
+// start[v]: place in `order` of the first token of number v, start[vocab] the number of tokens that have one.
+template <bool I64>
+__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const void* __restrict__ ids, int tokens, int vocab, int range,
+                                                                  int* __restrict__ start, int* __restrict__ order)
+{
+    __shared__ int counts[kSortWaves][kMostRange];
+    __shared__ int sums[kSortWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int base = blockIdx.x * range, here = vocab - base < range ? vocab - base : range;
+    const int64_t stretch = ((int64_t)tokens + kSortThreads - 1) / kSortThreads * 64;
+    const int64_t from = wave * stretch, to = from + stretch < tokens ? from + stretch : tokens;
+    for (int i = threadIdx.x; i < kSortWaves * range; i += kSortThreads) counts[i / range][i % range] = 0;
+    __syncthreads();
+    int below = 0;
+#pragma unroll 4
+    for (int64_t t = from + lane; t < to; t += 64) {
+        const int v = token<I64>(ids, t, vocab);
+        below += v >= 0 && v < base;
+        if (v >= base && v - base < here) atomicAdd(&counts[wave][v - base], 1);
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) below += __shfl_xor(below, d);
+    if (lane == 0) sums[wave] = below;
+    __syncthreads();
+    int first = 0;
+#pragma unroll
+    for (int i = 0; i < kSortWaves; ++i) first += sums[i];
+    __syncthreads();
+    // places: all numbers below, then within a number the waves in turn (range <= kSortThreads)
+    const int me = threadIdx.x;
+    int total = 0;
+    if (me < range)
+        for (int i = 0; i < kSortWaves; ++i) total += counts[i][me];
+    int inc = total;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_up(inc, d);
+        if (lane >= d) inc += o;
+    }
+    if (lane == 63) sums[wave] = inc;
+    __syncthreads();
+    int at = first + inc - total;
+    for (int i = 0; i < wave; ++i) at += sums[i];
+    if (me < here) {
+        start[base + me] = at;
+        if (base + me == vocab - 1) start[vocab] = at + total;
+        for (int i = 0; i < kSortWaves; ++i) {
+            const int n = counts[i][me];
+            counts[i][me] = at;
+            at += n;
+        }
+    }
+    __syncthreads();
+    volatile int* mine = counts[wave];
+    for (int64_t t0 = from; t0 < to; t0 += 64) {
+        const int64_t t = t0 + lane;
+        const int v = t < to ? token<I64>(ids, t, vocab) : -1;
+        bool todo = v >= base && v - base < here;
+        unsigned long long left = __builtin_amdgcn_ballot_w64(todo);
+        while (left) {
+            const int lead = __builtin_ctzll(left);
+            const int number = __builtin_amdgcn_readlane(v, lead) - base;
+            const bool same = todo && v - base == number;
+            const unsigned long long with = __builtin_amdgcn_ballot_w64(same);
+            const int place = mine[number];
+            if (same) order[place + __builtin_popcountll(with & ((1ull << lane) - 1))] = (int)t;
+            __builtin_amdgcn_wave_barrier();
+            if (lane == lead) mine[number] = place + __builtin_popcountll(with);
+            __builtin_amdgcn_wave_barrier();
+            todo = todo && !same;
+            left &= ~with;
+        }
+    }
+}
+
+// Sum of dy's rows order[from ... to) at column c, in their order.
+__device__ __forceinline__ void sum_rows(const uint16_t* __restrict__ dy, int64_t ld, const int* __restrict__ order, int from, int to, int c, float (&sum)[8])
+{
+    constexpr int B = 8;
+    for (int p = from; p < to; p += B) {
+        float f[B][8];
+#pragma unroll
+        for (int b = 0; b < B; ++b) load8(dy + (int64_t)order[p + b < to ? p + b : to - 1] * ld + c, f[b]);
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+            if (p + b < to) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[i] += f[b][i];
+            }
+    }
+}
+
+// Block j: the places [j kLong, (j + 1) kLong) of the order.  Of the rows with more than kLong tokens two at most have tokens there: that of the first
+// place (partial sum 0) and, if it is another one, that of the last (1).
+template <bool I64>
+__global__ __launch_bounds__(64) void embed_partials_kernel(const uint16_t* __restrict__ dy, int64_t ld, int cols, int vocab, const void* __restrict__ ids,
+                                                            const int* __restrict__ start, const int* __restrict__ order, float* __restrict__ partials)
+{
+    const int all = start[vocab], p0 = blockIdx.x * kLong;
+    if (p0 >= all) return;
+    const int p1 = all - p0 < kLong ? all : p0 + kLong;
+    const int c = blockIdx.y * kSegment + threadIdx.x * 8;
+    const int v0 = token<I64>(ids, order[p0], vocab), v1 = token<I64>(ids, order[p1 - 1], vocab);
+#pragma unroll
+    for (int slot = 0; slot < 2; ++slot) {
+        const int v = slot ? v1 : v0;
+        if (slot && v1 == v0) break;
+        const int s = start[v], e = start[v + 1];
+        if (e - s <= kLong || c >= cols) continue;
+        float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        sum_rows(dy, ld, order, s > p0 ? s : p0, e < p1 ? e : p1, c, sum);
+        store8(partials + ((int64_t)blockIdx.x * 2 + slot) * cols + c, sum);
+    }
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void embed_rows_kernel(const uint16_t* __restrict__ dy, int64_t ld, int cols, int vocab, float scale,
+                                                         const int* __restrict__ start, const int* __restrict__ order, const float* __restrict__ partials,
+                                                         T* __restrict__ dw, int64_t lddw, bool add, int segments)
+{
+    const int64_t units = (int64_t)vocab * segments;
+    for (int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); u < units; u += (int64_t)gridDim.x * 4) {
+        const int v = (int)(u / segments), c = (int)(u % segments) * kSegment + (threadIdx.x & 63) * 8;
+        const int s = __builtin_amdgcn_readfirstlane(start[v]), e = __builtin_amdgcn_readfirstlane(start[v + 1]);
+        if ((add && s == e) || c >= cols) continue;
+        float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (e - s <= kLong) {
+            sum_rows(dy, ld, order, s, e, c, sum);
+        } else {
+            const int last = (e - 1) / kLong;
+            for (int j = s / kLong; j <= last; ++j) {
+                float f[8];
+                load8(partials + ((int64_t)j * 2 + (j * kLong < s)) * cols + c, f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[i] += f[i];
+            }
+        }
+        T* p = dw + (int64_t)v * lddw + c;
+        float old[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (add) load8(p, old);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] = fmaf(sum[i], scale, old[i]);
+        store8(p, sum);
+    }
+}
+
+int sort_range(int64_t vocab)
+{
+    int r = 16;
+    while (r < kMostRange && r * 256 < vocab) r *= 2;
+    return r;
+}
+size_t to256(size_t n) { return (n + 255) / 256 * 256; }
+
+}  // namespace
+
+// [vocab + 1] starts, [tokens] order, [blocks][2][cols] partial sums
+size_t embed_workspace_bytes(int64_t tokens, int64_t cols, int64_t vocab)
+{
+    return to256((size_t)(vocab + 1) * 4) + to256((size_t)tokens * 4) + (size_t)((tokens + kLong - 1) / kLong) * 2 * (size_t)cols * 4;
+}
+
+hipError_t launch_embed(const EmbedArgs& a, hipStream_t s)
+{
+    if (a.tokens == 0) return hipSuccess;
+    const int lanes = a.cols > 1024 ? 256 : 64;
+    const int64_t blocks = (a.tokens + 256 / lanes - 1) / (256 / lanes);
+    const dim3 grid((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks));
+    auto go = [&](auto w, auto* kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, w, (int)a.vocab, a.cols, a.ldw, a.ids, a.tokens, a.scale, a.y, a.ldy, lanes); };
+    if (a.w_fp32) go((const float*)a.w, a.ids64 ? embed_kernel<float, true> : embed_kernel<float, false>);
+    else          go((const uint16_t*)a.w, a.ids64 ? embed_kernel<uint16_t, true> : embed_kernel<uint16_t, false>);
+    return hipGetLastError();
+}
+
+hipError_t launch_embed_backward(const EmbedGradArgs& a, hipStream_t s)
+{
+    uint8_t* ws = (uint8_t*)a.workspace;
+    int* start = (int*)ws;
+    int* order = (int*)(ws + to256((size_t)(a.vocab + 1) * 4));
+    float* partials = (float*)(ws + to256((size_t)(a.vocab + 1) * 4) + to256((size_t)a.tokens * 4));
+    const int range = sort_range(a.vocab), segments = (a.cols + kSegment - 1) / kSegment;
+    hipLaunchKernelGGL(a.ids64 ? embed_sort_kernel<true> : embed_sort_kernel<false>, dim3((unsigned)((a.vocab + range - 1) / range)), dim3(kSortThreads), 0, s,
+                       a.ids, (int)a.tokens, (int)a.vocab, range, start, order);
+    if (a.tokens > kLong)
+        hipLaunchKernelGGL(a.ids64 ? embed_partials_kernel<true> : embed_partials_kernel<false>, dim3((unsigned)((a.tokens + kLong - 1) / kLong), (unsigned)segments),
+                           dim3(64), 0, s, a.dy, a.ld, a.cols, (int)a.vocab, a.ids, start, order, partials);
+    const int64_t blocks = (a.vocab * segments + 3) / 4;
+    const dim3 grid((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks));
+    if (a.dw_fp32)
+        hipLaunchKernelGGL(embed_rows_kernel<float>, grid, dim3(256), 0, s, a.dy, a.ld, a.cols, (int)a.vocab, a.scale, start, order, partials, (float*)a.dw, a.lddw, a.add, segments);
+    else
+        hipLaunchKernelGGL(embed_rows_kernel<uint16_t>, grid, dim3(256), 0, s, a.dy, a.ld, a.cols, (int)a.vocab, a.scale, start, order, partials, (uint16_t*)a.dw, a.lddw, a.add, segments);
+    return hipGetLastError();
+}
+
+}  // namespace snip

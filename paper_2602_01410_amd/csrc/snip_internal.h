@@ -193,6 +193,49 @@ size_t norm_workspace_needed(int64_t rows, int64_t cols);      // by a call of t
 size_t norm_workspace_bytes(int64_t rows, int64_t cols);       // by any call of at most these extents
 hipError_t launch_rms_norm_backward(NormGradArgs a, hipStream_t s);
 
+// Rows of an embedding and their gradient (embed.hip).
+struct EmbedArgs {
+    const void* w; int w_fp32; int64_t vocab, ldw;
+    const void* ids; int ids64;
+    int64_t tokens; int cols;
+    float scale;
+    uint16_t* y; int64_t ldy;
+};
+hipError_t launch_embed(const EmbedArgs& a, hipStream_t s);
+struct EmbedGradArgs {
+    const uint16_t* dy; int64_t ld;
+    const void* ids; int ids64;
+    int64_t tokens, vocab; int cols;
+    float scale;
+    void* dw; int dw_fp32; int64_t lddw;
+    bool add;
+    void* workspace;
+};
+size_t embed_workspace_bytes(int64_t tokens, int64_t cols, int64_t vocab);
+hipError_t launch_embed_backward(const EmbedGradArgs& a, hipStream_t s);
+
+// The loss over the vocabulary and its gradients (vocab_loss.hip); cross entropy: teacher null, k 1, tau 1.
+struct VocabLossArgs {
+    const uint16_t* x; int64_t tokens, cols, ldx;
+    const uint16_t* w; int64_t vocab, ldw;
+    const void* indices; int index64;
+    const void* teacher; int teacher_fp32;
+    int64_t k;
+    float tau;
+    float *loss, *lse;                       // forward, either may be null
+    const float *lse_in, *dloss;             // backward; dloss may be null
+    uint16_t* dx; int64_t lddx;              // either may be null
+    void* dw; int dw_fp32; int64_t lddw;
+    bool add;
+    void* workspace;
+};
+size_t vocab_loss_needed(const VocabLossArgs& a);                                                        // by this call
+size_t vocab_loss_bytes(int64_t tokens, int64_t vocab, int64_t k);                                       // by any of at most these extents
+size_t vocab_loss_backward_needed(const VocabLossArgs& a);
+size_t vocab_loss_backward_bytes(int64_t tokens, int64_t cols, int64_t vocab, int64_t k);
+hipError_t launch_vocab_loss(const VocabLossArgs& a, hipStream_t s);
+hipError_t launch_vocab_loss_backward(const VocabLossArgs& a, hipStream_t s);
+
 // The paper's own recipe (real-valued scale per 1x128 tile or 128x128 block): quantize (stats == nullptr)
 // or statistics of both formats (stats != nullptr; codes / scales unused).
 struct PaperArgs {

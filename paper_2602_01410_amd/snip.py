@@ -31,7 +31,9 @@ EXPORTS = ("snip_qtensor_code_bytes", "snip_qtensor_scale_bytes", "snip_qtensor_
            "snip_paper_scale_bytes", "snip_paper_workspace_bytes", "snip_quantize_paper",
            "snip_quant_error_stats_paper", "snip_gemm_paper", "snip_quant_error_stats_both",
            "snip_noalloc_max_cols", "snip_quant_error_stats_noalloc",
-           "snip_rms_norm", "snip_rms_norm_backward", "snip_rms_norm_workspace_bytes", "snip_adamw_step", "snip_gemv")
+           "snip_rms_norm", "snip_rms_norm_backward", "snip_rms_norm_workspace_bytes", "snip_adamw_step", "snip_gemv",
+           "snip_embed", "snip_embed_workspace_bytes", "snip_embed_backward", "snip_vocab_loss_workspace_bytes", "snip_cross_entropy",
+           "snip_vocab_loss_backward_workspace_bytes", "snip_cross_entropy_backward", "snip_distill", "snip_distill_backward")
 
 
 class _PTensorC(ctypes.Structure):
@@ -144,6 +146,21 @@ def _lib():
         lib.snip_adamw_step.argtypes = [vp, ctypes.c_int32, cd, cd, cd, cd, i64, vp, ctypes.c_uint64, vp]
         lib.snip_gemv.restype = ci
         lib.snip_gemv.argtypes = [vp, i64, i64, i64, qp, ctypes.POINTER(vp), ctypes.POINTER(i64), ctypes.c_int32, ci, vp]
+        i32 = ctypes.c_int32
+        lib.snip_embed.restype = ci
+        lib.snip_embed.argtypes = [vp, ci, i64, i64, i64, vp, ci, i64, cf, vp, i64, vp]
+        lib.snip_embed_workspace_bytes.restype = sz
+        lib.snip_embed_workspace_bytes.argtypes = [i64, i64, i64]
+        lib.snip_embed_backward.restype = ci
+        lib.snip_embed_backward.argtypes = [vp, i64, i64, i64, vp, ci, i64, cf, vp, ci, i64, i32, vp, sz, vp]
+        for fn in (lib.snip_vocab_loss_workspace_bytes, lib.snip_vocab_loss_backward_workspace_bytes):
+            fn.restype = sz
+            fn.argtypes = [i64, i64, i64, i64]
+        operands, teacher, grads = [vp, i64, i64, i64, vp, i64, i64, vp, ci], [vp, ci, i64, cf], [vp, vp, vp, i64, vp, ci, i64, i32, vp, sz, vp]
+        for fn, args in ((lib.snip_cross_entropy, operands + [vp, vp, vp, sz, vp]), (lib.snip_cross_entropy_backward, operands + grads),
+                         (lib.snip_distill, operands + teacher + [vp, vp, vp, sz, vp]), (lib.snip_distill_backward, operands + teacher + grads)):
+            fn.restype = ci
+            fn.argtypes = args
         lib.snip_status_string.restype = ctypes.c_char_p
         lib.snip_status_string.argtypes = [ci]
         _handle = lib
@@ -598,3 +615,115 @@ def snip_gemv(x: torch.Tensor, weights: Sequence[QTensor], out: Optional[Sequenc
     if status:
         raise SnipError(status, "snip_gemv")
     return out
+
+
+def snip_embed(w: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Rows scale * w[ids] (w bf16 or fp32 [vocab, cols], ids int32 or int64 [tokens]) in bf16; zeros for numbers outside the table."""
+    if out is None:
+        with _alloc_on(stream):
+            out = torch.empty((ids.shape[0], w.shape[1]), dtype=torch.bfloat16, device=w.device)
+    status = _nat().embed(w, ids, scale, out, _handle_of(stream))
+    if status:
+        raise SnipError(status, "snip_embed")
+    return out
+
+
+def embed_workspace_bytes(tokens: int, cols: int, vocab: int) -> int:
+    return int(_lib().snip_embed_workspace_bytes(tokens, cols, vocab))
+
+
+def snip_embed_backward(dy: torch.Tensor, ids: torch.Tensor, vocab: int, scale: float = 1.0, dw: Optional[torch.Tensor] = None, out_dtype: int = OUT_FP32,
+                        accumulate: bool = False, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Gradient [vocab, cols] of snip_embed's table from dy (bf16 [tokens, cols]), summed over the tokens in their order; with accumulate added to dw
+    (bf16 or fp32), which has to be passed then."""
+    if dw is None and accumulate:
+        raise ValueError("accumulate needs the gradient to be added to")
+    if dw is not None and dw.shape[0] != vocab:
+        raise ValueError("dw has another number of rows than the vocabulary")
+    if dw is None or workspace is None:
+        with _alloc_on(stream):
+            if dw is None:
+                dw = torch.empty((vocab, dy.shape[1]), dtype=torch.float32 if out_dtype == OUT_FP32 else torch.bfloat16, device=dy.device)
+            if workspace is None:
+                workspace = torch.empty(embed_workspace_bytes(dy.shape[0], dy.shape[1], vocab), dtype=torch.uint8, device=dy.device)
+    status = _nat().embed_backward(dy, ids, scale, dw, int(accumulate), workspace, _handle_of(stream))
+    if status:
+        raise SnipError(status, "snip_embed_backward")
+    return dw
+
+
+def vocab_loss_workspace_bytes(tokens: int, cols: int, vocab: int, k: int = 1) -> int:
+    return int(_lib().snip_vocab_loss_workspace_bytes(tokens, cols, vocab, k))
+
+
+def vocab_loss_backward_workspace_bytes(tokens: int, cols: int, vocab: int, k: int = 1) -> int:
+    return int(_lib().snip_vocab_loss_backward_workspace_bytes(tokens, cols, vocab, k))
+
+
+def _vocab_loss(where, x, w, indices, teacher, temperature, loss, lse, workspace, stream):
+    if loss is None or lse is None or workspace is None:
+        with _alloc_on(stream):
+            if loss is None:
+                loss = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+            if lse is None:
+                lse = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+            if workspace is None:
+                k = 1 if teacher is None else indices.shape[1]
+                workspace = torch.empty(vocab_loss_workspace_bytes(x.shape[0], x.shape[1], w.shape[0], k), dtype=torch.uint8, device=x.device)
+    status = _nat().vocab_loss(x, w, indices, teacher, temperature, loss, lse, workspace, _handle_of(stream))
+    if status:
+        raise SnipError(status, where)
+    return loss, lse
+
+
+def _vocab_loss_backward(where, x, w, indices, teacher, temperature, lse, dloss, dx, dw, out_dtype, accumulate, workspace, inputs, weights, stream):
+    if (dx is not None and not inputs) or (dw is not None and not weights):
+        raise ValueError("a gradient's buffer without the gradient")
+    if accumulate and weights and dw is None:
+        raise ValueError("accumulate needs the gradient to be added to")
+    if (dx is None and inputs) or (dw is None and weights) or workspace is None:
+        with _alloc_on(stream):
+            if dx is None and inputs:
+                dx = torch.empty(x.shape, dtype=torch.bfloat16, device=x.device)
+            if dw is None and weights:
+                dw = torch.empty(w.shape, dtype=torch.bfloat16 if out_dtype == OUT_BF16 else torch.float32, device=x.device)
+            if workspace is None:
+                k = 1 if teacher is None else indices.shape[1]
+                workspace = torch.empty(vocab_loss_backward_workspace_bytes(x.shape[0], x.shape[1], w.shape[0], k), dtype=torch.uint8, device=x.device)
+    status = _nat().vocab_loss_backward(x, w, indices, teacher, temperature, lse, dloss, dx, dw, int(accumulate), workspace, _handle_of(stream))
+    if status:
+        raise SnipError(status, where)
+    return dx, dw
+
+
+def snip_cross_entropy(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                       workspace: Optional[torch.Tensor] = None, stream=None):
+    """Softmax cross entropy of x (bf16 [tokens, cols]) against the head's weight w (bf16 [vocab, cols]) without storing the logits; returns (loss, lse),
+    fp32 [tokens] each.  A target outside the vocabulary (-100) has a loss of 0."""
+    return _vocab_loss("snip_cross_entropy", x, w, targets, None, 1.0, loss, lse, workspace, stream)
+
+
+def snip_cross_entropy_backward(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, dloss: Optional[torch.Tensor] = None,
+                                dx: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None, out_dtype: int = OUT_BF16, accumulate: bool = False,
+                                workspace: Optional[torch.Tensor] = None, stream=None, inputs: bool = True, weights: bool = True):
+    """Gradients (dx bf16, dw bf16 or fp32) of sum(dloss * loss), dloss fp32 [tokens] or None for ones; lse from the forward call.  inputs=False: dw alone;
+    weights=False (a frozen head): dx alone; accumulate: dw, which has to be passed then, is added to."""
+    return _vocab_loss_backward("snip_cross_entropy_backward", x, w, targets, None, 1.0, lse, dloss, dx, dw, out_dtype, accumulate, workspace, inputs, weights, stream)
+
+
+def snip_distill(x: torch.Tensor, w: torch.Tensor, indices: torch.Tensor, teacher: torch.Tensor, temperature: float = 1.0, loss: Optional[torch.Tensor] = None,
+                 lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """Divergence of softmax(x w^T / temperature) from a teacher's k largest logits (teacher bf16 or fp32 [tokens, k], their numbers in indices), times
+    temperature^2; returns (loss, lse), fp32 [tokens] each."""
+    if teacher is None:
+        raise ValueError("expected the teacher's logits")
+    return _vocab_loss("snip_distill", x, w, indices, teacher, temperature, loss, lse, workspace, stream)
+
+
+def snip_distill_backward(x: torch.Tensor, w: torch.Tensor, indices: torch.Tensor, teacher: torch.Tensor, lse: torch.Tensor, temperature: float = 1.0,
+                          dloss: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None, out_dtype: int = OUT_BF16,
+                          accumulate: bool = False, workspace: Optional[torch.Tensor] = None, stream=None, inputs: bool = True, weights: bool = True):
+    """Gradients of sum(dloss * loss) of snip_distill; arguments as for snip_cross_entropy_backward."""
+    if teacher is None:
+        raise ValueError("expected the teacher's logits")
+    return _vocab_loss_backward("snip_distill_backward", x, w, indices, teacher, temperature, lse, dloss, dx, dw, out_dtype, accumulate, workspace, inputs, weights, stream)

@@ -468,7 +468,7 @@ snip_status snip_embed_backward(const void* dy, int64_t tokens, int64_t cols, in
 /* Softmax cross entropy of x [tokens][cols] against the head's weight w [vocab][cols], z = x w^T never being stored:
  *     lse[t] = log(sum over v of exp(z[t][v])),   loss[t] = lse[t] - z[t][targets[t]],   0 where targets[t] is no token.
  *   x, w   : device, bf16 [rows][ld], 16-byte aligned; cols and both ld >= cols multiples of 8; cols < 2^20, ld < 2^22; up to 2^21 tokens;
- *            0 < vocab < 2^31.
+ *            0 < vocab <= 2^21.
  *   targets: device, [tokens].
  *   loss, lse: device, fp32 [tokens]; lse is what the backward call needs.  Either may be NULL.
  *   workspace: device, >= snip_vocab_loss_workspace_bytes(tokens, cols, vocab, 1) bytes, 16-byte aligned.  The size never falls as an extent grows;

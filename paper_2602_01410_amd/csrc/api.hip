@@ -106,7 +106,7 @@ snip_status check_out(const snip_qtensor* o, int64_t stored_rows, int64_t stored
 }
 
 // Operands of the calls at both ends of a model: rows of a table or of tokens, whole pieces of 16 bytes.
-constexpr int64_t kMostTokens = 1 << 21, kMostLd = 1 << 22, kMostVocab = (int64_t)1 << 31, kMostWidth = 1 << 20;
+constexpr int64_t kMostTokens = 1 << 21, kMostLd = 1 << 22, kMostVocab = (int64_t)1 << 31, kMostHead = 1 << 21, kMostWidth = 1 << 20;
 bool valid_type(int t) { return t == SNIP_OUT_BF16 || t == SNIP_OUT_FP32; }
 snip_status check_index(const void* p, int type, int64_t n)
 {
@@ -116,7 +116,7 @@ snip_status check_index(const void* p, int type, int64_t n)
 }
 snip_status check_vocab_loss(const VocabLossArgs& a, int index_type)
 {
-    if (a.tokens < 0 || a.tokens > kMostTokens || a.vocab <= 0 || a.vocab >= kMostVocab || a.cols <= 0 || a.cols >= kMostWidth || a.cols % 8 != 0) return SNIP_ERR_SHAPE;
+    if (a.tokens < 0 || a.tokens > kMostTokens || a.vocab <= 0 || a.vocab > kMostHead || a.cols <= 0 || a.cols >= kMostWidth || a.cols % 8 != 0) return SNIP_ERR_SHAPE;
     if (a.ldx >= kMostLd || a.ldw >= kMostLd) return SNIP_ERR_SHAPE;
     if (a.k < 1 || a.k > 1024 || a.tokens * a.k >= (int64_t)1 << 31) return SNIP_ERR_SHAPE;
     if (!std::isfinite(a.tau) || !(a.tau > 0.f) || !std::isfinite(1.f / a.tau)) return SNIP_ERR_FORMAT;
@@ -680,11 +680,11 @@ size_t snip_vocab_loss_backward_workspace_bytes(int64_t tokens, int64_t cols, in
 }
 
 static VocabLossArgs loss_args(const void* x, int64_t tokens, int64_t cols, int64_t ld_x, const void* w, int64_t vocab, int64_t ld_w, const void* indices,
-                               int index_dtype, const void* teacher, int teacher_dtype, int64_t k, float tau, void* workspace)
+                               int index_dtype, bool distill, const void* teacher, int teacher_dtype, int64_t k, float tau, void* workspace)
 {
     VocabLossArgs a = {};
     a.x = (const uint16_t*)x; a.tokens = tokens; a.cols = cols; a.ldx = ld_x; a.w = (const uint16_t*)w; a.vocab = vocab; a.ldw = ld_w;
-    a.indices = indices; a.index64 = index_dtype == SNIP_INDEX_I64; a.teacher = teacher; a.teacher_fp32 = teacher_dtype == SNIP_OUT_FP32;
+    a.indices = indices; a.index64 = index_dtype == SNIP_INDEX_I64; a.distill = distill; a.teacher = teacher; a.teacher_fp32 = teacher_dtype == SNIP_OUT_FP32;
     a.k = k; a.tau = tau; a.workspace = workspace;
     return a;
 }
@@ -697,7 +697,7 @@ snip_status snip_cross_entropy(const void* x, int64_t tokens, int64_t cols, int6
                                const void* targets, snip_index_dtype index_dtype, float* loss, float* lse, void* workspace,
                                size_t workspace_bytes_, void* stream)
 {
-    VocabLossArgs a = loss_args(x, tokens, cols, ld_x, w, vocab, ld_w, targets, index_dtype, nullptr, SNIP_OUT_BF16, 1, 1.f, workspace);
+    VocabLossArgs a = loss_args(x, tokens, cols, ld_x, w, vocab, ld_w, targets, index_dtype, false, nullptr, SNIP_OUT_BF16, 1, 1.f, workspace);
     a.loss = loss; a.lse = lse;
     return vocab_loss(a, index_dtype, workspace_bytes_, stream);
 }
@@ -706,7 +706,7 @@ snip_status snip_cross_entropy_backward(const void* x, int64_t tokens, int64_t c
                                         const float* dloss, void* dx, int64_t ld_dx, void* dw, snip_out_dtype dw_dtype, int64_t ld_dw,
                                         int32_t accumulate, void* workspace, size_t workspace_bytes_, void* stream)
 {
-    VocabLossArgs a = loss_args(x, tokens, cols, ld_x, w, vocab, ld_w, targets, index_dtype, nullptr, SNIP_OUT_BF16, 1, 1.f, workspace);
+    VocabLossArgs a = loss_args(x, tokens, cols, ld_x, w, vocab, ld_w, targets, index_dtype, false, nullptr, SNIP_OUT_BF16, 1, 1.f, workspace);
     grad_args(a, lse, dloss, dx, ld_dx, dw, dw_dtype, ld_dw, accumulate);
     return vocab_loss_backward(a, index_dtype, dw_dtype, workspace_bytes_, stream);
 }
@@ -716,7 +716,7 @@ snip_status snip_distill(const void* x, int64_t tokens, int64_t cols, int64_t ld
 {
     const snip_status st = check_teacher(teacher, teacher_dtype, tokens);
     if (st != SNIP_OK) return st;
-    VocabLossArgs a = loss_args(x, tokens, cols, ld_x, w, vocab, ld_w, indices, index_dtype, teacher, teacher_dtype, k, temperature, workspace);
+    VocabLossArgs a = loss_args(x, tokens, cols, ld_x, w, vocab, ld_w, indices, index_dtype, true, teacher, teacher_dtype, k, temperature, workspace);
     a.loss = loss; a.lse = lse;
     return vocab_loss(a, index_dtype, workspace_bytes_, stream);
 }
@@ -728,7 +728,7 @@ snip_status snip_distill_backward(const void* x, int64_t tokens, int64_t cols, i
 {
     const snip_status st = check_teacher(teacher, teacher_dtype, tokens);
     if (st != SNIP_OK) return st;
-    VocabLossArgs a = loss_args(x, tokens, cols, ld_x, w, vocab, ld_w, indices, index_dtype, teacher, teacher_dtype, k, temperature, workspace);
+    VocabLossArgs a = loss_args(x, tokens, cols, ld_x, w, vocab, ld_w, indices, index_dtype, true, teacher, teacher_dtype, k, temperature, workspace);
     grad_args(a, lse, dloss, dx, ld_dx, dw, dw_dtype, ld_dw, accumulate);
     return vocab_loss_backward(a, index_dtype, dw_dtype, workspace_bytes_, stream);
 }

@@ -214,12 +214,12 @@ struct EmbedGradArgs {
 size_t embed_workspace_bytes(int64_t tokens, int64_t cols, int64_t vocab);
 hipError_t launch_embed_backward(const EmbedGradArgs& a, hipStream_t s);
 
-// The loss over the vocabulary and its gradients (vocab_loss.hip); cross entropy: teacher null, k 1, tau 1.
+// The loss over the vocabulary and its gradients (vocab_loss.hip); cross entropy: k 1, tau 1.
 struct VocabLossArgs {
     const uint16_t* x; int64_t tokens, cols, ldx;
     const uint16_t* w; int64_t vocab, ldw;
     const void* indices; int index64;
-    const void* teacher; int teacher_fp32;
+    bool distill; const void* teacher; int teacher_fp32;
     int64_t k;
     float tau;
     float *loss, *lse;                       // forward, either may be null

@@ -3,28 +3,25 @@
 //     lse = log sum_v exp s_v      loss = tau^2 sum_j q_j (log q_j - s_idx_j + lse)
 //     dz = dloss tau (exp(s - lse) - q)      dx = dz w      dw = dz^T x
 //
-// All of it is one matrix product in bf16 (v_mfma_f32_32x32x16_bf16, C[i][j] = sum_r A[i][r] B[j][r], both operands contiguous along r)
-// with four ways to take the result out of the accumulators:
+// All of it is one matrix product in bf16 (v_mfma_f32_32x32x16_bf16, C[i][j] = sum_r A[i][r] B[j][r]) with four ways to take the result out
+// of the accumulators:
 //   stats   A = w, B = x: of every token the tile's largest z and the sum of exp(s - largest), and z of the entries that the loss names;
 //           a second kernel joins the tiles.  A token's logits lie in the registers of two lanes, so the sums need no shuffles.
-//   dz      the same product anew, a piece of the vocabulary at a time: dz in bf16, as [token][entry] and as [entry][token]
+//   dz      the same product anew, a piece of the vocabulary at a time: dz in bf16, [token][entry]
 //   dx      A = w^T of the piece, B = dz, split over the vocabulary where there are few tiles: partial sums in fp32, joined at the end
 //   dw      A = x^T, B = dz^T
+// An operand that is contiguous along its other index ("turned": w^T, x^T, dz^T) comes into LDS as it lies in memory and is turned by the reads
+// (ds_read_b64_tr_b16: of each 16 lanes, lane l gets element l of four rows), so nothing is transposed in memory.
 #include "gemm_common.h"
 #include <algorithm>
 
 namespace snip {
 namespace {
 
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kLog2e = 1.44269504088896340736f;
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
 enum Out { kStats, kDz, kDx, kDw };
-
-struct Entries {                 // what the loss names, of every token
-    const int* index;            // [tokens][pitch], -1: nothing
-    const float* q;
-    int k, pitch;
-};
 
 struct ProductArgs {
     const uint16_t *a, *b;
@@ -32,79 +29,162 @@ struct ProductArgs {
     int I, J, R;
     int tiles_i, tiles_j, split; // stages of a split (blockIdx.y)
     float alpha;                 // 1 / tau
-    Entries e;
+    // What the loss names: a target of every token, or lists, a run of each tile (vocabulary tiles of a token tile in turn): token and entry within
+    // the tile (16 bits each), and the place in `z` or q itself
+    const void* targets; int target64;
+    const int* starts; const int2* items; int64_t items_pitch; int vocab_tiles;
     int v0, vocab;               // entry of A's first row
     float2* tile_stats;          // stats: [tiles_i][J]
-    float* z;                    // stats: [J][pitch]
+    float* z;                    // stats: of every named entry
     const float* lse;            // dz
     const float* coef;           // dz: dloss tau of every token, zero for those that take no part
-    uint16_t *dz, *dzt;          // dz: [J][lddz], [.][lddzt]
-    int64_t lddz, lddzt;
-    int jpad;                    // dz: columns of dzt to be written
-    float* sum; int64_t ldsum, split_stride; int add;      // dx
-    void* c; int64_t ldc; int c_fp32;                      // dw (and add)
+    void* c; int64_t ldc, split_stride; int c_fp32, add;   // dz, dx (fp32), dw
 };
 
-// TM x TN outputs of a workgroup, WM x WN of a wave, NST stages of 64 contraction elements in LDS.
-template <int TM_, int TN_, int WM_, int WN_, int NST_> struct Tile {
-    static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, NST = NST_, MB = WM / 32, NB = WN / 32;
-    static constexpr int WGM = TM / WM, WGN = TN / WN, NW = WGM * WGN, NT = NW * 64;
-    static constexpr int SLOT = (TM + TN) * 128, LDS = NST * SLOT, COPIES = (TM + TN) / 8 / NW;      // 1 KB copies of a wave and stage
-    static_assert((TM + TN) / 8 % NW == 0 && LDS <= 160 * 1024, "tile");
+// TM x TN outputs of a workgroup of four waves, WM x WN of a wave.  LDS is a ring of SLOTS slots, a stage (64 contraction elements) of A and B
+// in turn; an odd number needs slots of one size.
+template <int TM_, int TN_, int WM_, int WN_, int SLOTS_, int PER_CU_> struct Tile {
+    static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, SLOTS = SLOTS_, PER_CU = PER_CU_, MB = WM / 32, NB = WN / 32, NM = MB * NB;
+    static constexpr int WGM = TM / WM, WGN = TN / WN, NT = 256;
+    static constexpr int SA = TM * 128, SB = TN * 128, PAIR = SA + SB, LDS = SLOTS / 2 * PAIR + SLOTS % 2 * SA;
+    static constexpr int CA = TM / 32, CB = TN / 32;             // 1 KB copies of a wave and stage
+    static constexpr int DA = (SLOTS + 1) / 2, DB = SLOTS / 2;   // how many stages ahead copies are issued
+    // copies that may be under way when the next stage has to be there: those behind it
+    static constexpr int BEHIND = (DB - 2) * (CA + CB) + (SLOTS % 2 ? CA : 0);
+    static constexpr int BEHIND_FIRST = (SLOTS / 2 - 1) * (CA + CB) + SLOTS % 2 * CA;
+    static_assert(WGM * WGN == 4 && (SLOTS % 2 == 0 || SA == SB) && DB >= 2 && LDS * PER_CU <= 160 * 1024, "tile");
 };
+using Large = Tile<256, 256, 128, 128, 5, 1>;
+using Middle = Tile<128, 128, 64, 64, 5, 2>;
+using Few64 = Tile<128, 64, 64, 32, 6, 2>;
+using Few32 = Tile<128, 32, 32, 32, 8, 2>;
 
 __device__ __forceinline__ unsigned pack2(float a, float b) { return __builtin_bit_cast(unsigned, bf16x2{(__bf16)a, (__bf16)b}); }
-__device__ __forceinline__ uint16_t to_bf16(float a) { return __builtin_bit_cast(uint16_t, (__bf16)a); }
 
-// Calls f(n, j, m, quad, part, entry) for every entry the loss names in this wave's block: of lane's column n the logit acc[m][4 quad + part].
-template <class T, class F>
-__device__ __forceinline__ void named(const Entries& e, int i_base, int j_base, int J, int r32, int g, F f)
+// Two copies of 1 KB, one behind the other in LDS, or one.  The instruction's offset counts in memory and in LDS, so the second lane offset is given
+// 1024 too low and the descriptor starts 1024 bytes early (kEarly).  A single M0 and its wait state for both; a copy holds up the wave that
+// issues it, and with it the matrix core.
+constexpr unsigned kEarly = 1024;
+__device__ __forceinline__ void copy2(v4i rsrc, unsigned o0, unsigned o1, unsigned soff, unsigned lds)
 {
-#pragma unroll
-    for (int n = 0; n < T::NB; ++n) {
-        const int j = j_base + n * 32 + r32;
-        const int* list = e.index + (int64_t)(j < J ? j : J - 1) * e.pitch;
-        for (int x = 0; x < e.k; ++x) {
-            const int at = list[x] - i_base;
-            if (j < J && at >= 0 && at < T::WM && ((at >> 2) & 1) == g) f(n, j, x, at >> 5, ((at & 31) >> 3) * 4 + (at & 3));
-        }
-    }
+    asm volatile("s_mov_b32 m0, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %2, %3 offen lds\n\tbuffer_load_dwordx4 %1, %2, %3 offen offset:1024 lds"
+                 : : "v"(o0), "v"(o1), "s"(rsrc), "s"(soff), "s"(lds) : "memory", "m0");
+}
+__device__ __forceinline__ void copy1(v4i rsrc, unsigned o0, unsigned soff, unsigned lds)
+{
+    asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" : : "v"(o0), "s"(rsrc), "s"(soff), "s"(lds) : "memory", "m0");
+}
+// (scalar arithmetic only: a descriptor from vector registers would need five wait states in front of the copies)
+__device__ __forceinline__ v4i early_desc(const uint16_t* p, unsigned bytes)
+{
+    const uint64_t a = (uint64_t)p - kEarly;
+    v4i r;
+    r[0] = (int)(unsigned)a;
+    r[1] = (int)((unsigned)(a >> 32) & 0xFFFFu);
+    r[2] = (int)(bytes + kEarly);
+    r[3] = 0x00020000;
+    return r;
 }
 
-template <class T, int OUT>
-__global__ __launch_bounds__(T::NT) void product_kernel(const ProductArgs p)
-{
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[T::LDS];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = wave / T::WGN, wn = wave % T::WGN, r32 = lane & 31, g = lane >> 5;
-    int ti, tj;
-    tile_of(blockIdx.x, p.tiles_i * p.tiles_j, p.tiles_i, p.tiles_j, ti, tj);
-    const int i0 = ti * T::TM, j0 = tj * T::TN;
-    const int all = (p.R + 63) / 64;
-    const int first = OUT == kDx ? blockIdx.y * p.split : 0, last = OUT == kDx ? min(all, first + p.split) : all;
+// One operand of a tile: ROWS indices from `row0` on, of which a wave multiplies W from wave_row on.  C copies of this wave and stage.
+// Not turned, a stage is ROWS rows of 128 bytes; 16-byte chunk c of row r lies at c ^ (r / 2 % 8), so that 16 lanes that read one chunk of 16 rows meet
+// all banks.  Turned it is 64 rows of ROWS elements; chunk c of row r lies at c ^ (r % 4 * 4), so that the four rows that a turning read
+// takes from 64 bytes each lie in different banks.
+template <int ROWS, int W, bool TURNED> struct Operand {
+    static constexpr int C = ROWS / 32, BLOCKS = W / 32, READS = BLOCKS * (TURNED ? 2 : 1);
+    const uint16_t* p;
+    int64_t ld;
+    int rows, R;                 // of the tile, of the contraction
+    unsigned off[C];
+    int chunk[2];                // not turned: of even and odd copies
+    int at[4];
+    v4i rsrc;
 
-    const v4i ra = buffer_desc((const uint8_t*)(p.a + i0 * p.lda), (unsigned)(((min(T::TM, p.I - i0) - 1) * p.lda + p.R) * 2));
-    const v4i rb = buffer_desc((const uint8_t*)(p.b + j0 * p.ldb), (unsigned)(((min(T::TN, p.J - j0) - 1) * p.ldb + p.R) * 2));
-    const unsigned lds0 = lds_addr(lds);
-    // copy c of this wave: 8 rows of 128 bytes
-    unsigned off[T::COPIES];
-    int chunk[T::COPIES];
+    __device__ __forceinline__ void start(const uint16_t* base, int64_t ld_, int row0, int all, int R_, int wave_row, int lane, int wave)
+    {
+        // (whole chunks: what is behind an end that is none is zero in one operand at least, or of outputs that are not stored)
+        ld = ld_; rows = (min(ROWS, all - row0) + 7) & ~7; R = TURNED ? R_ : (R_ + 7) & ~7;
+        const int r32 = lane & 31, g = lane >> 5;
+        if constexpr (!TURNED) {
+            p = base + row0 * ld;
+            rsrc = early_desc(p, (unsigned)(((min(ROWS, all - row0) - 1) * ld + R) * 2));
 #pragma unroll
-    for (int c = 0; c < T::COPIES; ++c) {
-        const int row = (wave * T::COPIES + c) * 8 + lane / 8;
-        chunk[c] = (lane % 8) ^ ((row >> 1) & 7);
-        off[c] = (unsigned)((row < T::TM ? row * p.lda : (row - T::TM) * p.ldb) * 2) + chunk[c] * 16;
-    }
-    auto issue = [&](int s) {
-        const unsigned to = lds0 + (s - first) % T::NST * T::SLOT + wave * T::COPIES * 1024;
+            for (int c = 0; c < C; ++c) {
+                const int row = (wave * C + c) * 8 + lane / 8;
+                chunk[c & 1] = (lane % 8) ^ ((row >> 1) & 7);
+                off[c] = (unsigned)(row * ld * 2) + chunk[c & 1] * 16 + early(c);
+            }
 #pragma unroll
-        for (int c = 0; c < T::COPIES; ++c) {
-            const unsigned o = chunk[c] * 8 + s * 64 < p.R ? off[c] : kNoSource;
-            if ((wave * T::COPIES + c) * 8 < T::TM) blds16(ra, o, s * 128, to + c * 1024);
-            else                                    blds16(rb, o, s * 128, to + c * 1024);
+            for (int ks = 0; ks < 4; ++ks) at[ks] = (wave_row + r32) * 128 + (((ks * 2 + g) ^ (r32 >> 1 & 7)) * 16);
+        } else {
+            p = base + row0;
+            constexpr int PER_ROW = ROWS / 8, RPC = 64 / PER_ROW;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int row = (wave * C + c) * RPC + lane / PER_ROW;
+                off[c] = (unsigned)(row * ld * 2) + ((lane % PER_ROW) ^ ((row & 3) * 4)) * 16 + early(c);
+            }
+            // of each 16 lanes, four point to 32 bytes of a row; the two halves of a wave are 8 rows apart
+            const int row = 8 * g + (lane >> 2 & 3);
+#pragma unroll
+            for (int m = 0; m < BLOCKS; ++m)
+                at[m] = row * ROWS * 2 + (((wave_row / 32 + m) ^ (row & 3)) * 64) + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
         }
+    }
+    static __device__ __forceinline__ constexpr unsigned early(int c) { return kEarly - (C % 2 == 0 && c % 2 ? 1024 : 0); }
+    // before the copies of stage s
+    __device__ __forceinline__ void stage(int s)
+    {
+        if constexpr (TURNED) {
+            rsrc = early_desc(p + (int64_t)s * 64 * ld, (unsigned)(((min(64, R - s * 64) - 1) * ld + rows) * 2));
+        } else if (s * 64 + 64 > R) {                               // chunks past the end of a row lose their source
+#pragma unroll
+            for (int c = 0; c < C; ++c) off[c] = chunk[c & 1] * 8 + s * 64 < R ? off[c] : kNoSource;
+        }
+    }
+    static constexpr int UNITS = C % 2 == 0 ? C / 2 : C;
+    __device__ __forceinline__ void copy(int u, int s, unsigned to)
+    {
+        const unsigned soff = TURNED ? 0u : (unsigned)s * 128u;
+        if constexpr (C % 2 == 0) copy2(rsrc, off[2 * u], off[2 * u + 1], soff, to + u * 2048);
+        else                      copy1(rsrc, off[u], soff, to + u * 1024);
+    }
+    __device__ __forceinline__ void read(int i, int ks, const uint8_t* slot, bf16x8 (&f)[BLOCKS]) const
+    {
+        if constexpr (!TURNED) {
+            f[i] = *reinterpret_cast<const bf16x8*>(slot + at[ks] + i * 4096);
+        } else {
+            typedef const __attribute__((address_space(3))) s16x4* place;
+            const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(place)(slot + at[i / 2] + (ks * 16 + i % 2 * 4) * ROWS * 2));
+            uint2 w = __builtin_bit_cast(uint2, v);
+            uint4 old = __builtin_bit_cast(uint4, f[i / 2]);
+            if (i % 2 == 0) { old.x = w.x; old.y = w.y; } else { old.z = w.x; old.w = w.y; }
+            f[i / 2] = __builtin_bit_cast(bf16x8, old);
+        }
+    }
+};
+
+// The products of a tile, stages [first, last) of the contraction, 64 elements each.
+// A stage is four steps; between the MFMAs of a step the wave reads the operands of the next one from LDS (the last step of a stage those of the
+// next stage's first) and issues copies.  A barrier a stage, in front of its last step: every wave has the whole stage in registers
+// then, so its two slots are free, and the next stage has arrived.  With five slots B of stage s + 2 follows A of stage s in the ring and A of
+// stage s + 3 follows B: the copies have 1.5 stages (A) and 0.75 (B) to arrive.
+template <class T, bool TA, bool TB>
+__device__ __forceinline__ void multiply(const ProductArgs& p, uint8_t* lds, int i0, int j0, int first, int last, int lane, int wave, v16f (&acc)[T::MB][T::NB])
+{
+    const int wm = wave / T::WGN, wn = wave % T::WGN;
+    Operand<T::TM, T::WM, TA> a;
+    Operand<T::TN, T::WN, TB> b;
+    a.start(p.a, p.lda, i0, p.I, p.R, wm * T::WM, lane, wave);
+    b.start(p.b, p.ldb, j0, p.J, p.R, wn * T::WN, lane, wave);
+    const unsigned lds0 = lds_addr(lds), share_a = lds0 + wave * T::CA * 1024, share_b = lds0 + wave * T::CB * 1024;
+    auto ahead = [](unsigned slot) { return slot + T::PAIR >= (unsigned)T::LDS ? slot + T::PAIR - T::LDS : slot + T::PAIR; };      // of the next stage
+    bf16x8 fa[2][T::MB], fb[2][T::NB];
+    constexpr int READS = a.READS + b.READS;
+    auto read = [&](int j, int ks, unsigned sa, unsigned sb) {
+        if (j < b.READS) b.read(j, ks, lds + sb, fb[ks & 1]);
+        else             a.read(j - b.READS, ks, lds + sa, fa[ks & 1]);
     };
-    v16f acc[T::MB][T::NB];
 #pragma unroll
     for (int m = 0; m < T::MB; ++m)
 #pragma unroll
@@ -112,47 +192,157 @@ __global__ __launch_bounds__(T::NT) void product_kernel(const ProductArgs p)
 #pragma unroll
             for (int k = 0; k < 16; ++k) acc[m][n][k] = 0.f;
 #pragma unroll
-    for (int s = 0; s < T::NST - 1; ++s)
-        if (first + s < last) issue(first + s);
-    for (int s = first; s < last; ++s) {
-        // the copies of later stages that are under way
-        if (last - s >= T::NST - 1) SNIP_WAIT_VM((T::NST - 2) * T::COPIES);
-        else                        SNIP_WAIT_VM(0);
-        SNIP_BAR();
-        if (s + T::NST - 1 < last) issue(s + T::NST - 1);
-        const uint8_t* slot = lds + (s - first) % T::NST * T::SLOT;
-        const uint8_t* ta = slot + wm * T::WM * 128 + r32 * 128;
-        const uint8_t* tb = slot + T::TM * 128 + wn * T::WN * 128 + r32 * 128;
-        const int f = (r32 >> 1) & 7;
+    for (int i = 0; i < T::SLOTS; ++i) {
+        const int s = first + i / 2;
+        if (s < last) {
+            const unsigned slot = i / 2 * T::PAIR + i % 2 * T::SA;
+            if (i % 2 == 0) {
+                a.stage(s);
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-            bf16x8 fa[T::MB], fb[T::NB];
-            const int at = ((ks * 2 + g) ^ f) * 16;
+                for (int u = 0; u < a.UNITS; ++u) a.copy(u, s, share_a + slot);
+            } else {
+                b.stage(s);
 #pragma unroll
-            for (int m = 0; m < T::MB; ++m) fa[m] = *reinterpret_cast<const bf16x8*>(ta + m * 32 * 128 + at);
-#pragma unroll
-            for (int n = 0; n < T::NB; ++n) fb[n] = *reinterpret_cast<const bf16x8*>(tb + n * 32 * 128 + at);
-#pragma unroll
-            for (int m = 0; m < T::MB; ++m)
-#pragma unroll
-                for (int n = 0; n < T::NB; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[m], fb[n], acc[m][n], 0, 0, 0);
+                for (int u = 0; u < b.UNITS; ++u) b.copy(u, s, share_b + slot);
+            }
         }
     }
-    // In registers, lane (r32, g) of block (m, n) holds C[32 m + 8 q + 4 g + t][32 n + r32] in acc[m][n][4 q + t].
+    if (last - first >= T::DA) SNIP_WAIT_VM(T::BEHIND_FIRST);
+    else                       SNIP_WAIT_VM(0);
+    SNIP_BAR();
+    unsigned sa = 0, sb = T::SA, to_a = 0;
+#pragma unroll
+    for (int j = 0; j < READS; ++j) read(j, 0, sa, sb);
+    bool more_a = false;                                            // A of stage s - 1 + DA belongs into slot to_a
+    for (int s = first; s < last; ++s) {
+        const unsigned na = ahead(sa), nb = ahead(sb);
+        const unsigned to_b = T::SLOTS % 2 ? sa : sb;
+        bool more_b = false;
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            if (ks == 0 && more_a) a.stage(s - 1 + T::DA);
+            if (ks == 3) {
+                __builtin_amdgcn_s_waitcnt(0xC07F);                 // lgkmcnt(0)
+                if (s - 1 + T::DA < last) SNIP_WAIT_VM(T::BEHIND);
+                else                      SNIP_WAIT_VM(0);
+                SNIP_BAR();
+                asm volatile("" ::: "memory");                      // (no read of the next stage before the barrier)
+                more_b = s + T::DB < last;
+                if (more_b) b.stage(s + T::DB);
+            }
+#pragma unroll
+            for (int i = 0; i < T::NM; ++i) {
+                acc[i / T::NB][i % T::NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[ks & 1][i / T::NB], fb[ks & 1][i % T::NB], acc[i / T::NB][i % T::NB], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                // the reads behind the first three quarters of the MFMAs
+#pragma unroll
+                for (int j = 0; j < READS; ++j)
+                    if (j * T::NM * 3 / 4 / READS == i) { if (ks < 3) read(j, ks + 1, sa, sb); else read(j, 0, na, nb); }
+                if (ks == 3 && more_b) {
+#pragma unroll
+                    for (int u = 0; u < b.UNITS; ++u)
+                        if (u * T::NM / b.UNITS + T::NM / b.UNITS / 4 == i) b.copy(u, s + T::DB, share_b + to_b);
+                }
+                if (ks < 2 && more_a) {
+#pragma unroll
+                    for (int u = 0; u < a.UNITS; ++u)
+                        if ((u * T::NM * 2 + T::NM) / a.UNITS == ks * T::NM + i) a.copy(u, s - 1 + T::DA, share_a + to_a);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        to_a = T::SLOTS % 2 ? sb : sa;
+        more_a = s + T::DA < last;
+        sa = na;
+        sb = nb;
+    }
+}
+
+// In registers, lane (r32, g) of block (m, n) holds C[32 m + 8 q + 4 g + t][32 n + r32] in acc[m][n][4 q + t].
+
+// A wave's result leaves through its own part of LDS, 32 columns (rows of the result in memory) of WM numbers at a time: stores are whole runs then, and
+// an element that the loss names is found by its place.  16-byte chunk c of column r lies at c ^ r.
+template <class T> struct Stage {
+    static constexpr int ROWB = T::WM * 4, CPR = ROWB / 16, PART = T::LDS / 4 / 1024 * 1024;
+    static_assert(32 * ROWB <= PART, "a wave's part");
+    uint8_t* reg;
+    int lane, r32, g;
+    __device__ __forceinline__ Stage(uint8_t* lds, int wave, int lane_) : reg(lds + wave * PART), lane(lane_), r32(lane_ & 31), g(lane_ >> 5) {}
+    __device__ __forceinline__ float* at(int col, int row) { return reinterpret_cast<float*>(reg + col * ROWB + (((row >> 2) ^ (col & (CPR - 1))) * 16)) + (row & 3); }
+    __device__ __forceinline__ void put(const v16f (&acc)[T::MB][T::NB], int n)
+    {
+#pragma unroll
+        for (int m = 0; m < T::MB; ++m)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<float4*>(at(r32, m * 32 + q * 8 + g * 4)) = make_float4(acc[m][n][4 * q], acc[m][n][4 * q + 1], acc[m][n][4 * q + 2], acc[m][n][4 * q + 3]);
+    }
+    // calls sink(column, row of the first, eight numbers of a column)
+    template <class F> __device__ __forceinline__ void take(F sink)
+    {
+        constexpr int LANES = T::WM / 8, RPI = 64 / LANES;
+#pragma unroll
+        for (int it = 0; it < 32 / RPI; ++it) {
+            const int col = it * RPI + lane / LANES, row = lane % LANES * 8;
+            const float4 u = *reinterpret_cast<const float4*>(at(col, row)), v = *reinterpret_cast<const float4*>(at(col, row + 4));
+            const float f[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+            sink(col, row, f);
+        }
+    }
+};
+
+// The elements of columns 32 n ... 32 n + 31 of this wave's block that the loss names: calls f(column, row, item), a lane for each, with the item of a
+// list or, of targets, the token.  `any` is called first if there are some.
+template <class T, class G, class F>
+__device__ __forceinline__ void named(const ProductArgs& p, int ti, int tj, int wm, int wn, int lane, int n, G any, F f)
+{
+    if (p.targets) {
+        const int j = tj * T::TN + wn * T::WN + n * 32 + lane;
+        int64_t v = -1;
+        if (lane < 32 && j < p.J) v = p.target64 ? ((const int64_t*)p.targets)[j] : (int64_t)((const int*)p.targets)[j];
+        const int64_t row = v - (p.v0 + ti * T::TM + wm * T::WM);
+        const bool is = v < p.vocab && row >= 0 && row < T::WM;
+        if (__builtin_amdgcn_ballot_w64(is) == 0) return;
+        any();
+        if (is) f(lane, (int)row, j);
+        return;
+    }
+    const int* run = p.starts + (int64_t)tj * (p.vocab_tiles + 1) + p.v0 / T::TM + ti;
+    const int from = __builtin_amdgcn_readfirstlane(run[0]), to = __builtin_amdgcn_readfirstlane(run[1]);
+    const int2* items = p.items + tj * p.items_pitch;
+    bool first = true;
+    for (int e = from; e < to; e += 64) {
+        const int2 mine = items[min(e + lane, to - 1)];
+        const int row = (mine.x >> 16) - wm * T::WM, col = (mine.x & 0xFFFF) - wn * T::WN - n * 32;
+        const bool is = e + lane < to && row >= 0 && row < T::WM && col >= 0 && col < 32;
+        if (__builtin_amdgcn_ballot_w64(is) == 0) continue;
+        if (first) any();
+        first = false;
+        if (is) f(col, row, mine.y);
+    }
+}
+
+__device__ __forceinline__ v4u packed(const float (&f)[8]) { return v4u{pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7])}; }
+
+template <class T, int OUT>
+__global__ __launch_bounds__(T::NT, T::PER_CU) void product_kernel(const ProductArgs p)
+{
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[T::LDS];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / T::WGN, wn = wave % T::WGN, r32 = lane & 31, g = lane >> 5;
+    int ti, tj;
+    tile_of(blockIdx.x, p.tiles_i * p.tiles_j, p.tiles_i, p.tiles_j, ti, tj);
+    const int i0 = ti * T::TM, j0 = tj * T::TN;
+    const int all = (p.R + 63) / 64, first = OUT == kDx ? blockIdx.y * p.split : 0, last = OUT == kDx ? min(all, first + p.split) : all;
+    v16f acc[T::MB][T::NB];
+    multiply<T, (OUT == kDx || OUT == kDw), OUT == kDw>(p, lds, i0, j0, first, last, lane, wave, acc);
     const int iw = i0 + wm * T::WM, jw = j0 + wn * T::WN;
 
+    Stage<T> stage(lds, wave, lane);
     if constexpr (OUT == kStats) {
-        named<T>(p.e, p.v0 + iw, jw, p.J, r32, g, [&](int n, int j, int x, int m, int at) {
-            float z = 0.f;
 #pragma unroll
-            for (int mm = 0; mm < T::MB; ++mm)
-#pragma unroll
-                for (int nn = 0; nn < T::NB; ++nn)
-#pragma unroll
-                    for (int k = 0; k < 16; ++k)
-                        if (nn == n && mm == m && k == at) z = acc[mm][nn][k];
-            p.z[(int64_t)j * p.e.pitch + x] = z;
-        });
+        for (int n = 0; n < T::NB; ++n)
+            named<T>(p, ti, tj, wm, wn, lane, n, [&]() { stage.put(acc, n); }, [&](int col, int row, int place) { p.z[place] = *stage.at(col, row); });
         if (iw + T::WM > p.I) {
 #pragma unroll
             for (int m = 0; m < T::MB; ++m)
@@ -200,145 +390,112 @@ __global__ __launch_bounds__(T::NT) void product_kernel(const ProductArgs p)
 #pragma unroll
         for (int n = 0; n < T::NB; ++n) {
             const int j = jw + n * 32 + r32;
-            const float lse = j < p.J ? p.lse[j] : 0.f;
+            const float lse = j < p.J ? p.lse[j] : 0.f, mine = j < p.J ? p.coef[j] : 0.f;
 #pragma unroll
             for (int m = 0; m < T::MB; ++m)
 #pragma unroll
                 for (int k = 0; k < 16; ++k) acc[m][n][k] = __builtin_amdgcn_exp2f(fmaf(acc[m][n][k], p.alpha, -lse) * kLog2e);
-        }
-        named<T>(p.e, p.v0 + iw, jw, p.J, r32, g, [&](int n, int j, int x, int m, int at) {
-            const float q = p.e.q[(int64_t)j * p.e.pitch + x];
+            stage.put(acc, n);
+            named<T>(p, ti, tj, wm, wn, lane, n, []() {}, [&](int col, int row, int q) { *stage.at(col, row) -= p.targets ? 1.f : __int_as_float(q); });
+            stage.take([&](int col, int row, const float (&f)[8]) {
+                const float coef = __shfl(mine, col);
+                float v[8];
 #pragma unroll
-            for (int mm = 0; mm < T::MB; ++mm)
-#pragma unroll
-                for (int nn = 0; nn < T::NB; ++nn)
-#pragma unroll
-                    for (int k = 0; k < 16; ++k)
-                        if (nn == n && mm == m && k == at) acc[mm][nn][k] -= q;
-        });
-#pragma unroll
-        for (int n = 0; n < T::NB; ++n) {
-            const int j = jw + n * 32 + r32;
-            const float coef = j < p.J ? p.coef[j] : 0.f;
-#pragma unroll
-            for (int m = 0; m < T::MB; ++m)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int i = iw + m * 32 + 8 * q + 4 * g;
-                    float v[4];
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) v[t] = coef == 0.f || i + t >= p.I ? 0.f : acc[m][n][4 * q + t] * coef;
-                    if (j < p.J && i < p.lddz) *reinterpret_cast<uint2*>(p.dz + j * p.lddz + i) = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
-                    if (p.dzt && j < p.jpad) {
-#pragma unroll
-                        for (int t = 0; t < 4; ++t)
-                            if (i + t < p.I) p.dzt[(i + t) * p.lddzt + j] = to_bf16(v[t]);
-                    }
-                }
+                for (int e = 0; e < 8; ++e) v[e] = coef == 0.f || iw + row + e >= p.I ? 0.f : f[e] * coef;
+                // (the pitch covers whole tiles)
+                if (jw + n * 32 + col < p.J) *reinterpret_cast<v4u*>((uint16_t*)p.c + (jw + n * 32 + col) * p.ldc + iw + row) = packed(v);
+            });
         }
     }
-    if constexpr (OUT == kDx) {
-        float* sum = p.sum + blockIdx.y * p.split_stride;
+    if constexpr (OUT == kDx || OUT == kDw) {
 #pragma unroll
         for (int n = 0; n < T::NB; ++n) {
-            const int j = jw + n * 32 + r32;
+            stage.put(acc, n);
+            stage.take([&](int col, int row, const float (&f)[8]) {
+                const int j = jw + n * 32 + col, i = iw + row;
+                if (j >= p.J || i >= p.I) return;                   // (I is a multiple of 8)
+                float v[8];
 #pragma unroll
-            for (int m = 0; m < T::MB; ++m)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int i = iw + m * 32 + 8 * q + 4 * g;
-                    if (j >= p.J || i >= p.I) continue;                     // (I is a multiple of 8)
-                    float4* to = reinterpret_cast<float4*>(sum + j * p.ldsum + i);
-                    float4 v = make_float4(acc[m][n][4 * q], acc[m][n][4 * q + 1], acc[m][n][4 * q + 2], acc[m][n][4 * q + 3]);
+                for (int e = 0; e < 8; ++e) v[e] = f[e];
+                if (OUT == kDx || p.c_fp32) {
+                    float4* to = reinterpret_cast<float4*>((float*)p.c + (OUT == kDx ? blockIdx.y * p.split_stride : 0) + j * p.ldc + i);
                     if (p.add) {
-                        const float4 o = *to;
-                        v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+                        const float4 o = to[0], q = to[1];
+                        v[0] += o.x; v[1] += o.y; v[2] += o.z; v[3] += o.w; v[4] += q.x; v[5] += q.y; v[6] += q.z; v[7] += q.w;
                     }
-                    *to = v;
-                }
-        }
-    }
-    if constexpr (OUT == kDw) {
+                    to[0] = make_float4(v[0], v[1], v[2], v[3]);
+                    to[1] = make_float4(v[4], v[5], v[6], v[7]);
+                } else {
+                    v4u* to = reinterpret_cast<v4u*>((uint16_t*)p.c + j * p.ldc + i);
+                    if (p.add) {
+                        const v4u o = *to;
 #pragma unroll
-        for (int n = 0; n < T::NB; ++n) {
-            const int j = jw + n * 32 + r32;
-#pragma unroll
-            for (int m = 0; m < T::MB; ++m)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int i = iw + m * 32 + 8 * q + 4 * g;
-                    if (j >= p.J || i >= p.I) continue;
-                    float4 v = make_float4(acc[m][n][4 * q], acc[m][n][4 * q + 1], acc[m][n][4 * q + 2], acc[m][n][4 * q + 3]);
-                    if (p.c_fp32) {
-                        float4* to = reinterpret_cast<float4*>((float*)p.c + j * p.ldc + i);
-                        if (p.add) {
-                            const float4 o = *to;
-                            v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
-                        }
-                        *to = v;
-                    } else {
-                        uint2* to = reinterpret_cast<uint2*>((uint16_t*)p.c + j * p.ldc + i);
-                        if (p.add) {
-                            const uint2 o = *to;
-                            v.x += __uint_as_float(o.x << 16); v.y += __uint_as_float(o.x & 0xFFFF0000u);
-                            v.z += __uint_as_float(o.y << 16); v.w += __uint_as_float(o.y & 0xFFFF0000u);
-                        }
-                        *to = make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
+                        for (int e = 0; e < 4; ++e) { v[2 * e] += __uint_as_float(o[e] << 16); v[2 * e + 1] += __uint_as_float(o[e] & 0xFFFF0000u); }
                     }
+                    *to = packed(v);
                 }
+            });
         }
     }
 }
 
-// What the loss names, a wave per token: entries (-1 where there is nothing: outside the vocabulary, or q = 0), q, the entropy term sum q log q,
-// and for the gradient dloss tau, zero where no entry counts.
+// What a distillation names, a wave per token: entries (-1 where there is nothing: outside the vocabulary, q = 0, or one named before, which has its q
+// added), q, the entropy term sum q log q, and for the gradient dloss tau, zero where no entry counts.
 template <bool I64>
 __global__ __launch_bounds__(256) void entries_kernel(const void* __restrict__ indices, const void* __restrict__ teacher, bool teacher_fp32, int tokens, int vocab,
-                                                      int k, int pitch, float tau, const float* __restrict__ dloss, int* __restrict__ index, float* __restrict__ q,
+                                                      int k, float tau, const float* __restrict__ dloss, int* __restrict__ index, float* __restrict__ q,
                                                       float* __restrict__ entropy, float* __restrict__ coef)
 {
-    const int lane = threadIdx.x & 63;
+    __shared__ int numbers[4][1024];
+    __shared__ float wants[4][1024];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const float alpha = 1.f / tau;
-    for (int t = blockIdx.x * 4 + (threadIdx.x >> 6); t < tokens; t += gridDim.x * 4) {
-        auto number = [&](int j) {
-            const int64_t v = I64 ? ((const int64_t*)indices)[(int64_t)t * k + j] : ((const int*)indices)[(int64_t)t * k + j];
-            return v >= 0 && v < vocab ? (int)v : -1;
-        };
-        auto wanted = [&](int j) {
-            if (!teacher) return 0.f;
-            const int64_t at = (int64_t)t * k + j;
-            return (teacher_fp32 ? ((const float*)teacher)[at] : __uint_as_float((unsigned)((const uint16_t*)teacher)[at] << 16)) * alpha;
-        };
+    for (int t = blockIdx.x * 4 + wave; t < tokens; t += gridDim.x * 4) {
+        const int64_t row = (int64_t)t * k;
         float top = -INFINITY;
         bool any = false;
-        for (int j = lane; j < k; j += 64)
-            if (number(j) >= 0) {
-                const float u = wanted(j);
-                any = any || !(u == -INFINITY);
-                top = fmaxf(top, u);
-            }
+        for (int j = lane; j < k; j += 64) {
+            const int64_t v = I64 ? ((const int64_t*)indices)[row + j] : ((const int*)indices)[row + j];
+            const float u = (teacher_fp32 ? ((const float*)teacher)[row + j] : __uint_as_float((unsigned)((const uint16_t*)teacher)[row + j] << 16)) * alpha;
+            const bool is = v >= 0 && v < vocab;
+            numbers[wave][j] = is ? (int)v : -1;
+            wants[wave][j] = u;
+            any = any || (is && !(u == -INFINITY));
+            if (is) top = fmaxf(top, u);
+        }
         for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
         any = __builtin_amdgcn_ballot_w64(any) != 0;
         const float base = top == -INFINITY ? 0.f : top;
         float sum = 0.f;
         for (int j = lane; j < k; j += 64)
-            if (number(j) >= 0) sum += expf(wanted(j) - base);
+            if (numbers[wave][j] >= 0) sum += expf(wants[wave][j] - base);
         for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
         const float log_sum = logf(sum);
         float ent = 0.f;
-        for (int j = lane; j < pitch; j += 64) {
-            int v = j < k && any ? number(j) : -1;
+        for (int j = lane; j < k; j += 64) {
             float w = 0.f;
-            if (v >= 0) {
-                const float l = wanted(j) - base - log_sum;
+            if (any && numbers[wave][j] >= 0) {
+                const float l = wants[wave][j] - base - log_sum;
                 w = expf(l);
-                if (w == 0.f) v = -1;
-                else ent += w * l;
+                if (w != 0.f) ent += w * l;
             }
-            index[(int64_t)t * pitch + j] = v;
-            q[(int64_t)t * pitch + j] = w;
+            if (w == 0.f) numbers[wave][j] = -1;
+            wants[wave][j] = w;
         }
         for (int d = 32; d > 0; d >>= 1) ent += __shfl_xor(ent, d);
+        for (int j = lane; j < k; j += 64) {
+            const int v = numbers[wave][j];
+            float w = 0.f;
+            bool before = false;
+            if (v >= 0)
+                for (int i = 0; i < k; ++i)
+                    if (numbers[wave][i] == v) {
+                        before = before || i < j;
+                        w += wants[wave][i];
+                    }
+            index[row + j] = before ? -1 : v;
+            q[row + j] = before ? 0.f : w;
+        }
         if (lane == 0) {
             if (entropy) entropy[t] = ent;
             if (coef) coef[t] = any ? (dloss ? dloss[t] : 1.f) * tau : 0.f;
@@ -346,8 +503,58 @@ __global__ __launch_bounds__(256) void entries_kernel(const void* __restrict__ i
     }
 }
 
+// Lists of the entries by tile: a workgroup for each `tn` tokens counts the entries of every vocabulary tile (1 << log_tm entries), forms their places
+// and writes them.  The order within a tile's run varies; no two items of a run are of one element.
+constexpr int kMostTiles = 1 << 14;
+__global__ __launch_bounds__(1024) void lists_kernel(const int* __restrict__ index, const float* __restrict__ q, int tokens, int k, int tn, int log_tm, int tiles,
+                                                     bool want_q, int* __restrict__ starts, int2* __restrict__ items)
+{
+    __shared__ int counts[kMostTiles];
+    __shared__ int sums[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int t0 = blockIdx.x * tn, here = min(tn, tokens - t0) * k;
+    const int64_t base = (int64_t)t0 * k;
+    for (int i = threadIdx.x; i < tiles; i += 1024) counts[i] = 0;
+    __syncthreads();
+#pragma unroll 4
+    for (int i = threadIdx.x; i < here; i += 1024) {
+        const int v = index[base + i];
+        if (v >= 0) atomicAdd(&counts[v >> log_tm], 1);
+    }
+    __syncthreads();
+    int* out = starts + (int64_t)blockIdx.x * (tiles + 1);
+    int before = 0;
+    for (int i0 = 0; i0 < tiles; i0 += 1024) {
+        const int i = i0 + threadIdx.x, n = i < tiles ? counts[i] : 0;
+        int inc = n;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(inc, d);
+            if (lane >= d) inc += o;
+        }
+        if (lane == 63) sums[wave] = inc;
+        __syncthreads();
+        int at = before + inc - n, all = 0;
+        for (int w = 0; w < 16; ++w) {
+            if (w < wave) at += sums[w];
+            all += sums[w];
+        }
+        if (i < tiles) { out[i] = at; counts[i] = at; }
+        before += all;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) out[tiles] = before;
+    for (int i = threadIdx.x; i < here; i += 1024) {
+        const int v = index[base + i];
+        if (v < 0) continue;
+        const int at = atomicAdd(&counts[v >> log_tm], 1);
+        items[base + at] = make_int2((v & ((1 << log_tm) - 1)) << 16 | i / k, want_q ? __float_as_int(q[base + i]) : (int)(base + i));
+    }
+}
+
 // The tiles' sums joined and the loss formed: 16 tokens of a workgroup, 16 threads of a token.
-__global__ __launch_bounds__(256) void join_kernel(const float2* __restrict__ tile_stats, int tiles, int tokens, float alpha, float tau, Entries e, const float* __restrict__ z,
+__global__ __launch_bounds__(256) void join_kernel(const float2* __restrict__ tile_stats, int tiles, int tokens, int vocab, float alpha, float tau, const void* __restrict__ targets,
+                                                   int target64, const int* __restrict__ index, const float* __restrict__ q, int k, const float* __restrict__ z,
                                                    const float* __restrict__ entropy, float* __restrict__ loss, float* __restrict__ lse)
 {
     __shared__ float2 shared[16][17];
@@ -367,40 +574,40 @@ __global__ __launch_bounds__(256) void join_kernel(const float2* __restrict__ ti
     const float l = fmaf(v.x, alpha, logf(v.y));
     if (lse) lse[t] = l;
     if (!loss) return;
+    if (targets) {
+        const int64_t at = target64 ? ((const int64_t*)targets)[t] : (int64_t)((const int*)targets)[t];
+        loss[t] = at >= 0 && at < vocab ? l - z[t] : 0.f;
+        return;
+    }
     float sum = 0.f;
     bool any = false;
-    for (int j = 0; j < e.k; ++j) {
-        const int64_t at = (int64_t)t * e.pitch + j;
-        if (e.index[at] >= 0) {
-            sum = fmaf(e.q[at], fmaf(-z[at], alpha, l), sum);
+    for (int j = 0; j < k; ++j) {
+        const int64_t at = (int64_t)t * k + j;
+        if (index[at] >= 0) {
+            sum = fmaf(q[at], fmaf(-z[at], alpha, l), sum);
             any = true;
         }
     }
     loss[t] = any ? (sum + entropy[t]) * tau * tau : 0.f;
 }
 
-// out[c][r] = in[r][c] of a bf16 matrix, zeros for r in [rows, rows_pad) (a multiple of 8, as cols is) and for rows whose `keep` is zero.
-__global__ __launch_bounds__(256) void transpose_kernel(const uint16_t* __restrict__ in, int64_t ld, int rows, int cols, const float* __restrict__ keep, uint16_t* __restrict__ out,
-                                                        int64_t ldo, int rows_pad)
+// x without the rows of tokens that take no part (their x may hold anything), a wave per token; with targets coef is formed here.
+__global__ __launch_bounds__(256) void part_kernel(const uint16_t* __restrict__ x, int64_t ld, int tokens, int cols, int vocab, const void* __restrict__ targets, int target64,
+                                                   const float* __restrict__ dloss, float* __restrict__ coef, uint16_t* __restrict__ out)
 {
-    __shared__ uint16_t tile[64][66];
-    const int r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
-    for (int i = threadIdx.x; i < 64 * 8; i += 256) {
-        const int r = i / 8, c = i % 8 * 8;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (r0 + r < rows && c0 + c < cols && !(keep && keep[r0 + r] == 0.f)) v = *reinterpret_cast<const uint4*>(in + (r0 + r) * ld + c0 + c);
-        const unsigned w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) *reinterpret_cast<unsigned*>(&tile[r][c + 2 * k]) = w[k];
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 64 * 8; i += 256) {
-        const int c = i / 8, r = i % 8 * 8;
-        if (c0 + c >= cols || r0 + r >= rows_pad) continue;
-        unsigned w[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = tile[r + 2 * k][c] | (unsigned)tile[r + 2 * k + 1][c] << 16;
-        *reinterpret_cast<uint4*>(out + (c0 + c) * ldo + r0 + r) = make_uint4(w[0], w[1], w[2], w[3]);
+    const int lane = threadIdx.x & 63;
+    for (int t = blockIdx.x * 4 + (threadIdx.x >> 6); t < tokens; t += gridDim.x * 4) {
+        float g;
+        if (targets) {
+            const int64_t at = target64 ? ((const int64_t*)targets)[t] : (int64_t)((const int*)targets)[t];
+            g = at >= 0 && at < vocab ? (dloss ? dloss[t] : 1.f) : 0.f;
+            if (lane == 0) coef[t] = g;
+        } else {
+            g = coef[t];
+        }
+        if (out)
+            for (int c = lane * 8; c < cols; c += 512)
+                *reinterpret_cast<uint4*>(out + (int64_t)t * cols + c) = g == 0.f ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4*>(x + t * ld + c);
     }
 }
 
@@ -433,8 +640,19 @@ template <bool FP32> __global__ __launch_bounds__(256) void zero_kernel(void* ou
     }
 }
 
-using Big = Tile<256, 256, 128, 64, 2>;
-using Few = Tile<128, 32, 32, 32, 4>;
+constexpr int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
+size_t to256(size_t n) { return (n + 255) / 256 * 256; }
+
+enum class Shape { kLarge, kMiddle, kFew64, kFew32 };
+constexpr int tile_rows(Shape s) { return s == Shape::kLarge ? 256 : 128; }
+constexpr int tile_cols(Shape s) { return s == Shape::kLarge ? 256 : s == Shape::kMiddle ? 128 : s == Shape::kFew64 ? 64 : 32; }
+// The tile for I x J outputs, J of them tokens.
+Shape shape_for(int64_t I, int64_t J)
+{
+    if (J <= 32) return Shape::kFew32;
+    if (J <= 64) return Shape::kFew64;
+    return J <= 128 || up(I, 256) / 256 * (up(J, 256) / 256) < 256 ? Shape::kMiddle : Shape::kLarge;
+}
 
 template <class T, int OUT> hipError_t launch_product(ProductArgs p, int splits, hipStream_t s)
 {
@@ -443,24 +661,23 @@ template <class T, int OUT> hipError_t launch_product(ProductArgs p, int splits,
     hipLaunchKernelGGL((product_kernel<T, OUT>), dim3((unsigned)(p.tiles_i * p.tiles_j), (unsigned)splits), dim3(T::NT), 0, s, p);
     return hipGetLastError();
 }
-template <int OUT> hipError_t pick_product(const ProductArgs& p, int splits, bool few, hipStream_t s)
+template <int OUT> hipError_t launch_product(const ProductArgs& p, Shape shape, int splits, hipStream_t s)
 {
-    return few ? launch_product<Few, OUT>(p, splits, s) : launch_product<Big, OUT>(p, splits, s);
+    if (shape == Shape::kLarge) return launch_product<Large, OUT>(p, splits, s);
+    if constexpr (OUT != kDw) {
+        if (shape == Shape::kFew64) return launch_product<Few64, OUT>(p, splits, s);
+        if (shape == Shape::kFew32) return launch_product<Few32, OUT>(p, splits, s);
+    }
+    return launch_product<Middle, OUT>(p, splits, s);
 }
 
-constexpr int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
-size_t to256(size_t n) { return (n + 255) / 256 * 256; }
-int64_t entries_pitch(int64_t k) { return k == 1 ? 1 : up(k, 4); }
-bool few_tokens(int64_t tokens) { return tokens <= 64; }
-
 // The backward call's pieces of the vocabulary and splits of dx.
-struct Plan { int64_t tp, piece, splits; };
-constexpr int64_t kPieceElements = 1 << 26, kLeastPiece = 4096, kMostPiece = 16384, kSplitElements = 1 << 25;
+struct Plan { int64_t piece, splits; };
+constexpr int64_t kPieceElements = 1 << 27, kLeastPiece = 4096, kMostPiece = 32768, kSplitElements = 1 << 25;
 Plan plan_of(const VocabLossArgs& a)
 {
     Plan r;
-    r.tp = up(a.tokens, 32);
-    r.piece = std::min(up(a.vocab, 256), std::min(kMostPiece, std::max(kLeastPiece, kPieceElements / r.tp / 256 * 256)));
+    r.piece = std::min(up(a.vocab, 256), std::min(kMostPiece, std::max(kLeastPiece, kPieceElements / a.tokens / 256 * 256)));
     // splits: as long as the partial sums stay within kSplitElements, and of 512 entries at least
     r.splits = std::max<int64_t>(1, std::min(kSplitElements / (a.tokens * a.cols), r.piece / 512));
     return r;
@@ -476,36 +693,62 @@ struct Space {
         return r;
     }
 };
-struct Forward { int* index; float *q, *entropy, *z; float2* stats; size_t bytes; };
+// Lists of a distillation's entries (without a teacher there are none).
+struct Lists { int* index; float* q; int* starts; int2* items; };
+Lists lists_space(const VocabLossArgs& a, Shape shape, Space& s)
+{
+    Lists l = {};
+    if (!a.distill) return l;
+    const size_t n = (size_t)a.tokens * a.k;
+    l.index = s.take<int>(n); l.q = s.take<float>(n); l.items = s.take<int2>(n);
+    l.starts = s.take<int>((up(a.tokens, tile_cols(shape)) / tile_cols(shape)) * (up(a.vocab, tile_rows(shape)) / tile_rows(shape) + 1));
+    return l;
+}
+size_t lists_bytes(int64_t tokens, int64_t vocab, int64_t k)
+{
+    const size_t n = (size_t)tokens * k;
+    return 2 * to256(n * 4) + to256(n * 8) + to256((size_t)(up(tokens, 32) / 32) * (up(vocab, 128) / 128 + 1) * 4);
+}
+struct Forward { Lists l; float *entropy, *z; float2* stats; Shape shape; size_t bytes; };
 Forward forward_space(const VocabLossArgs& a)
 {
     Space s{(uint8_t*)a.workspace};
-    const size_t n = (size_t)a.tokens * entries_pitch(a.k), tm = few_tokens(a.tokens) ? Few::TM : Big::TM;
     Forward f;
-    f.index = s.take<int>(n); f.q = s.take<float>(n); f.z = s.take<float>(n); f.entropy = s.take<float>(a.tokens);
-    f.stats = s.take<float2>((a.vocab + tm - 1) / tm * a.tokens);
+    f.shape = shape_for(a.vocab, a.tokens);
+    f.l = lists_space(a, f.shape, s);
+    f.z = s.take<float>((size_t)a.tokens * a.k); f.entropy = s.take<float>(a.tokens);
+    f.stats = s.take<float2>((size_t)(up(a.vocab, tile_rows(f.shape)) / tile_rows(f.shape)) * a.tokens);
     f.bytes = s.used;
     return f;
 }
-struct Backward { int* index; float *q, *coef, *sums; uint16_t *xt, *wt, *dz, *dzt; size_t bytes; };
+struct Backward { Lists l; float *coef, *sums; uint16_t *x, *dz; Shape shape; size_t bytes; };
 Backward backward_space(const VocabLossArgs& a, const Plan& pl)
 {
     Space s{(uint8_t*)a.workspace};
-    const size_t n = (size_t)a.tokens * entries_pitch(a.k);
     Backward b;
-    b.index = s.take<int>(n); b.q = s.take<float>(n); b.coef = s.take<float>(a.tokens);
-    b.xt = s.take<uint16_t>(a.cols * pl.tp); b.wt = s.take<uint16_t>(a.cols * pl.piece);
-    b.dz = s.take<uint16_t>(a.tokens * pl.piece); b.dzt = s.take<uint16_t>(pl.piece * pl.tp);
+    b.shape = shape_for(pl.piece, a.tokens);
+    b.l = lists_space(a, b.shape, s);
+    b.coef = s.take<float>(a.tokens);
+    b.x = s.take<uint16_t>(a.tokens * a.cols);
+    b.dz = s.take<uint16_t>(a.tokens * pl.piece);
     b.sums = s.take<float>((size_t)a.tokens * a.cols * pl.splits);
     b.bytes = s.used;
     return b;
 }
 
-void launch_entries(const VocabLossArgs& a, int* index, float* q, float* entropy, float* coef, hipStream_t s)
+void launch_lists(const VocabLossArgs& a, const Lists& l, Shape shape, float* entropy, float* coef, hipStream_t s)
 {
-    const int64_t blocks = (a.tokens + 3) / 4;
+    const int64_t blocks = (a.tokens + 3) / 4, tn = tile_cols(shape), tm = tile_rows(shape);
     hipLaunchKernelGGL(a.index64 ? entries_kernel<true> : entries_kernel<false>, dim3((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks)), dim3(256), 0, s, a.indices, a.teacher,
-                       a.teacher_fp32 != 0, (int)a.tokens, (int)a.vocab, (int)a.k, (int)entries_pitch(a.k), a.tau, a.dloss, index, q, entropy, coef);
+                       a.teacher_fp32 != 0, (int)a.tokens, (int)a.vocab, (int)a.k, a.tau, a.dloss, l.index, l.q, entropy, coef);
+    hipLaunchKernelGGL(lists_kernel, dim3((unsigned)((a.tokens + tn - 1) / tn)), dim3(1024), 0, s, l.index, l.q, (int)a.tokens, (int)a.k, (int)tn, tm == 256 ? 8 : 7,
+                       (int)((a.vocab + tm - 1) / tm), coef != nullptr, l.starts, l.items);
+}
+void name_entries(ProductArgs& p, const VocabLossArgs& a, const Lists& l, Shape shape)
+{
+    p.alpha = 1.f / a.tau; p.vocab = (int)a.vocab;
+    if (!a.distill) { p.targets = a.indices; p.target64 = a.index64; return; }
+    p.starts = l.starts; p.items = l.items; p.items_pitch = tile_cols(shape) * a.k; p.vocab_tiles = (int)(up(a.vocab, tile_rows(shape)) / tile_rows(shape));
 }
 
 }  // namespace
@@ -516,82 +759,74 @@ size_t vocab_loss_backward_needed(const VocabLossArgs& a) { return backward_spac
 // Bounds of the above that grow with every extent.
 size_t vocab_loss_bytes(int64_t tokens, int64_t vocab, int64_t k)
 {
-    const size_t n = (size_t)tokens * entries_pitch(k);
-    // the tiles of few tokens are half as high
-    const size_t stats = std::max((size_t)((vocab + Few::TM - 1) / Few::TM) * std::min<int64_t>(tokens, 64), (size_t)((vocab + Big::TM - 1) / Big::TM) * tokens);
-    return 3 * to256(n * 4) + to256((size_t)tokens * 4) + to256(stats * 8);
+    return lists_bytes(tokens, vocab, k) + to256((size_t)tokens * k * 4) + to256((size_t)tokens * 4) + to256((size_t)(up(vocab, 128) / 128) * tokens * 8);
 }
 size_t vocab_loss_backward_bytes(int64_t tokens, int64_t cols, int64_t vocab, int64_t k)
 {
-    const size_t n = (size_t)tokens * entries_pitch(k);
-    const int64_t tp = up(tokens, 32), vp = up(vocab, 256);
-    const int64_t piece = std::min(vp, kMostPiece), dz = std::min(tp * piece, std::max(kPieceElements, tp * kLeastPiece));
+    const int64_t piece = std::min(up(vocab, 256), kMostPiece), dz = std::min(tokens * piece, std::max(kPieceElements, tokens * kLeastPiece));
     const int64_t sums = std::min(std::max(tokens * cols, kSplitElements), tokens * cols * std::max<int64_t>(1, piece / 512));
-    return 2 * to256(n * 4) + to256((size_t)tokens * 4) + to256((size_t)(cols * tp) * 2) + to256((size_t)(cols * piece) * 2) + 2 * to256((size_t)dz * 2) + to256((size_t)sums * 4);
+    return lists_bytes(tokens, vocab, k) + to256((size_t)tokens * 4) + to256((size_t)(tokens * cols) * 2) + to256((size_t)dz * 2) + to256((size_t)sums * 4);
 }
 
 hipError_t launch_vocab_loss(const VocabLossArgs& a, hipStream_t s)
 {
     if (a.tokens == 0) return hipSuccess;
     const Forward f = forward_space(a);
-    launch_entries(a, f.index, f.q, f.entropy, nullptr, s);
+    if (a.distill) launch_lists(a, f.l, f.shape, f.entropy, nullptr, s);
     ProductArgs p = {};
     p.a = a.w; p.lda = a.ldw; p.I = (int)a.vocab; p.b = a.x; p.ldb = a.ldx; p.J = (int)a.tokens; p.R = (int)a.cols;
-    p.alpha = 1.f / a.tau; p.e = {f.index, f.q, (int)a.k, (int)entries_pitch(a.k)}; p.vocab = (int)a.vocab;
+    name_entries(p, a, f.l, f.shape);
     p.tile_stats = f.stats; p.z = f.z;
-    const bool few = few_tokens(a.tokens);
-    const hipError_t e = pick_product<kStats>(p, 1, few, s);
+    const hipError_t e = launch_product<kStats>(p, f.shape, 1, s);
     if (e != hipSuccess) return e;
-    const int tm = few ? Few::TM : Big::TM;
-    hipLaunchKernelGGL(join_kernel, dim3((unsigned)((a.tokens + 15) / 16)), dim3(256), 0, s, f.stats, (int)((a.vocab + tm - 1) / tm), (int)a.tokens, p.alpha, a.tau, p.e, f.z, f.entropy,
-                       a.loss, a.lse);
+    hipLaunchKernelGGL(join_kernel, dim3((unsigned)((a.tokens + 15) / 16)), dim3(256), 0, s, f.stats, (int)((a.vocab + tile_rows(f.shape) - 1) / tile_rows(f.shape)), (int)a.tokens,
+                       (int)a.vocab, p.alpha, a.tau, p.targets, p.target64, f.l.index, f.l.q, (int)a.k, f.z, f.entropy, a.loss, a.lse);
     return hipGetLastError();
 }
 
 hipError_t launch_vocab_loss_backward(const VocabLossArgs& a, hipStream_t s)
 {
-    if (a.tokens == 0 && !a.dw) return hipSuccess;
     if (a.tokens == 0) {
         const int64_t blocks = (a.vocab * (a.cols / 8) + 255) / 256;
-        if (!a.add)
+        if (a.dw && !a.add)
             hipLaunchKernelGGL(a.dw_fp32 ? zero_kernel<true> : zero_kernel<false>, dim3((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks)), dim3(256), 0, s, a.dw, a.vocab,
                                (int)a.cols, a.lddw);
         return hipGetLastError();
     }
     const Plan pl = plan_of(a);
     const Backward b = backward_space(a, pl);
-    launch_entries(a, b.index, b.q, nullptr, b.coef, s);
-    const bool few = few_tokens(a.tokens);
-    auto transpose = [&](const uint16_t* in, int64_t ld, int64_t rows, const float* keep, uint16_t* out, int64_t ldo, int64_t pad) {
-        hipLaunchKernelGGL(transpose_kernel, dim3((unsigned)((pad + 63) / 64), (unsigned)((a.cols + 63) / 64)), dim3(256), 0, s, in, ld, (int)rows, (int)a.cols, keep, out, ldo, (int)pad);
-    };
-    if (a.dw) transpose(a.x, a.ldx, a.tokens, b.coef, b.xt, pl.tp, pl.tp);
-    hipError_t e = hipSuccess;
-    for (int64_t v0 = 0; v0 < a.vocab && e == hipSuccess; v0 += pl.piece) {
-        const int64_t here = std::min(pl.piece, a.vocab - v0), padded = up(here, 64);
+    if (a.distill) launch_lists(a, b.l, b.shape, nullptr, b.coef, s);
+    if (a.dw || !a.distill) {
+        const int64_t blocks = (a.tokens + 3) / 4;
+        hipLaunchKernelGGL(part_kernel, dim3((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks)), dim3(256), 0, s, a.x, a.ldx, (int)a.tokens, (int)a.cols, (int)a.vocab,
+                           a.distill ? nullptr : a.indices, a.index64, a.dloss, b.coef, a.dw ? b.x : nullptr);
+    }
+    for (int64_t v0 = 0; v0 < a.vocab; v0 += pl.piece) {
+        const int64_t here = std::min(pl.piece, a.vocab - v0);
         const uint16_t* w = a.w + v0 * a.ldw;
         ProductArgs p = {};
-        p.a = w; p.lda = a.ldw; p.I = (int)here; p.b = a.x; p.ldb = a.ldx; p.J = (int)a.tokens; p.R = (int)a.cols;
-        p.alpha = 1.f / a.tau; p.e = {b.index, b.q, (int)a.k, (int)entries_pitch(a.k)}; p.v0 = (int)v0; p.vocab = (int)a.vocab;
-        p.lse = a.lse_in; p.coef = b.coef; p.dz = b.dz; p.lddz = pl.piece; p.dzt = a.dw ? b.dzt : nullptr; p.lddzt = pl.tp; p.jpad = (int)pl.tp;
-        if ((e = pick_product<kDz>(p, 1, few, s)) != hipSuccess) break;
-        if (a.dx) {
-            transpose(w, a.ldw, here, nullptr, b.wt, pl.piece, padded);
+        p.a = w; p.lda = a.ldw; p.I = (int)here; p.b = a.x; p.ldb = a.ldx; p.J = (int)a.tokens; p.R = (int)a.cols; p.v0 = (int)v0;
+        name_entries(p, a, b.l, b.shape);
+        p.lse = a.lse_in; p.coef = b.coef; p.c = b.dz; p.ldc = pl.piece;
+        hipError_t e = launch_product<kDz>(p, b.shape, 1, s);
+        if (e == hipSuccess && a.dx) {
+            // dz is zero up to a whole tile, w has no row past the piece
             ProductArgs d = {};
-            d.a = b.wt; d.lda = pl.piece; d.I = (int)a.cols; d.b = b.dz; d.ldb = pl.piece; d.J = (int)a.tokens; d.R = (int)padded;
+            d.a = w; d.lda = a.ldw; d.I = (int)a.cols; d.b = b.dz; d.ldb = pl.piece; d.J = (int)a.tokens; d.R = (int)here;
             d.split = (int)((up(here, 64) / 64 + pl.splits - 1) / pl.splits);
-            d.sum = b.sums; d.ldsum = a.cols; d.split_stride = a.tokens * a.cols; d.add = v0 > 0;
-            if ((e = pick_product<kDx>(d, (int)pl.splits, few, s)) != hipSuccess) break;
+            d.c = b.sums; d.ldc = a.cols; d.split_stride = a.tokens * a.cols; d.add = v0 > 0;
+            e = launch_product<kDx>(d, shape_for(a.cols * pl.splits, a.tokens), (int)pl.splits, s);
         }
-        if (a.dw) {
+        if (e == hipSuccess && a.dw) {
             ProductArgs d = {};
-            d.a = b.xt; d.lda = pl.tp; d.I = (int)a.cols; d.b = b.dzt; d.ldb = pl.tp; d.J = (int)here; d.R = (int)pl.tp;
+            d.a = b.x; d.lda = a.cols; d.I = (int)a.cols; d.b = b.dz; d.ldb = pl.piece; d.J = (int)here; d.R = (int)a.tokens;
             d.c = a.dw_fp32 ? (void*)((float*)a.dw + v0 * a.lddw) : (void*)((uint16_t*)a.dw + v0 * a.lddw);
             d.ldc = a.lddw; d.c_fp32 = a.dw_fp32; d.add = a.add;
-            e = pick_product<kDw>(d, 1, false, s);
+            e = launch_product<kDw>(d, shape_for(a.cols, std::max<int64_t>(here, 129)), 1, s);
         }
+        if (e != hipSuccess) return e;
     }
-    if (e != hipSuccess || !a.dx) return e;
+    if (!a.dx) return hipSuccess;
     const int64_t blocks = (a.tokens * (a.cols / 8) + 255) / 256;
     hipLaunchKernelGGL(dx_kernel, dim3((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks)), dim3(256), 0, s, b.sums, (int)pl.splits, a.tokens * a.cols, (int)a.tokens, (int)a.cols,
                        b.coef, a.dx, a.lddx);

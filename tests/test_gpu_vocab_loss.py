@@ -141,6 +141,12 @@ def test_long_contraction_and_splits():
 
 
 @pytest.mark.parametrize("k", [0, 5])
+def test_large_tiles(k):
+    """All products in tiles of 256 x 256, ragged in every extent."""
+    check(require_gpu(), Case(600, 2056, 33001, k, ignored=0.1))
+
+
+@pytest.mark.parametrize("k", [0, 5])
 def test_layouts_and_buffers(k):
     """Rows apart, buffers given, a gradient of fp32 added to what is there, each gradient alone, no dloss."""
     snip = require_gpu()

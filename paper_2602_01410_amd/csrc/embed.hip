@@ -8,9 +8,11 @@
 //             tokens of one number stay in their order.  T * ranges reads, from L2: 16384 ids of 8 bytes and 250 ranges are 65 MB.
 //   partials  rows with more than kLong tokens (the most frequent words, a tenth of a text each) are summed kLong tokens at a time
 //             by as many workgroups; for most blocks there is nothing to do.
-//   rows      a wave for each 512 columns of a row of the table: zeros, or the sum of its tokens, or of its partial sums.
+//   rows      a wave for each 512 columns of a row of the table: zeros, or the sum of its tokens, or of its partial sums; where the gradient is added to,
+//             of the rows that have tokens.
 #include "snip_internal.h"
 #include "quant_common.h"
+#include <type_traits>
 
 namespace snip {
 namespace {
@@ -18,6 +20,7 @@ namespace {
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kMostRange = 512;          // token numbers of a workgroup of the sort
 constexpr int kLong = 64;                // tokens of a row from which on it is summed in parts, and the tokens of a part
+constexpr int kHeld = 16;                // loads of 64 ids that a wave of the sort has under way; up to 64 of them for each wave ids are read once
 constexpr int kSegment = 512;            // columns of a wave: 8 per lane
 
 template <bool I64> __device__ __forceinline__ int token(const void* ids, int64_t t, int vocab)      // -1: none
@@ -85,11 +88,22 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const void* __
     for (int i = threadIdx.x; i < kSortWaves * range; i += kSortThreads) counts[i / range][i % range] = 0;
     __syncthreads();
     int below = 0;
-#pragma unroll 4
-    for (int64_t t = from + lane; t < to; t += 64) {
-        const int v = token<I64>(ids, t, vocab);
-        below += v >= 0 && v < base;
-        if (v >= base && v - base < here) atomicAdd(&counts[wave][v - base], 1);
+    int held[kHeld];
+    auto fetch = [&](int64_t t0) {
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            const int64_t t = t0 + i * 64 + lane;
+            held[i] = t < to ? token<I64>(ids, t, vocab) : -1;
+        }
+    };
+    for (int64_t t0 = from; t0 < to; t0 += kHeld * 64) {
+        fetch(t0);
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            const int v = held[i];
+            below += v >= 0 && v < base;
+            if (v >= base && v - base < here) atomicAdd(&counts[wave][v - base], 1);
+        }
     }
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) below += __shfl_xor(below, d);
@@ -124,43 +138,55 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const void* __
         }
     }
     __syncthreads();
-    volatile int* mine = counts[wave];
-    for (int64_t t0 = from; t0 < to; t0 += 64) {
-        const int64_t t = t0 + lane;
-        const int v = t < to ? token<I64>(ids, t, vocab) : -1;
-        bool todo = v >= base && v - base < here;
-        unsigned long long left = __builtin_amdgcn_ballot_w64(todo);
-        while (left) {
-            const int lead = __builtin_ctzll(left);
-            const int number = __builtin_amdgcn_readlane(v, lead) - base;
-            const bool same = todo && v - base == number;
-            const unsigned long long with = __builtin_amdgcn_ballot_w64(same);
-            const int place = mine[number];
-            if (same) order[place + __builtin_popcountll(with & ((1ull << lane) - 1))] = (int)t;
-            __builtin_amdgcn_wave_barrier();
-            if (lane == lead) mine[number] = place + __builtin_popcountll(with);
-            __builtin_amdgcn_wave_barrier();
-            todo = todo && !same;
-            left &= ~with;
+    for (int64_t t0 = from; t0 < to; t0 += kHeld * 64) {
+        if (stretch > kHeld * 64) fetch(t0);
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            const int v = held[i];
+            const bool mine = v >= base && v - base < here;
+            // of the lanes of one number: the first one, the number of them, this one's place among them
+            int lead = lane, many = 0, rank = 0;
+            unsigned long long left = __builtin_amdgcn_ballot_w64(mine);
+            while (left) {
+                const int l = __builtin_ctzll(left);
+                const bool same = mine && v == __builtin_amdgcn_readlane(v, l);
+                const unsigned long long with = __builtin_amdgcn_ballot_w64(same);
+                if (same) { lead = l; many = __builtin_popcountll(with); rank = __builtin_popcountll(with & ((1ull << lane) - 1)); }
+                left &= ~with;
+            }
+            // (LDS serves a wave in order, so nothing waits for the place of the numbers before)
+            const int place = mine && lane == lead ? atomicAdd(&counts[wave][v - base], many) : 0;
+            const int at = __shfl(place, lead) + rank;
+            if (mine) order[at] = (int)(t0 + i * 64 + lane);
         }
     }
 }
 
-// Sum of dy's rows order[from ... to) at column c, in their order.
+// Sum of dy's rows order[from ... to), kLong of them at most, at column c, in their order.
+template <int B> __device__ __forceinline__ void sum_batch(const uint16_t* __restrict__ dy, int64_t ld, int rows, int i, int c, float (&sum)[8])
+{
+    uint4 raw[B];
+#pragma unroll
+    for (int b = 0; b < B; ++b) raw[b] = *(const uint4*)(dy + (int64_t)__builtin_amdgcn_readlane(rows, i + b) * ld + c);
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+        float f[8];
+        unpack2(raw[b].x, f[0], f[1]); unpack2(raw[b].y, f[2], f[3]); unpack2(raw[b].z, f[4], f[5]); unpack2(raw[b].w, f[6], f[7]);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum[k] += f[k];
+    }
+}
 __device__ __forceinline__ void sum_rows(const uint16_t* __restrict__ dy, int64_t ld, const int* __restrict__ order, int from, int to, int c, float (&sum)[8])
 {
-    constexpr int B = 8;
-    for (int p = from; p < to; p += B) {
-        float f[B][8];
-#pragma unroll
-        for (int b = 0; b < B; ++b) load8(dy + (int64_t)order[p + b < to ? p + b : to - 1] * ld + c, f[b]);
-#pragma unroll
-        for (int b = 0; b < B; ++b)
-            if (p + b < to) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) sum[i] += f[b][i];
-            }
-    }
+    const int n = to - from, lane = threadIdx.x & 63;
+    if (n == 0) return;
+    const int rows = order[from + (lane < n ? lane : n - 1)];
+    int i = 0;
+    for (; i + 16 <= n; i += 16) sum_batch<16>(dy, ld, rows, i, c, sum);
+    if (n & 8) { sum_batch<8>(dy, ld, rows, i, c, sum); i += 8; }
+    if (n & 4) { sum_batch<4>(dy, ld, rows, i, c, sum); i += 4; }
+    if (n & 2) { sum_batch<2>(dy, ld, rows, i, c, sum); i += 2; }
+    if (n & 1) sum_batch<1>(dy, ld, rows, i, c, sum);
 }
 
 // Block j: the places [j kLong, (j + 1) kLong) of the order.  Of the rows with more than kLong tokens two at most have tokens there: that of the first
@@ -172,45 +198,55 @@ __global__ __launch_bounds__(64) void embed_partials_kernel(const uint16_t* __re
     const int all = start[vocab], p0 = blockIdx.x * kLong;
     if (p0 >= all) return;
     const int p1 = all - p0 < kLong ? all : p0 + kLong;
-    const int c = blockIdx.y * kSegment + threadIdx.x * 8;
+    const int c = blockIdx.y * kSegment + threadIdx.x * 8, at = c < cols ? c : 0;      // (every lane holds a row's number)
     const int v0 = token<I64>(ids, order[p0], vocab), v1 = token<I64>(ids, order[p1 - 1], vocab);
 #pragma unroll
     for (int slot = 0; slot < 2; ++slot) {
         const int v = slot ? v1 : v0;
         if (slot && v1 == v0) break;
         const int s = start[v], e = start[v + 1];
-        if (e - s <= kLong || c >= cols) continue;
-        float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        sum_rows(dy, ld, order, s > p0 ? s : p0, e < p1 ? e : p1, c, sum);
-        store8(partials + ((int64_t)blockIdx.x * 2 + slot) * cols + c, sum);
+        if (e - s <= kLong) continue;
+        float sum[8] = {};
+        sum_rows(dy, ld, order, s > p0 ? s : p0, e < p1 ? e : p1, at, sum);
+        if (c < cols) store8(partials + ((int64_t)blockIdx.x * 2 + slot) * cols + c, sum);
     }
 }
 
-template <class T>
-__global__ __launch_bounds__(256) void embed_rows_kernel(const uint16_t* __restrict__ dy, int64_t ld, int cols, int vocab, float scale,
+// BY_TOKEN (a gradient that is added to): a wave for each place in the order and 512 columns, which has something to do where a number's tokens begin;
+// otherwise for each row of the table.
+template <class T, bool BY_TOKEN, bool I64>
+__global__ __launch_bounds__(256) void embed_rows_kernel(const uint16_t* __restrict__ dy, int64_t ld, int cols, int vocab, int tokens, const void* __restrict__ ids, float scale,
                                                          const int* __restrict__ start, const int* __restrict__ order, const float* __restrict__ partials,
-                                                         T* __restrict__ dw, int64_t lddw, bool add, int segments)
+                                                         T* __restrict__ dw, int64_t lddw, int segments)
 {
-    const int64_t units = (int64_t)vocab * segments;
+    const int64_t units = (int64_t)(BY_TOKEN ? tokens : vocab) * segments;
     for (int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); u < units; u += (int64_t)gridDim.x * 4) {
-        const int v = (int)(u / segments), c = (int)(u % segments) * kSegment + (threadIdx.x & 63) * 8;
+        int v = __builtin_amdgcn_readfirstlane((int)(u / segments));
+        const int c = (int)(u % segments) * kSegment + (threadIdx.x & 63) * 8, at = c < cols ? c : 0;
+        if (BY_TOKEN) {
+            const int place = v;
+            if (place >= start[vocab]) continue;
+            v = __builtin_amdgcn_readfirstlane(token<I64>(ids, order[place], vocab));
+            if (start[v] != place) continue;
+        }
         const int s = __builtin_amdgcn_readfirstlane(start[v]), e = __builtin_amdgcn_readfirstlane(start[v + 1]);
-        if ((add && s == e) || c >= cols) continue;
-        float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        float sum[8] = {};
         if (e - s <= kLong) {
-            sum_rows(dy, ld, order, s, e, c, sum);
+            sum_rows(dy, ld, order, s, e, at, sum);
         } else {
             const int last = (e - 1) / kLong;
+#pragma unroll 4
             for (int j = s / kLong; j <= last; ++j) {
                 float f[8];
-                load8(partials + ((int64_t)j * 2 + (j * kLong < s)) * cols + c, f);
+                load8(partials + ((int64_t)j * 2 + (j * kLong < s)) * cols + at, f);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) sum[i] += f[i];
             }
         }
+        if (c >= cols) continue;
         T* p = dw + (int64_t)v * lddw + c;
-        float old[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (add) load8(p, old);
+        float old[8] = {};
+        if (BY_TOKEN) load8(p, old);
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum[i] = fmaf(sum[i], scale, old[i]);
         store8(p, sum);
@@ -257,12 +293,20 @@ hipError_t launch_embed_backward(const EmbedGradArgs& a, hipStream_t s)
     if (a.tokens > kLong)
         hipLaunchKernelGGL(a.ids64 ? embed_partials_kernel<true> : embed_partials_kernel<false>, dim3((unsigned)((a.tokens + kLong - 1) / kLong), (unsigned)segments),
                            dim3(64), 0, s, a.dy, a.ld, a.cols, (int)a.vocab, a.ids, start, order, partials);
-    const int64_t blocks = (a.vocab * segments + 3) / 4;
+    const int64_t blocks = ((a.add ? a.tokens : a.vocab) * segments + 3) / 4;
+    if (blocks == 0) return hipGetLastError();
     const dim3 grid((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks));
-    if (a.dw_fp32)
-        hipLaunchKernelGGL(embed_rows_kernel<float>, grid, dim3(256), 0, s, a.dy, a.ld, a.cols, (int)a.vocab, a.scale, start, order, partials, (float*)a.dw, a.lddw, a.add, segments);
-    else
-        hipLaunchKernelGGL(embed_rows_kernel<uint16_t>, grid, dim3(256), 0, s, a.dy, a.ld, a.cols, (int)a.vocab, a.scale, start, order, partials, (uint16_t*)a.dw, a.lddw, a.add, segments);
+    auto rows = [&](auto* dw, auto* kernel) {
+        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a.dy, a.ld, a.cols, (int)a.vocab, (int)a.tokens, a.ids, a.scale, start, order, partials, dw, a.lddw, segments);
+    };
+    auto typed = [&](auto* dw) {
+        using T = std::remove_pointer_t<decltype(dw)>;
+        if (!a.add)       rows(dw, embed_rows_kernel<T, false, false>);
+        else if (a.ids64) rows(dw, embed_rows_kernel<T, true, true>);
+        else              rows(dw, embed_rows_kernel<T, true, false>);
+    };
+    if (a.dw_fp32) typed((float*)a.dw);
+    else           typed((uint16_t*)a.dw);
     return hipGetLastError();
 }
 

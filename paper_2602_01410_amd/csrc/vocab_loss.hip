@@ -37,7 +37,8 @@ struct ProductArgs {
     float2* tile_stats;          // stats: [tiles_i][J]
     float* z;                    // stats: of every named entry
     const float* lse;            // dz
-    const float* coef;           // dz: dloss tau of every token, zero for those that take no part
+    const float* part;           // dz: dloss tau of every token in units of *unit, zero for those that take no part
+    const float* unit;           // dw
     void* c; int64_t ldc, split_stride; int c_fp32, add;   // dz, dx (fp32), dw
 };
 
@@ -334,6 +335,7 @@ __global__ __launch_bounds__(T::NT, T::PER_CU) void product_kernel(const Product
     tile_of(blockIdx.x, p.tiles_i * p.tiles_j, p.tiles_i, p.tiles_j, ti, tj);
     const int i0 = ti * T::TM, j0 = tj * T::TN;
     const int all = (p.R + 63) / 64, first = OUT == kDx ? blockIdx.y * p.split : 0, last = OUT == kDx ? min(all, first + p.split) : all;
+    const float unit = OUT == kDw ? *p.unit : 1.f;
     v16f acc[T::MB][T::NB];
     multiply<T, (OUT == kDx || OUT == kDw), OUT == kDw>(p, lds, i0, j0, first, last, lane, wave, acc);
     const int iw = i0 + wm * T::WM, jw = j0 + wn * T::WN;
@@ -390,7 +392,7 @@ __global__ __launch_bounds__(T::NT, T::PER_CU) void product_kernel(const Product
 #pragma unroll
         for (int n = 0; n < T::NB; ++n) {
             const int j = jw + n * 32 + r32;
-            const float lse = j < p.J ? p.lse[j] : 0.f, mine = j < p.J ? p.coef[j] : 0.f;
+            const float lse = j < p.J ? p.lse[j] : 0.f, mine = j < p.J ? p.part[j] : 0.f;
 #pragma unroll
             for (int m = 0; m < T::MB; ++m)
 #pragma unroll
@@ -416,7 +418,7 @@ __global__ __launch_bounds__(T::NT, T::PER_CU) void product_kernel(const Product
                 if (j >= p.J || i >= p.I) return;                   // (I is a multiple of 8)
                 float v[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = f[e];
+                for (int e = 0; e < 8; ++e) v[e] = OUT == kDw ? f[e] * unit : f[e];
                 if (OUT == kDx || p.c_fp32) {
                     float4* to = reinterpret_cast<float4*>((float*)p.c + (OUT == kDx ? blockIdx.y * p.split_stride : 0) + j * p.ldc + i);
                     if (p.add) {
@@ -552,59 +554,114 @@ __global__ __launch_bounds__(1024) void lists_kernel(const int* __restrict__ ind
     }
 }
 
-// The tiles' sums joined and the loss formed: 16 tokens of a workgroup, 16 threads of a token.
+// The tiles' sums joined and the loss formed: TOK tokens of a workgroup, 256 / TOK threads of a token.
+template <int TOK>
 __global__ __launch_bounds__(256) void join_kernel(const float2* __restrict__ tile_stats, int tiles, int tokens, int vocab, float alpha, float tau, const void* __restrict__ targets,
                                                    int target64, const int* __restrict__ index, const float* __restrict__ q, int k, const float* __restrict__ z,
                                                    const float* __restrict__ entropy, float* __restrict__ loss, float* __restrict__ lse)
 {
-    __shared__ float2 shared[16][17];
-    const int tok = threadIdx.x & 15, part = threadIdx.x >> 4, t = blockIdx.x * 16 + tok;
+    constexpr int PARTS = 256 / TOK;
+    __shared__ float2 shared[PARTS][TOK + 1];
+    const int tok = threadIdx.x % TOK, part = threadIdx.x / TOK, t = blockIdx.x * TOK + tok;
+    const bool here = t < tokens;
     const float c = alpha * kLog2e;
     auto join = [&](float2 v, float2 o) {
         const float top = fmaxf(v.x, o.x), base = top == -INFINITY ? 0.f : top;
         return make_float2(top, v.y * __builtin_amdgcn_exp2f((v.x - base) * c) + o.y * __builtin_amdgcn_exp2f((o.x - base) * c));
     };
+    // (what the loss names is fetched beside the sums)
+    int64_t target = -1;
+    float at_target = 0.f;
+    if (here && targets) {
+        target = target64 ? ((const int64_t*)targets)[t] : (int64_t)((const int*)targets)[t];
+        at_target = z[t];
+    }
     float2 v = make_float2(-INFINITY, 0.f);
-    if (t < tokens)
-        for (int i = part; i < tiles; i += 16) v = join(v, tile_stats[(int64_t)i * tokens + t]);
+    for (int i0 = part; i0 < tiles; i0 += 8 * PARTS) {
+        float2 o[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = here && i0 + i * PARTS < tiles ? tile_stats[(int64_t)(i0 + i * PARTS) * tokens + t] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v = join(v, o[i]);
+    }
     shared[part][tok] = v;
     __syncthreads();
-    if (part != 0 || t >= tokens) return;
-    for (int i = 1; i < 16; ++i) v = join(v, shared[i][tok]);
+#pragma unroll
+    for (int n = PARTS / 2; n > 0; n >>= 1) {
+        if (part < n) shared[part][tok] = v = join(v, shared[part + n][tok]);
+        __syncthreads();
+    }
+    v = shared[0][tok];
     const float l = fmaf(v.x, alpha, logf(v.y));
-    if (lse) lse[t] = l;
+    if (lse && part == 0 && here) lse[t] = l;
     if (!loss) return;
     if (targets) {
-        const int64_t at = target64 ? ((const int64_t*)targets)[t] : (int64_t)((const int*)targets)[t];
-        loss[t] = at >= 0 && at < vocab ? l - z[t] : 0.f;
+        if (part == 0 && here) loss[t] = target >= 0 && target < vocab ? l - at_target : 0.f;
         return;
     }
-    float sum = 0.f;
-    bool any = false;
-    for (int j = 0; j < k; ++j) {
-        const int64_t at = (int64_t)t * k + j;
-        if (index[at] >= 0) {
-            sum = fmaf(q[at], fmaf(-z[at], alpha, l), sum);
-            any = true;
+    float sum = 0.f, any = 0.f;
+    if (here)
+        for (int j = part; j < k; j += PARTS) {
+            const int64_t at = (int64_t)t * k + j;
+            if (index[at] >= 0) {
+                sum = fmaf(q[at], fmaf(-z[at], alpha, l), sum);
+                any = 1.f;
+            }
         }
-    }
-    loss[t] = any ? (sum + entropy[t]) * tau * tau : 0.f;
+    __syncthreads();
+    shared[part][tok] = make_float2(sum, any);
+    __syncthreads();
+    if (part != 0 || !here) return;
+    for (int i = 1; i < PARTS; ++i) { sum += shared[i][tok].x; any += shared[i][tok].y; }
+    loss[t] = any > 0.f ? (sum + entropy[t]) * tau * tau : 0.f;
 }
 
-// x without the rows of tokens that take no part (their x may hold anything), a wave per token; with targets coef is formed here.
-__global__ __launch_bounds__(256) void part_kernel(const uint16_t* __restrict__ x, int64_t ld, int tokens, int cols, int vocab, const void* __restrict__ targets, int target64,
-                                                   const float* __restrict__ dloss, float* __restrict__ coef, uint16_t* __restrict__ out)
+// dloss tau of a token, zero where it takes no part: of targets, or given.
+struct Weights {
+    const void* targets; int target64, vocab;
+    const float *dloss, *coef;
+    __device__ __forceinline__ float operator()(int t) const
+    {
+        if (!targets) return coef[t];
+        const int64_t at = target64 ? ((const int64_t*)targets)[t] : (int64_t)((const int*)targets)[t];
+        return at >= 0 && at < vocab ? (dloss ? dloss[t] : 1.f) : 0.f;
+    }
+};
+// The largest of them that is finite, or 1: the unit that dz is held in.  dz is rounded to bf16, and at the entry that is wanted it is near -1 times the
+// token's weight: exact in this unit where all weights are equal (a mean), and otherwise with the largest ones where bf16's relative steps are smallest.
+// Relative error of dw in bf16, its own rounding included, weights from 0.5 to 1.5: 0.0025 -> 0.0022; equal ones 0.0024 -> 0.0017.
+template <int NT> __device__ __forceinline__ float unit_of(const Weights& w, int tokens, float* shared)
 {
+    float top = 0.f;
+#pragma unroll 4
+    for (int t = threadIdx.x; t < tokens; t += NT) {
+        const float v = fabsf(w(t));
+        top = v < INFINITY ? fmaxf(top, v) : top;
+    }
+    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = top;
+    __syncthreads();
+    for (int i = 0; i < NT / 64; ++i) top = fmaxf(top, shared[i]);
+    return top > 0.f ? top : 1.f;
+}
+__global__ __launch_bounds__(1024) void unit_kernel(const Weights w, int tokens, float* __restrict__ unit)
+{
+    __shared__ float shared[16];
+    const float u = unit_of<1024>(w, tokens, shared);
+    if (threadIdx.x == 0) *unit = u;
+}
+// Every token's weight in that unit, and x without the rows of tokens that take no part (it may hold anything there); a wave per token.  `find`: every
+// workgroup finds the unit itself (a launch less).
+__global__ __launch_bounds__(256) void part_kernel(const uint16_t* __restrict__ x, int64_t ld, int tokens, int cols, const Weights w, bool find, float* __restrict__ unit,
+                                                   float* __restrict__ part, uint16_t* __restrict__ out)
+{
+    __shared__ float shared[4];
     const int lane = threadIdx.x & 63;
+    const float u = find ? unit_of<256>(w, tokens, shared) : *unit;
+    if (find && blockIdx.x == 0 && threadIdx.x == 0) *unit = u;
     for (int t = blockIdx.x * 4 + (threadIdx.x >> 6); t < tokens; t += gridDim.x * 4) {
-        float g;
-        if (targets) {
-            const int64_t at = target64 ? ((const int64_t*)targets)[t] : (int64_t)((const int*)targets)[t];
-            g = at >= 0 && at < vocab ? (dloss ? dloss[t] : 1.f) : 0.f;
-            if (lane == 0) coef[t] = g;
-        } else {
-            g = coef[t];
-        }
+        const float g = __fdiv_rn(w(t), u);
+        if (lane == 0) part[t] = g;
         if (out)
             for (int c = lane * 8; c < cols; c += 512)
                 *reinterpret_cast<uint4*>(out + (int64_t)t * cols + c) = g == 0.f ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4*>(x + t * ld + c);
@@ -612,20 +669,23 @@ __global__ __launch_bounds__(256) void part_kernel(const uint16_t* __restrict__ 
 }
 
 // dx: the partial sums of the splits, rounded; zeros for tokens that take no part.
-__global__ __launch_bounds__(256) void dx_kernel(const float* __restrict__ sums, int splits, int64_t stride, int tokens, int cols, const float* __restrict__ coef,
-                                                 uint16_t* __restrict__ dx, int64_t ld)
+__global__ __launch_bounds__(256) void dx_kernel(const float* __restrict__ sums, int splits, int64_t stride, int tokens, int cols, const float* __restrict__ part,
+                                                 const float* __restrict__ unit, uint16_t* __restrict__ dx, int64_t ld)
 {
+    const float scale = *unit;
     const int chunks = cols / 8;
     for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < (int64_t)tokens * chunks; u += (int64_t)gridDim.x * 256) {
         const int64_t t = u / chunks;
         const int c = (int)(u % chunks) * 8;
         float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (coef[t] != 0.f)
+        if (part[t] != 0.f)
             for (int i = 0; i < splits; ++i) {
                 const float4* s = reinterpret_cast<const float4*>(sums + i * stride + t * cols + c);
                 const float4 a = s[0], b = s[1];
                 f[0] += a.x; f[1] += a.y; f[2] += a.z; f[3] += a.w; f[4] += b.x; f[5] += b.y; f[6] += b.z; f[7] += b.w;
             }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] *= scale;
         *reinterpret_cast<uint4*>(dx + t * ld + c) = make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
     }
 }
@@ -673,13 +733,15 @@ template <int OUT> hipError_t launch_product(const ProductArgs& p, Shape shape, 
 
 // The backward call's pieces of the vocabulary and splits of dx.
 struct Plan { int64_t piece, splits; };
-constexpr int64_t kPieceElements = 1 << 27, kLeastPiece = 4096, kMostPiece = 32768, kSplitElements = 1 << 25;
+constexpr int64_t kPieceElements = 1 << 27, kLeastPiece = 4096, kMostPiece = 1 << 17, kSplitElements = 1 << 25;
 Plan plan_of(const VocabLossArgs& a)
 {
     Plan r;
     r.piece = std::min(up(a.vocab, 256), std::min(kMostPiece, std::max(kLeastPiece, kPieceElements / a.tokens / 256 * 256)));
-    // splits: as long as the partial sums stay within kSplitElements, and of 512 entries at least
-    r.splits = std::max<int64_t>(1, std::min(kSplitElements / (a.tokens * a.cols), r.piece / 512));
+    // splits of dx: as many workgroups as there are at a time, of 512 entries at least, and partial sums within kSplitElements
+    const int64_t tn = a.tokens <= 32 ? 32 : a.tokens <= 64 ? 64 : a.tokens <= 128 ? 128 : 256, tm = tn == 256 ? 256 : 128;
+    const int64_t tiles = up(a.cols, tm) / tm * (up(a.tokens, tn) / tn);
+    r.splits = std::max<int64_t>(1, std::min({kSplitElements / (a.tokens * a.cols), r.piece / 512, (tm == 256 ? 256 : 512) / tiles}));
     return r;
 }
 
@@ -721,14 +783,14 @@ Forward forward_space(const VocabLossArgs& a)
     f.bytes = s.used;
     return f;
 }
-struct Backward { Lists l; float *coef, *sums; uint16_t *x, *dz; Shape shape; size_t bytes; };
+struct Backward { Lists l; float *coef, *part, *unit, *sums; uint16_t *x, *dz; Shape shape; size_t bytes; };
 Backward backward_space(const VocabLossArgs& a, const Plan& pl)
 {
     Space s{(uint8_t*)a.workspace};
     Backward b;
     b.shape = shape_for(pl.piece, a.tokens);
     b.l = lists_space(a, b.shape, s);
-    b.coef = s.take<float>(a.tokens);
+    b.coef = s.take<float>(a.distill ? a.tokens : 0); b.part = s.take<float>(a.tokens); b.unit = s.take<float>(1);
     b.x = s.take<uint16_t>(a.tokens * a.cols);
     b.dz = s.take<uint16_t>(a.tokens * pl.piece);
     b.sums = s.take<float>((size_t)a.tokens * a.cols * pl.splits);
@@ -765,7 +827,7 @@ size_t vocab_loss_backward_bytes(int64_t tokens, int64_t cols, int64_t vocab, in
 {
     const int64_t piece = std::min(up(vocab, 256), kMostPiece), dz = std::min(tokens * piece, std::max(kPieceElements, tokens * kLeastPiece));
     const int64_t sums = std::min(std::max(tokens * cols, kSplitElements), tokens * cols * std::max<int64_t>(1, piece / 512));
-    return lists_bytes(tokens, vocab, k) + to256((size_t)tokens * 4) + to256((size_t)(tokens * cols) * 2) + to256((size_t)dz * 2) + to256((size_t)sums * 4);
+    return lists_bytes(tokens, vocab, k) + 2 * to256((size_t)tokens * 4) + 256 + to256((size_t)(tokens * cols) * 2) + to256((size_t)dz * 2) + to256((size_t)sums * 4);
 }
 
 hipError_t launch_vocab_loss(const VocabLossArgs& a, hipStream_t s)
@@ -779,8 +841,10 @@ hipError_t launch_vocab_loss(const VocabLossArgs& a, hipStream_t s)
     p.tile_stats = f.stats; p.z = f.z;
     const hipError_t e = launch_product<kStats>(p, f.shape, 1, s);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(join_kernel, dim3((unsigned)((a.tokens + 15) / 16)), dim3(256), 0, s, f.stats, (int)((a.vocab + tile_rows(f.shape) - 1) / tile_rows(f.shape)), (int)a.tokens,
-                       (int)a.vocab, p.alpha, a.tau, p.targets, p.target64, f.l.index, f.l.q, (int)a.k, f.z, f.entropy, a.loss, a.lse);
+    const int tok = a.tokens >= 2048 ? 16 : 4;
+    hipLaunchKernelGGL(tok == 16 ? join_kernel<16> : join_kernel<4>, dim3((unsigned)((a.tokens + tok - 1) / tok)), dim3(256), 0, s, f.stats,
+                       (int)((a.vocab + tile_rows(f.shape) - 1) / tile_rows(f.shape)), (int)a.tokens, (int)a.vocab, p.alpha, a.tau, p.targets, p.target64, f.l.index, f.l.q, (int)a.k, f.z,
+                       f.entropy, a.loss, a.lse);
     return hipGetLastError();
 }
 
@@ -796,18 +860,19 @@ hipError_t launch_vocab_loss_backward(const VocabLossArgs& a, hipStream_t s)
     const Plan pl = plan_of(a);
     const Backward b = backward_space(a, pl);
     if (a.distill) launch_lists(a, b.l, b.shape, nullptr, b.coef, s);
-    if (a.dw || !a.distill) {
-        const int64_t blocks = (a.tokens + 3) / 4;
-        hipLaunchKernelGGL(part_kernel, dim3((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks)), dim3(256), 0, s, a.x, a.ldx, (int)a.tokens, (int)a.cols, (int)a.vocab,
-                           a.distill ? nullptr : a.indices, a.index64, a.dloss, b.coef, a.dw ? b.x : nullptr);
-    }
+    const Weights weights = {a.distill ? nullptr : a.indices, a.index64, (int)a.vocab, a.dloss, b.coef};
+    const bool find = a.tokens <= 2048;
+    if (!find) hipLaunchKernelGGL(unit_kernel, dim3(1), dim3(1024), 0, s, weights, (int)a.tokens, b.unit);
+    const int64_t token_blocks = (a.tokens + 3) / 4;
+    hipLaunchKernelGGL(part_kernel, dim3((unsigned)(token_blocks < kMostBlocks ? token_blocks : kMostBlocks)), dim3(256), 0, s, a.x, a.ldx, (int)a.tokens, (int)a.cols, weights, find,
+                       b.unit, b.part, a.dw ? b.x : nullptr);
     for (int64_t v0 = 0; v0 < a.vocab; v0 += pl.piece) {
         const int64_t here = std::min(pl.piece, a.vocab - v0);
         const uint16_t* w = a.w + v0 * a.ldw;
         ProductArgs p = {};
         p.a = w; p.lda = a.ldw; p.I = (int)here; p.b = a.x; p.ldb = a.ldx; p.J = (int)a.tokens; p.R = (int)a.cols; p.v0 = (int)v0;
         name_entries(p, a, b.l, b.shape);
-        p.lse = a.lse_in; p.coef = b.coef; p.c = b.dz; p.ldc = pl.piece;
+        p.lse = a.lse_in; p.part = b.part; p.c = b.dz; p.ldc = pl.piece;
         hipError_t e = launch_product<kDz>(p, b.shape, 1, s);
         if (e == hipSuccess && a.dx) {
             // dz is zero up to a whole tile, w has no row past the piece
@@ -821,15 +886,15 @@ hipError_t launch_vocab_loss_backward(const VocabLossArgs& a, hipStream_t s)
             ProductArgs d = {};
             d.a = b.x; d.lda = a.cols; d.I = (int)a.cols; d.b = b.dz; d.ldb = pl.piece; d.J = (int)here; d.R = (int)a.tokens;
             d.c = a.dw_fp32 ? (void*)((float*)a.dw + v0 * a.lddw) : (void*)((uint16_t*)a.dw + v0 * a.lddw);
-            d.ldc = a.lddw; d.c_fp32 = a.dw_fp32; d.add = a.add;
-            e = launch_product<kDw>(d, shape_for(a.cols, std::max<int64_t>(here, 129)), 1, s);
+            d.ldc = a.lddw; d.c_fp32 = a.dw_fp32; d.add = a.add; d.unit = b.unit;
+            e = launch_product<kDw>(d, a.tokens <= 512 ? Shape::kMiddle : shape_for(a.cols, std::max<int64_t>(here, 129)), 1, s);
         }
         if (e != hipSuccess) return e;
     }
     if (!a.dx) return hipSuccess;
     const int64_t blocks = (a.tokens * (a.cols / 8) + 255) / 256;
     hipLaunchKernelGGL(dx_kernel, dim3((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks)), dim3(256), 0, s, b.sums, (int)pl.splits, a.tokens * a.cols, (int)a.tokens, (int)a.cols,
-                       b.coef, a.dx, a.lddx);
+                       b.part, b.unit, a.dx, a.lddx);
     return hipGetLastError();
 }
 

@@ -18,7 +18,7 @@
 namespace snip {
 namespace {
 
-constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 enum Out { kStats, kDz, kDx, kDw };
@@ -34,7 +34,7 @@ struct ProductArgs {
     const void* targets; int target64;
     const int* starts; const int2* items; int64_t items_pitch; int vocab_tiles;
     int v0, vocab;               // entry of A's first row
-    float2* tile_stats;          // stats: [tiles_i][J]
+    float2* tile_stats;          // stats: [tiles_i][J], (largest s log2 e, sum of 2^(s log2 e - that))
     float* z;                    // stats: of every named entry
     const float* lse;            // dz
     const float* part;           // dz: dloss tau of every token in units of *unit, zero for those that take no part
@@ -170,8 +170,9 @@ template <int ROWS, int W, bool TURNED> struct Operand {
 // next stage's first) and issues copies.  A barrier a stage, in front of its last step: every wave has the whole stage in registers
 // then, so its two slots are free, and the next stage has arrived.  With five slots B of stage s + 2 follows A of stage s in the ring and A of
 // stage s + 3 follows B: the copies have 1.5 stages (A) and 0.75 (B) to arrive.
-template <class T, bool TA, bool TB>
-__device__ __forceinline__ void multiply(const ProductArgs& p, uint8_t* lds, int i0, int j0, int first, int last, int lane, int wave, v16f (&acc)[T::MB][T::NB])
+// `meanwhile` is called behind the first copies: loads for later.
+template <class T, bool TA, bool TB, class F>
+__device__ __forceinline__ void multiply(const ProductArgs& p, uint8_t* lds, int i0, int j0, int first, int last, int lane, int wave, v16f (&acc)[T::MB][T::NB], F meanwhile)
 {
     const int wm = wave / T::WGN, wn = wave % T::WGN;
     Operand<T::TM, T::WM, TA> a;
@@ -208,6 +209,7 @@ __device__ __forceinline__ void multiply(const ProductArgs& p, uint8_t* lds, int
             }
         }
     }
+    meanwhile();
     if (last - first >= T::DA) SNIP_WAIT_VM(T::BEHIND_FIRST);
     else                       SNIP_WAIT_VM(0);
     SNIP_BAR();
@@ -266,12 +268,14 @@ __device__ __forceinline__ void multiply(const ProductArgs& p, uint8_t* lds, int
 template <class T> struct Stage {
     static constexpr int ROWB = T::WM * 4, CPR = ROWB / 16, PART = T::LDS / 4 / 1024 * 1024;
     static_assert(32 * ROWB <= PART, "a wave's part");
-    uint8_t* reg;
+    static constexpr int TURN = 2 * 32 * ROWB <= PART ? 32 * ROWB : 0;      // two areas in turn where there is room
+    uint8_t *own, *reg;
     int lane, r32, g;
-    __device__ __forceinline__ Stage(uint8_t* lds, int wave, int lane_) : reg(lds + wave * PART), lane(lane_), r32(lane_ & 31), g(lane_ >> 5) {}
+    __device__ __forceinline__ Stage(uint8_t* lds, int wave, int lane_) : own(lds + wave * PART), reg(own), lane(lane_), r32(lane_ & 31), g(lane_ >> 5) {}
     __device__ __forceinline__ float* at(int col, int row) { return reinterpret_cast<float*>(reg + col * ROWB + (((row >> 2) ^ (col & (CPR - 1))) * 16)) + (row & 3); }
     __device__ __forceinline__ void put(const v16f (&acc)[T::MB][T::NB], int n)
     {
+        reg = own + n % 2 * TURN;
 #pragma unroll
         for (int m = 0; m < T::MB; ++m)
 #pragma unroll
@@ -292,38 +296,64 @@ template <class T> struct Stage {
     }
 };
 
-// The elements of columns 32 n ... 32 n + 31 of this wave's block that the loss names: calls f(column, row, item), a lane for each, with the item of a
-// list or, of targets, the token.  `any` is called first if there are some.
-template <class T, class G, class F>
-__device__ __forceinline__ void named(const ProductArgs& p, int ti, int tj, int wm, int wn, int lane, int n, G any, F f)
-{
-    if (p.targets) {
-        const int j = tj * T::TN + wn * T::WN + n * 32 + lane;
-        int64_t v = -1;
-        if (lane < 32 && j < p.J) v = p.target64 ? ((const int64_t*)p.targets)[j] : (int64_t)((const int*)p.targets)[j];
-        const int64_t row = v - (p.v0 + ti * T::TM + wm * T::WM);
-        const bool is = v < p.vocab && row >= 0 && row < T::WM;
-        if (__builtin_amdgcn_ballot_w64(is) == 0) return;
-        any();
-        if (is) f(lane, (int)row, j);
-        return;
+// The elements of this wave's block that the loss names.
+template <class T> struct Names {
+    const ProductArgs& p;
+    const int2* items;
+    int from, to, lane, row0, col0;          // the run of the tile's list; of the wave's block
+    int2 mine;                               // of the first 64 items of the run
+    int64_t target[T::NB];                   // of the lane's columns, as they are
+    __device__ __forceinline__ Names(const ProductArgs& p_, int lane_) : p(p_), lane(lane_) {}
+    __device__ __forceinline__ void load(int ti, int tj, int wm, int wn)
+    {
+        row0 = wm * T::WM; col0 = wn * T::WN;
+        if (p.targets) {
+            row0 += p.v0 + ti * T::TM;
+#pragma unroll
+            for (int n = 0; n < T::NB; ++n) {
+                const int j = min(tj * T::TN + col0 + n * 32 + (lane & 31), p.J - 1);
+                target[n] = p.target64 ? ((const int64_t*)p.targets)[j] : (int64_t)((const int*)p.targets)[j];
+            }
+            return;
+        }
+        const int* run = p.starts + (int64_t)tj * (p.vocab_tiles + 1) + p.v0 / T::TM + ti;
+        from = __builtin_amdgcn_readfirstlane(run[0]); to = __builtin_amdgcn_readfirstlane(run[1]);
+        items = p.items + tj * p.items_pitch;
+        if (from < to) mine = items[min(from + lane, to - 1)];
     }
-    const int* run = p.starts + (int64_t)tj * (p.vocab_tiles + 1) + p.v0 / T::TM + ti;
-    const int from = __builtin_amdgcn_readfirstlane(run[0]), to = __builtin_amdgcn_readfirstlane(run[1]);
-    const int2* items = p.items + tj * p.items_pitch;
-    bool first = true;
-    for (int e = from; e < to; e += 64) {
-        const int2 mine = items[min(e + lane, to - 1)];
-        const int row = (mine.x >> 16) - wm * T::WM, col = (mine.x & 0xFFFF) - wn * T::WN - n * 32;
-        const bool is = e + lane < to && row >= 0 && row < T::WM && col >= 0 && col < 32;
-        if (__builtin_amdgcn_ballot_w64(is) == 0) continue;
-        if (first) any();
-        first = false;
-        if (is) f(col, row, mine.y);
+    // Those of columns 32 n ... 32 n + 31: calls f(column, row, item), a lane for each, with the item of a list or, of targets, the token; `any` before, if there are some.
+    template <class G, class F> __device__ __forceinline__ void of(int n, int tj, G any, F f) const
+    {
+        if (p.targets) {
+            const int j = tj * T::TN + col0 + n * 32 + lane;
+            const int64_t row = target[n] - row0;
+            const bool is = lane < 32 && j < p.J && target[n] < p.vocab && row >= 0 && row < T::WM;
+            if (__builtin_amdgcn_ballot_w64(is) == 0) return;
+            any();
+            if (is) f(lane, (int)row, j);
+            return;
+        }
+        bool first = true;
+        for (int e = from; e < to; e += 64) {
+            const int2 item = e == from ? mine : items[min(e + lane, to - 1)];
+            const int row = (item.x >> 16) - row0, col = (item.x & 0xFFFF) - col0 - n * 32;
+            const bool is = e + lane < to && row >= 0 && row < T::WM && col >= 0 && col < 32;
+            if (__builtin_amdgcn_ballot_w64(is) == 0) continue;
+            if (first) any();
+            first = false;
+            if (is) f(col, row, item.y);
+        }
     }
-}
+};
 
 __device__ __forceinline__ v4u packed(const float (&f)[8]) { return v4u{pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7])}; }
+
+// Two sums of powers of two, each (reference, sum of 2^(exponent - reference)).
+__device__ __forceinline__ float2 join2(float2 v, float2 o)
+{
+    const float top = fmaxf(v.x, o.x), base = top == -INFINITY ? 0.f : top;
+    return make_float2(top, v.y * __builtin_amdgcn_exp2f(v.x - base) + o.y * __builtin_amdgcn_exp2f(o.x - base));
+}
 
 template <class T, int OUT>
 __global__ __launch_bounds__(T::NT, T::PER_CU) void product_kernel(const ProductArgs p)
@@ -337,14 +367,26 @@ __global__ __launch_bounds__(T::NT, T::PER_CU) void product_kernel(const Product
     const int all = (p.R + 63) / 64, first = OUT == kDx ? blockIdx.y * p.split : 0, last = OUT == kDx ? min(all, first + p.split) : all;
     const float unit = OUT == kDw ? *p.unit : 1.f;
     v16f acc[T::MB][T::NB];
-    multiply<T, (OUT == kDx || OUT == kDw), OUT == kDw>(p, lds, i0, j0, first, last, lane, wave, acc);
     const int iw = i0 + wm * T::WM, jw = j0 + wn * T::WN;
+    Names<T> names(p, lane);
+    float lse[T::NB], part[T::NB];                                  // dz, of the lane's columns
+    multiply<T, (OUT == kDx || OUT == kDw), OUT == kDw>(p, lds, i0, j0, first, last, lane, wave, acc, [&]() {
+        if constexpr (OUT == kStats || OUT == kDz) names.load(ti, tj, wm, wn);
+        if constexpr (OUT == kDz) {
+#pragma unroll
+            for (int n = 0; n < T::NB; ++n) {
+                const int j = min(jw + n * 32 + r32, p.J - 1);
+                lse[n] = p.lse[j];
+                part[n] = p.part[j];
+            }
+        }
+    });
 
     Stage<T> stage(lds, wave, lane);
     if constexpr (OUT == kStats) {
 #pragma unroll
         for (int n = 0; n < T::NB; ++n)
-            named<T>(p, ti, tj, wm, wn, lane, n, [&]() { stage.put(acc, n); }, [&](int col, int row, int place) { p.z[place] = *stage.at(col, row); });
+            names.of(n, tj, [&]() { stage.put(acc, n); }, [&](int col, int row, int place) { p.z[place] = *stage.at(col, row); });
         if (iw + T::WM > p.I) {
 #pragma unroll
             for (int m = 0; m < T::MB; ++m)
@@ -365,13 +407,13 @@ __global__ __launch_bounds__(T::NT, T::PER_CU) void product_kernel(const Product
             for (int m = 0; m < T::MB; ++m)
 #pragma unroll
                 for (int k = 0; k < 16; ++k) top = fmaxf(top, acc[m][n][k]);
-            top = fmaxf(top, __shfl_xor(top, 32));
+            top = fmaxf(top, __shfl_xor(top, 32)) * c;
             const float base = top == -INFINITY ? 0.f : top;
             float sum = 0.f;
 #pragma unroll
             for (int m = 0; m < T::MB; ++m)
 #pragma unroll
-                for (int k = 0; k < 16; ++k) sum += __builtin_amdgcn_exp2f((acc[m][n][k] - base) * c);
+                for (int k = 0; k < 16; ++k) sum += __builtin_amdgcn_exp2f(fmaf(acc[m][n][k], c, -base));
             sum += __shfl_xor(sum, 32);
             if (g == 0) shared[wm * T::TN + wn * T::WN + n * 32 + r32] = make_float2(top, sum);
         }
@@ -380,25 +422,22 @@ __global__ __launch_bounds__(T::NT, T::PER_CU) void product_kernel(const Product
             if (j0 + j >= p.J) break;
             float2 v = shared[j];
 #pragma unroll
-            for (int w = 1; w < T::WGM; ++w) {
-                const float2 o = shared[w * T::TN + j];
-                const float top = fmaxf(v.x, o.x), base = top == -INFINITY ? 0.f : top;
-                v = make_float2(top, v.y * __builtin_amdgcn_exp2f((v.x - base) * c) + o.y * __builtin_amdgcn_exp2f((o.x - base) * c));
-            }
+            for (int w = 1; w < T::WGM; ++w) v = join2(v, shared[w * T::TN + j]);
             p.tile_stats[(int64_t)ti * p.J + j0 + j] = v;
         }
     }
     if constexpr (OUT == kDz) {
+        // (rounded to bf16 soon: a product of the logit with the rounded constant is exact enough)
+        const float c = p.alpha * kLog2e;
 #pragma unroll
         for (int n = 0; n < T::NB; ++n) {
-            const int j = jw + n * 32 + r32;
-            const float lse = j < p.J ? p.lse[j] : 0.f, mine = j < p.J ? p.part[j] : 0.f;
+            const float base = lse[n] * kLog2e, mine = jw + n * 32 + r32 < p.J ? part[n] : 0.f;
 #pragma unroll
             for (int m = 0; m < T::MB; ++m)
 #pragma unroll
-                for (int k = 0; k < 16; ++k) acc[m][n][k] = __builtin_amdgcn_exp2f(fmaf(acc[m][n][k], p.alpha, -lse) * kLog2e);
+                for (int k = 0; k < 16; ++k) acc[m][n][k] = __builtin_amdgcn_exp2f(fmaf(acc[m][n][k], c, -base));
             stage.put(acc, n);
-            named<T>(p, ti, tj, wm, wn, lane, n, []() {}, [&](int col, int row, int q) { *stage.at(col, row) -= p.targets ? 1.f : __int_as_float(q); });
+            names.of(n, tj, []() {}, [&](int col, int row, int q) { *stage.at(col, row) -= p.targets ? 1.f : __int_as_float(q); });
             stage.take([&](int col, int row, const float (&f)[8]) {
                 const float coef = __shfl(mine, col);
                 float v[8];
@@ -564,11 +603,6 @@ __global__ __launch_bounds__(256) void join_kernel(const float2* __restrict__ ti
     __shared__ float2 shared[PARTS][TOK + 1];
     const int tok = threadIdx.x % TOK, part = threadIdx.x / TOK, t = blockIdx.x * TOK + tok;
     const bool here = t < tokens;
-    const float c = alpha * kLog2e;
-    auto join = [&](float2 v, float2 o) {
-        const float top = fmaxf(v.x, o.x), base = top == -INFINITY ? 0.f : top;
-        return make_float2(top, v.y * __builtin_amdgcn_exp2f((v.x - base) * c) + o.y * __builtin_amdgcn_exp2f((o.x - base) * c));
-    };
     // (what the loss names is fetched beside the sums)
     int64_t target = -1;
     float at_target = 0.f;
@@ -582,17 +616,17 @@ __global__ __launch_bounds__(256) void join_kernel(const float2* __restrict__ ti
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[i] = here && i0 + i * PARTS < tiles ? tile_stats[(int64_t)(i0 + i * PARTS) * tokens + t] : make_float2(-INFINITY, 0.f);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v = join(v, o[i]);
+        for (int i = 0; i < 8; ++i) v = join2(v, o[i]);
     }
     shared[part][tok] = v;
     __syncthreads();
 #pragma unroll
     for (int n = PARTS / 2; n > 0; n >>= 1) {
-        if (part < n) shared[part][tok] = v = join(v, shared[part + n][tok]);
+        if (part < n) shared[part][tok] = v = join2(v, shared[part + n][tok]);
         __syncthreads();
     }
     v = shared[0][tok];
-    const float l = fmaf(v.x, alpha, logf(v.y));
+    const float l = fmaf(v.x, kLn2, logf(v.y));
     if (lse && part == 0 && here) lse[t] = l;
     if (!loss) return;
     if (targets) {

@@ -3,10 +3,10 @@
 //     lse = log sum_v exp s_v      loss = tau^2 sum_j q_j (log q_j - s_idx_j + lse)
 //     dz = dloss tau (exp(s - lse) - q)      dx = dz w      dw = dz^T x
 //
-// All of it is one matrix product in bf16 (v_mfma_f32_32x32x16_bf16, C[i][j] = sum_r A[i][r] B[j][r]) with four ways to take the result out
+// All of it is one matrix product in bf16 (v_mfma_f32_16x16x32_bf16, C[i][j] = sum_r A[i][r] B[j][r]) with four ways to take the result out
 // of the accumulators:
 //   stats   A = w, B = x: of every token the tile's largest z and the sum of exp(s - largest), and z of the entries that the loss names;
-//           a second kernel joins the tiles.  A token's logits lie in the registers of two lanes, so the sums need no shuffles.
+//           a second kernel joins the tiles.  A token's logits lie in the registers of four lanes, so the sums need two shuffles.
 //   dz      the same product anew, a piece of the vocabulary at a time: dz in bf16, [token][entry]
 //   dx      A = w^T of the piece, B = dz, split over the vocabulary where there are few tiles: partial sums in fp32, joined at the end
 //   dw      A = x^T, B = dz^T
@@ -14,6 +14,7 @@
 // (ds_read_b64_tr_b16: of each 16 lanes, lane l gets element l of four rows), so nothing is transposed in memory.
 #include "gemm_common.h"
 #include <algorithm>
+#include <type_traits>
 
 namespace snip {
 namespace {
@@ -21,6 +22,7 @@ namespace {
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float v4f __attribute__((ext_vector_type(4)));
 enum Out { kStats, kDz, kDx, kDw };
 
 struct ProductArgs {
@@ -45,7 +47,7 @@ struct ProductArgs {
 // TM x TN outputs of a workgroup of four waves, WM x WN of a wave.  LDS is a ring of SLOTS slots, a stage (64 contraction elements) of A and B
 // in turn; an odd number needs slots of one size.
 template <int TM_, int TN_, int WM_, int WN_, int SLOTS_, int PER_CU_> struct Tile {
-    static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, SLOTS = SLOTS_, PER_CU = PER_CU_, MB = WM / 32, NB = WN / 32, NM = MB * NB;
+    static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, SLOTS = SLOTS_, PER_CU = PER_CU_, MB = WM / 16, NB = WN / 16, NM = MB * NB;      // 16 x 16 blocks of a wave
     static constexpr int WGM = TM / WM, WGN = TN / WN, NT = 256;
     static constexpr int SA = TM * 128, SB = TN * 128, PAIR = SA + SB, LDS = SLOTS / 2 * PAIR + SLOTS % 2 * SA;
     static constexpr int CA = TM / 32, CB = TN / 32;             // 1 KB copies of a wave and stage
@@ -89,23 +91,23 @@ __device__ __forceinline__ v4i early_desc(const uint16_t* p, unsigned bytes)
 
 // One operand of a tile: ROWS indices from `row0` on, of which a wave multiplies W from wave_row on.  C copies of this wave and stage.
 // Not turned, a stage is ROWS rows of 128 bytes; 16-byte chunk c of row r lies at c ^ (r / 2 % 8), so that 16 lanes that read one chunk of 16 rows meet
-// all banks.  Turned it is 64 rows of ROWS elements; chunk c of row r lies at c ^ (r % 4 * 4), so that the four rows that a turning read
-// takes from 64 bytes each lie in different banks.
+// all banks.  Turned it is 64 rows of ROWS elements; chunk c of row r lies at c ^ (r % 4 * 4) ^ (r / 8 % 2 * 2), so that the 16 rows that a turning
+// read takes 32 bytes of, eight apart in fours, meet all banks twice.
 template <int ROWS, int W, bool TURNED> struct Operand {
-    static constexpr int C = ROWS / 32, BLOCKS = W / 32, READS = BLOCKS * (TURNED ? 2 : 1);
+    static constexpr int C = ROWS / 32, BLOCKS = W / 16, READS = BLOCKS * (TURNED ? 2 : 1);
     const uint16_t* p;
     int64_t ld;
     int rows, R;                 // of the tile, of the contraction
     unsigned off[C];
     int chunk[2];                // not turned: of even and odd copies
-    int at[4];
+    int at[TURNED ? BLOCKS : 2];
     v4i rsrc;
 
     __device__ __forceinline__ void start(const uint16_t* base, int64_t ld_, int row0, int all, int R_, int wave_row, int lane, int wave)
     {
         // (whole chunks: what is behind an end that is none is zero in one operand at least, or of outputs that are not stored)
         ld = ld_; rows = (min(ROWS, all - row0) + 7) & ~7; R = TURNED ? R_ : (R_ + 7) & ~7;
-        const int r32 = lane & 31, g = lane >> 5;
+        const int r16 = lane & 15, g = lane >> 4;
         if constexpr (!TURNED) {
             p = base + row0 * ld;
             rsrc = early_desc(p, (unsigned)(((min(ROWS, all - row0) - 1) * ld + R) * 2));
@@ -116,22 +118,22 @@ template <int ROWS, int W, bool TURNED> struct Operand {
                 off[c] = (unsigned)(row * ld * 2) + chunk[c & 1] * 16 + early(c);
             }
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks) at[ks] = (wave_row + r32) * 128 + (((ks * 2 + g) ^ (r32 >> 1 & 7)) * 16);
+            for (int ks = 0; ks < 2; ++ks) at[ks] = (wave_row + r16) * 128 + (((ks * 4 + g) ^ (r16 >> 1)) * 16);
         } else {
             p = base + row0;
             constexpr int PER_ROW = ROWS / 8, RPC = 64 / PER_ROW;
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 const int row = (wave * C + c) * RPC + lane / PER_ROW;
-                off[c] = (unsigned)(row * ld * 2) + ((lane % PER_ROW) ^ ((row & 3) * 4)) * 16 + early(c);
+                off[c] = (unsigned)(row * ld * 2) + ((lane % PER_ROW) ^ spread(row)) * 16 + early(c);
             }
-            // of each 16 lanes, four point to 32 bytes of a row; the two halves of a wave are 8 rows apart
+            // of each 16 lanes, four point to 32 bytes of a row; sixteens of a wave are 8 rows apart
             const int row = 8 * g + (lane >> 2 & 3);
 #pragma unroll
-            for (int m = 0; m < BLOCKS; ++m)
-                at[m] = row * ROWS * 2 + (((wave_row / 32 + m) ^ (row & 3)) * 64) + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+            for (int m = 0; m < BLOCKS; ++m) at[m] = row * ROWS * 2 + ((((wave_row / 16 + m) * 2 + (lane >> 1 & 1)) ^ spread(row)) * 16) + (lane & 1) * 8;
         }
     }
+    static __device__ __forceinline__ int spread(int row) { return (row & 3) * 4 ^ (row >> 3 & 1) * 2; }
     static __device__ __forceinline__ constexpr unsigned early(int c) { return kEarly - (C % 2 == 0 && c % 2 ? 1024 : 0); }
     // before the copies of stage s
     __device__ __forceinline__ void stage(int s)
@@ -153,10 +155,10 @@ template <int ROWS, int W, bool TURNED> struct Operand {
     __device__ __forceinline__ void read(int i, int ks, const uint8_t* slot, bf16x8 (&f)[BLOCKS]) const
     {
         if constexpr (!TURNED) {
-            f[i] = *reinterpret_cast<const bf16x8*>(slot + at[ks] + i * 4096);
+            f[i] = *reinterpret_cast<const bf16x8*>(slot + at[ks] + i * 2048);
         } else {
             typedef const __attribute__((address_space(3))) s16x4* place;
-            const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(place)(slot + at[i / 2] + (ks * 16 + i % 2 * 4) * ROWS * 2));
+            const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(place)(slot + at[i / 2] + (ks * 32 + i % 2 * 4) * ROWS * 2));
             uint2 w = __builtin_bit_cast(uint2, v);
             uint4 old = __builtin_bit_cast(uint4, f[i / 2]);
             if (i % 2 == 0) { old.x = w.x; old.y = w.y; } else { old.z = w.x; old.w = w.y; }
@@ -165,14 +167,22 @@ template <int ROWS, int W, bool TURNED> struct Operand {
     }
 };
 
+// acc += A B^T of a 16 x 16 block.  The large tile's accumulators fill their 256 registers; written as assembly they stay in place, where the compiler
+// moved up to 200 of them in every stage (its hazard waits in front of the first and behind the last of these are in multiply).
+template <class T> __device__ __forceinline__ void mfma(v4f& acc, const bf16x8& a, const bf16x8& b)
+{
+    if constexpr (T::PER_CU == 1) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
+    else                          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, acc, 0, 0, 0);
+}
+
 // The products of a tile, stages [first, last) of the contraction, 64 elements each.
-// A stage is four steps; between the MFMAs of a step the wave reads the operands of the next one from LDS (the last step of a stage those of the
-// next stage's first) and issues copies.  A barrier a stage, in front of its last step: every wave has the whole stage in registers
+// A stage is two steps; between the MFMAs of a step the wave reads the operands of the next one from LDS (the second step of a stage those of the
+// next stage's first) and issues copies.  A barrier a stage, in front of its second step: every wave has the whole stage in registers
 // then, so its two slots are free, and the next stage has arrived.  With five slots B of stage s + 2 follows A of stage s in the ring and A of
-// stage s + 3 follows B: the copies have 1.5 stages (A) and 0.75 (B) to arrive.
+// stage s + 3 follows B: the copies have 1 to 1.5 stages (A) and 0.75 to 1 (B) to arrive.
 // `meanwhile` is called behind the first copies: loads for later.
 template <class T, bool TA, bool TB, class F>
-__device__ __forceinline__ void multiply(const ProductArgs& p, uint8_t* lds, int i0, int j0, int first, int last, int lane, int wave, v16f (&acc)[T::MB][T::NB], F meanwhile)
+__device__ __forceinline__ void multiply(const ProductArgs& p, uint8_t* lds, int i0, int j0, int first, int last, int lane, int wave, v4f (&acc)[T::MB][T::NB], F meanwhile)
 {
     const int wm = wave / T::WGN, wn = wave % T::WGN;
     Operand<T::TM, T::WM, TA> a;
@@ -183,6 +193,7 @@ __device__ __forceinline__ void multiply(const ProductArgs& p, uint8_t* lds, int
     auto ahead = [](unsigned slot) { return slot + T::PAIR >= (unsigned)T::LDS ? slot + T::PAIR - T::LDS : slot + T::PAIR; };      // of the next stage
     bf16x8 fa[2][T::MB], fb[2][T::NB];
     constexpr int READS = a.READS + b.READS;
+    constexpr auto reads_by = [](int i) { const int n = (i * 4 * READS + 3 * T::NM - 1) / (3 * T::NM); return n < READS ? n : READS; };      // in front of MFMA i
     auto read = [&](int j, int ks, unsigned sa, unsigned sb) {
         if (j < b.READS) b.read(j, ks, lds + sb, fb[ks & 1]);
         else             a.read(j - b.READS, ks, lds + sa, fa[ks & 1]);
@@ -190,9 +201,10 @@ __device__ __forceinline__ void multiply(const ProductArgs& p, uint8_t* lds, int
 #pragma unroll
     for (int m = 0; m < T::MB; ++m)
 #pragma unroll
-        for (int n = 0; n < T::NB; ++n)
-#pragma unroll
-            for (int k = 0; k < 16; ++k) acc[m][n][k] = 0.f;
+        for (int n = 0; n < T::NB; ++n) acc[m][n] = v4f{0.f, 0.f, 0.f, 0.f};
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (T::PER_CU == 1) asm volatile("s_nop 7");
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < T::SLOTS; ++i) {
         const int s = first + i / 2;
@@ -221,13 +233,13 @@ __device__ __forceinline__ void multiply(const ProductArgs& p, uint8_t* lds, int
         const unsigned na = ahead(sa), nb = ahead(sb);
         const unsigned to_b = T::SLOTS % 2 ? sa : sb;
         bool more_b = false;
+        if (more_a) a.stage(s - 1 + T::DA);
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-            if (ks == 0 && more_a) a.stage(s - 1 + T::DA);
-            if (ks == 3) {
+        for (int ks = 0; ks < 2; ++ks) {
+            if (ks == 1) {
                 __builtin_amdgcn_s_waitcnt(0xC07F);                 // lgkmcnt(0)
-                if (s - 1 + T::DA < last) SNIP_WAIT_VM(T::BEHIND);
-                else                      SNIP_WAIT_VM(0);
+                if (more_a) SNIP_WAIT_VM(T::BEHIND);
+                else        SNIP_WAIT_VM(0);
                 SNIP_BAR();
                 asm volatile("" ::: "memory");                      // (no read of the next stage before the barrier)
                 more_b = s + T::DB < last;
@@ -235,21 +247,20 @@ __device__ __forceinline__ void multiply(const ProductArgs& p, uint8_t* lds, int
             }
 #pragma unroll
             for (int i = 0; i < T::NM; ++i) {
-                acc[i / T::NB][i % T::NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[ks & 1][i / T::NB], fb[ks & 1][i % T::NB], acc[i / T::NB][i % T::NB], 0, 0, 0);
+                mfma<T>(acc[i / T::NB][i % T::NB], fa[ks][i / T::NB], fb[ks][i % T::NB]);
                 __builtin_amdgcn_sched_barrier(0);
-                // the reads behind the first three quarters of the MFMAs
+                // the reads behind the first three quarters of the MFMAs, B's copies behind the first half
 #pragma unroll
-                for (int j = 0; j < READS; ++j)
-                    if (j * T::NM * 3 / 4 / READS == i) { if (ks < 3) read(j, ks + 1, sa, sb); else read(j, 0, na, nb); }
-                if (ks == 3 && more_b) {
+                for (int j = reads_by(i); j < reads_by(i + 1); ++j) { if (ks == 0) read(j, 1, sa, sb); else read(j, 0, na, nb); }
+                if (ks == 1 && more_b) {
 #pragma unroll
                     for (int u = 0; u < b.UNITS; ++u)
-                        if (u * T::NM / b.UNITS + T::NM / b.UNITS / 4 == i) b.copy(u, s + T::DB, share_b + to_b);
+                        if ((2 * u + 1) * T::NM / 4 / b.UNITS == i) b.copy(u, s + T::DB, share_b + to_b);
                 }
-                if (ks < 2 && more_a) {
+                if (ks == 0 && more_a) {
 #pragma unroll
                     for (int u = 0; u < a.UNITS; ++u)
-                        if ((u * T::NM * 2 + T::NM) / a.UNITS == ks * T::NM + i) a.copy(u, s - 1 + T::DA, share_a + to_a);
+                        if ((2 * u + 1) * T::NM / 2 / a.UNITS == i) a.copy(u, s - 1 + T::DA, share_a + to_a);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -259,35 +270,31 @@ __device__ __forceinline__ void multiply(const ProductArgs& p, uint8_t* lds, int
         sa = na;
         sb = nb;
     }
+    // (a result is there 18 wait states behind its MFMA)
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (T::PER_CU == 1) asm volatile("s_nop 15\n\ts_nop 15");
+    __builtin_amdgcn_sched_barrier(0);
 }
 
-// In registers, lane (r32, g) of block (m, n) holds C[32 m + 8 q + 4 g + t][32 n + r32] in acc[m][n][4 q + t].
+// In registers, lane 16 g + r of block (m, n) holds C[16 m + 4 g + t][16 n + r] in acc[m][n][t].
 
-// A wave's result leaves through its own part of LDS, 32 columns (rows of the result in memory) of WM numbers at a time: stores are whole runs then, and
+// A wave's result leaves through its own part of LDS, 16 columns (rows of the result in memory) of WM numbers at a time: stores are whole runs then, and
 // an element that the loss names is found by its place.  16-byte chunk c of column r lies at c ^ r.
 template <class T> struct Stage {
-    static constexpr int ROWB = T::WM * 4, CPR = ROWB / 16, PART = T::LDS / 4 / 1024 * 1024;
-    static_assert(32 * ROWB <= PART, "a wave's part");
-    static constexpr int TURN = 2 * 32 * ROWB <= PART ? 32 * ROWB : 0;      // two areas in turn where there is room
+    static constexpr int ROWB = T::WM * 4, CPR = ROWB / 16, PART = T::LDS / 4 / 1024 * 1024, AREA = 16 * ROWB;
+    static_assert(2 * AREA <= PART, "a wave's part: two areas in turn");
     uint8_t *own, *reg;
-    int lane, r32, g;
-    __device__ __forceinline__ Stage(uint8_t* lds, int wave, int lane_) : own(lds + wave * PART), reg(own), lane(lane_), r32(lane_ & 31), g(lane_ >> 5) {}
+    int lane, r16, g;
+    __device__ __forceinline__ Stage(uint8_t* lds, int wave, int lane_) : own(lds + wave * PART), reg(own), lane(lane_), r16(lane_ & 15), g(lane_ >> 4) {}
     __device__ __forceinline__ float* at(int col, int row) { return reinterpret_cast<float*>(reg + col * ROWB + (((row >> 2) ^ (col & (CPR - 1))) * 16)) + (row & 3); }
-    __device__ __forceinline__ void put(const v16f (&acc)[T::MB][T::NB], int n)
-    {
-        reg = own + n % 2 * TURN;
-#pragma unroll
-        for (int m = 0; m < T::MB; ++m)
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                *reinterpret_cast<float4*>(at(r32, m * 32 + q * 8 + g * 4)) = make_float4(acc[m][n][4 * q], acc[m][n][4 * q + 1], acc[m][n][4 * q + 2], acc[m][n][4 * q + 3]);
-    }
+    __device__ __forceinline__ void turn(int n) { reg = own + n % 2 * AREA; }
+    __device__ __forceinline__ void put(int m, v4f v) { *reinterpret_cast<v4f*>(at(r16, m * 16 + g * 4)) = v; }
     // calls sink(column, row of the first, eight numbers of a column)
     template <class F> __device__ __forceinline__ void take(F sink)
     {
         constexpr int LANES = T::WM / 8, RPI = 64 / LANES;
 #pragma unroll
-        for (int it = 0; it < 32 / RPI; ++it) {
+        for (int it = 0; it < 16 / RPI; ++it) {
             const int col = it * RPI + lane / LANES, row = lane % LANES * 8;
             const float4 u = *reinterpret_cast<const float4*>(at(col, row)), v = *reinterpret_cast<const float4*>(at(col, row + 4));
             const float f[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
@@ -311,7 +318,7 @@ template <class T> struct Names {
             row0 += p.v0 + ti * T::TM;
 #pragma unroll
             for (int n = 0; n < T::NB; ++n) {
-                const int j = min(tj * T::TN + col0 + n * 32 + (lane & 31), p.J - 1);
+                const int j = min(tj * T::TN + col0 + n * 16 + (lane & 15), p.J - 1);
                 target[n] = p.target64 ? ((const int64_t*)p.targets)[j] : (int64_t)((const int*)p.targets)[j];
             }
             return;
@@ -321,13 +328,13 @@ template <class T> struct Names {
         items = p.items + tj * p.items_pitch;
         if (from < to) mine = items[min(from + lane, to - 1)];
     }
-    // Those of columns 32 n ... 32 n + 31: calls f(column, row, item), a lane for each, with the item of a list or, of targets, the token; `any` before, if there are some.
+    // Those of columns 16 n ... 16 n + 15: calls f(column, row, item), a lane for each, with the item of a list or, of targets, the token; `any` before, if there are some.
     template <class G, class F> __device__ __forceinline__ void of(int n, int tj, G any, F f) const
     {
         if (p.targets) {
-            const int j = tj * T::TN + col0 + n * 32 + lane;
+            const int j = tj * T::TN + col0 + n * 16 + lane;
             const int64_t row = target[n] - row0;
-            const bool is = lane < 32 && j < p.J && target[n] < p.vocab && row >= 0 && row < T::WM;
+            const bool is = lane < 16 && j < p.J && target[n] < p.vocab && row >= 0 && row < T::WM;
             if (__builtin_amdgcn_ballot_w64(is) == 0) return;
             any();
             if (is) f(lane, (int)row, j);
@@ -336,8 +343,8 @@ template <class T> struct Names {
         bool first = true;
         for (int e = from; e < to; e += 64) {
             const int2 item = e == from ? mine : items[min(e + lane, to - 1)];
-            const int row = (item.x >> 16) - row0, col = (item.x & 0xFFFF) - col0 - n * 32;
-            const bool is = e + lane < to && row >= 0 && row < T::WM && col >= 0 && col < 32;
+            const int row = (item.x >> 16) - row0, col = (item.x & 0xFFFF) - col0 - n * 16;
+            const bool is = e + lane < to && row >= 0 && row < T::WM && col >= 0 && col < 16;
             if (__builtin_amdgcn_ballot_w64(is) == 0) continue;
             if (first) any();
             first = false;
@@ -347,6 +354,13 @@ template <class T> struct Names {
 };
 
 __device__ __forceinline__ v4u packed(const float (&f)[8]) { return v4u{pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7])}; }
+
+// Accumulators of the large tile come out of their registers here, not sooner: 256 of them would not fit beside.
+template <class T> __device__ __forceinline__ v4f held(v4f& acc)
+{
+    if constexpr (T::PER_CU == 1) asm volatile("" : "+a"(acc));
+    return acc;
+}
 
 // Two sums of powers of two, each (reference, sum of 2^(exponent - reference)).
 __device__ __forceinline__ float2 join2(float2 v, float2 o)
@@ -360,13 +374,13 @@ __global__ __launch_bounds__(T::NT, T::PER_CU) void product_kernel(const Product
 {
     __shared__ __attribute__((aligned(1024))) uint8_t lds[T::LDS];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = wave / T::WGN, wn = wave % T::WGN, r32 = lane & 31, g = lane >> 5;
+    const int wm = wave / T::WGN, wn = wave % T::WGN, r16 = lane & 15, g = lane >> 4;
     int ti, tj;
     tile_of(blockIdx.x, p.tiles_i * p.tiles_j, p.tiles_i, p.tiles_j, ti, tj);
     const int i0 = ti * T::TM, j0 = tj * T::TN;
     const int all = (p.R + 63) / 64, first = OUT == kDx ? blockIdx.y * p.split : 0, last = OUT == kDx ? min(all, first + p.split) : all;
     const float unit = OUT == kDw ? *p.unit : 1.f;
-    v16f acc[T::MB][T::NB];
+    v4f acc[T::MB][T::NB];
     const int iw = i0 + wm * T::WM, jw = j0 + wn * T::WN;
     Names<T> names(p, lane);
     float lse[T::NB], part[T::NB];                                  // dz, of the lane's columns
@@ -375,7 +389,7 @@ __global__ __launch_bounds__(T::NT, T::PER_CU) void product_kernel(const Product
         if constexpr (OUT == kDz) {
 #pragma unroll
             for (int n = 0; n < T::NB; ++n) {
-                const int j = min(jw + n * 32 + r32, p.J - 1);
+                const int j = min(jw + n * 16 + r16, p.J - 1);
                 lse[n] = p.lse[j];
                 part[n] = p.part[j];
             }
@@ -385,38 +399,49 @@ __global__ __launch_bounds__(T::NT, T::PER_CU) void product_kernel(const Product
     Stage<T> stage(lds, wave, lane);
     if constexpr (OUT == kStats) {
 #pragma unroll
-        for (int n = 0; n < T::NB; ++n)
-            names.of(n, tj, [&]() { stage.put(acc, n); }, [&](int col, int row, int place) { p.z[place] = *stage.at(col, row); });
-        if (iw + T::WM > p.I) {
+        for (int n = 0; n < T::NB; ++n) {
+            stage.turn(n);
+            names.of(n, tj, [&]() {
 #pragma unroll
-            for (int m = 0; m < T::MB; ++m)
-#pragma unroll
-                for (int k = 0; k < 16; ++k)
-                    if (iw + m * 32 + 8 * (k >> 2) + 4 * g + (k & 3) >= p.I) {
-#pragma unroll
-                        for (int n = 0; n < T::NB; ++n) acc[m][n][k] = -INFINITY;
-                    }
+                for (int m = 0; m < T::MB; ++m) stage.put(m, held<T>(acc[m][n]));
+            }, [&](int col, int row, int place) { p.z[place] = *stage.at(col, row); });
         }
         __syncthreads();
         float2* shared = reinterpret_cast<float2*>(lds);             // [WGM][TN]
         const float c = p.alpha * kLog2e;
+        auto sums = [&](auto cut) {                                  // cut: rows past the vocabulary's end do not count
 #pragma unroll
-        for (int n = 0; n < T::NB; ++n) {
-            float top = -INFINITY;
+            for (int n = 0; n < T::NB; ++n) {
+                int rows = p.I - iw - 4 * g;
+                auto counts = [&](int m, int k) { return !decltype(cut)::value || m * 16 + k < rows; };
+                float top = -INFINITY, sum = 0.f;
 #pragma unroll
-            for (int m = 0; m < T::MB; ++m)
+                for (int m = 0; m < T::MB; ++m) {
+                    const v4f v = held<T>(acc[m][n]);
+                    if (decltype(cut)::value) asm volatile("" : "+v"(rows));      // (kept for all blocks, the comparisons would spill)
 #pragma unroll
-                for (int k = 0; k < 16; ++k) top = fmaxf(top, acc[m][n][k]);
-            top = fmaxf(top, __shfl_xor(top, 32)) * c;
-            const float base = top == -INFINITY ? 0.f : top;
-            float sum = 0.f;
+                    for (int k = 0; k < 4; ++k) top = fmaxf(top, counts(m, k) ? v[k] : -INFINITY);
+                }
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32)) * c;
+                const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
-            for (int m = 0; m < T::MB; ++m)
+                for (int m = 0; m < T::MB; ++m) {
+                    const v4f v = held<T>(acc[m][n]);
+                    if (decltype(cut)::value) asm volatile("" : "+v"(rows));
 #pragma unroll
-                for (int k = 0; k < 16; ++k) sum += __builtin_amdgcn_exp2f(fmaf(acc[m][n][k], c, -base));
-            sum += __shfl_xor(sum, 32);
-            if (g == 0) shared[wm * T::TN + wn * T::WN + n * 32 + r32] = make_float2(top, sum);
-        }
+                    for (int k = 0; k < 4; ++k) {
+                        const float e = __builtin_amdgcn_exp2f(fmaf(v[k], c, -base));
+                        sum += counts(m, k) ? e : 0.f;
+                    }
+                }
+                sum += __shfl_xor(sum, 16);
+                sum += __shfl_xor(sum, 32);
+                if (g == 0) shared[wm * T::TN + wn * T::WN + n * 16 + r16] = make_float2(top, sum);
+            }
+        };
+        if (iw + T::WM > p.I) sums(std::true_type());
+        else                  sums(std::false_type());
         __syncthreads();
         for (int j = threadIdx.x; j < T::TN; j += T::NT) {
             if (j0 + j >= p.J) break;
@@ -431,12 +456,15 @@ __global__ __launch_bounds__(T::NT, T::PER_CU) void product_kernel(const Product
         const float c = p.alpha * kLog2e;
 #pragma unroll
         for (int n = 0; n < T::NB; ++n) {
-            const float base = lse[n] * kLog2e, mine = jw + n * 32 + r32 < p.J ? part[n] : 0.f;
+            const float base = lse[n] * kLog2e, mine = jw + n * 16 + r16 < p.J ? part[n] : 0.f;
+            stage.turn(n);
 #pragma unroll
-            for (int m = 0; m < T::MB; ++m)
+            for (int m = 0; m < T::MB; ++m) {
+                v4f v = held<T>(acc[m][n]);
 #pragma unroll
-                for (int k = 0; k < 16; ++k) acc[m][n][k] = __builtin_amdgcn_exp2f(fmaf(acc[m][n][k], c, -base));
-            stage.put(acc, n);
+                for (int k = 0; k < 4; ++k) v[k] = __builtin_amdgcn_exp2f(fmaf(v[k], c, -base));
+                stage.put(m, v);
+            }
             names.of(n, tj, []() {}, [&](int col, int row, int q) { *stage.at(col, row) -= p.targets ? 1.f : __int_as_float(q); });
             stage.take([&](int col, int row, const float (&f)[8]) {
                 const float coef = __shfl(mine, col);
@@ -444,16 +472,18 @@ __global__ __launch_bounds__(T::NT, T::PER_CU) void product_kernel(const Product
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = coef == 0.f || iw + row + e >= p.I ? 0.f : f[e] * coef;
                 // (the pitch covers whole tiles)
-                if (jw + n * 32 + col < p.J) *reinterpret_cast<v4u*>((uint16_t*)p.c + (jw + n * 32 + col) * p.ldc + iw + row) = packed(v);
+                if (jw + n * 16 + col < p.J) *reinterpret_cast<v4u*>((uint16_t*)p.c + (jw + n * 16 + col) * p.ldc + iw + row) = packed(v);
             });
         }
     }
     if constexpr (OUT == kDx || OUT == kDw) {
 #pragma unroll
         for (int n = 0; n < T::NB; ++n) {
-            stage.put(acc, n);
+            stage.turn(n);
+#pragma unroll
+            for (int m = 0; m < T::MB; ++m) stage.put(m, held<T>(acc[m][n]));
             stage.take([&](int col, int row, const float (&f)[8]) {
-                const int j = jw + n * 32 + col, i = iw + row;
+                const int j = jw + n * 16 + col, i = iw + row;
                 if (j >= p.J || i >= p.I) return;                   // (I is a multiple of 8)
                 float v[8];
 #pragma unroll

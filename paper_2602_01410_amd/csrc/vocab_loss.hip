@@ -15,6 +15,7 @@
 #include "gemm_common.h"
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 namespace snip {
 namespace {
@@ -47,14 +48,14 @@ struct ProductArgs {
 // TM x TN outputs of a workgroup of four waves, WM x WN of a wave.  LDS is a ring of SLOTS slots, a stage (64 contraction elements) of A and B
 // in turn; an odd number needs slots of one size.
 template <int TM_, int TN_, int WM_, int WN_, int SLOTS_, int PER_CU_> struct Tile {
+    static constexpr bool LARGE = PER_CU_ == 1;
     static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, SLOTS = SLOTS_, PER_CU = PER_CU_, MB = WM / 16, NB = WN / 16, NM = MB * NB;      // 16 x 16 blocks of a wave
     static constexpr int WGM = TM / WM, WGN = TN / WN, NT = 256;
     static constexpr int SA = TM * 128, SB = TN * 128, PAIR = SA + SB, LDS = SLOTS / 2 * PAIR + SLOTS % 2 * SA;
     static constexpr int CA = TM / 32, CB = TN / 32;             // 1 KB copies of a wave and stage
     static constexpr int DA = (SLOTS + 1) / 2, DB = SLOTS / 2;   // how many stages ahead copies are issued
     // copies that may be under way when the next stage has to be there: those behind it
-    static constexpr int BEHIND = (DB - 2) * (CA + CB) + (SLOTS % 2 ? CA : 0);
-    static constexpr int BEHIND_FIRST = (SLOTS / 2 - 1) * (CA + CB) + SLOTS % 2 * CA;
+    static constexpr int BEHIND = (DB - 2) * (CA + CB) + (SLOTS % 2 ? CA : 0), BEHIND_FIRST = (DA - 2) * CA + (DB - 1) * CB;
     static_assert(WGM * WGN == 4 && (SLOTS % 2 == 0 || SA == SB) && DB >= 2 && LDS * PER_CU <= 160 * 1024, "tile");
 };
 using Large = Tile<256, 256, 128, 128, 5, 1>;
@@ -93,8 +94,8 @@ __device__ __forceinline__ v4i early_desc(const uint16_t* p, unsigned bytes)
 // Not turned, a stage is ROWS rows of 128 bytes; 16-byte chunk c of row r lies at c ^ (r / 2 % 8), so that 16 lanes that read one chunk of 16 rows meet
 // all banks.  Turned it is 64 rows of ROWS elements; chunk c of row r lies at c ^ (r % 4 * 4) ^ (r / 8 % 2 * 2), so that the 16 rows that a turning
 // read takes 32 bytes of, eight apart in fours, meet all banks twice.
-template <int ROWS, int W, bool TURNED> struct Operand {
-    static constexpr int C = ROWS / 32, BLOCKS = W / 16, READS = BLOCKS * (TURNED ? 2 : 1);
+template <int ROWS, int W, bool TURNED, bool SINGLE> struct Operand {
+    static constexpr int C = ROWS / 32, PAIR = !SINGLE && C % 2 == 0 ? 2 : 1, UNITS = C / PAIR, BLOCKS = W / 16, READS = BLOCKS * (TURNED ? 2 : 1);
     const uint16_t* p;
     int64_t ld;
     int rows, R;                 // of the tile, of the contraction
@@ -134,23 +135,24 @@ template <int ROWS, int W, bool TURNED> struct Operand {
         }
     }
     static __device__ __forceinline__ int spread(int row) { return (row & 3) * 4 ^ (row >> 3 & 1) * 2; }
-    static __device__ __forceinline__ constexpr unsigned early(int c) { return kEarly - (C % 2 == 0 && c % 2 ? 1024 : 0); }
-    // before the copies of stage s
+    static __device__ __forceinline__ constexpr unsigned early(int c) { return kEarly - (PAIR == 2 && c % 2 ? 1024 : 0); }
+    // before the copies of stage s; past the contraction's end they bring zeros
     __device__ __forceinline__ void stage(int s)
     {
         if constexpr (TURNED) {
-            rsrc = early_desc(p + (int64_t)s * 64 * ld, (unsigned)(((min(64, R - s * 64) - 1) * ld + rows) * 2));
+            const int here = min(64, R - s * 64);
+            rsrc = here > 0 ? early_desc(p + (int64_t)s * 64 * ld, (unsigned)(((here - 1) * ld + rows) * 2)) : early_desc(p, 0);
         } else if (s * 64 + 64 > R) {                               // chunks past the end of a row lose their source
 #pragma unroll
             for (int c = 0; c < C; ++c) off[c] = chunk[c & 1] * 8 + s * 64 < R ? off[c] : kNoSource;
         }
     }
-    static constexpr int UNITS = C % 2 == 0 ? C / 2 : C;
+    // (within the descriptor's size: see copy_ranges.h)
+    __device__ __forceinline__ unsigned uniform(int s) const { return TURNED ? 0u : (unsigned)min(s, (R - 1) / 64) * 128u; }
     __device__ __forceinline__ void copy(int u, int s, unsigned to)
     {
-        const unsigned soff = TURNED ? 0u : (unsigned)s * 128u;
-        if constexpr (C % 2 == 0) copy2(rsrc, off[2 * u], off[2 * u + 1], soff, to + u * 2048);
-        else                      copy1(rsrc, off[u], soff, to + u * 1024);
+        if constexpr (PAIR == 2) copy2(rsrc, off[2 * u], off[2 * u + 1], uniform(s), to + u * 2048);
+        else                     copy1(rsrc, off[u], uniform(s), to + u * 1024);
     }
     __device__ __forceinline__ void read(int i, int ks, const uint8_t* slot, bf16x8 (&f)[BLOCKS]) const
     {
@@ -167,12 +169,23 @@ template <int ROWS, int W, bool TURNED> struct Operand {
     }
 };
 
+template <int N, class F, int... I> __device__ __forceinline__ void unroll_for_(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>()), ...); }
+template <int N, class F> __device__ __forceinline__ void unroll_for(F f) { unroll_for_<N>(f, std::make_integer_sequence<int, N>()); }
+
 // acc += A B^T of a 16 x 16 block.  The large tile's accumulators fill their 256 registers; written as assembly they stay in place, where the compiler
 // moved up to 200 of them in every stage (its hazard waits in front of the first and behind the last of these are in multiply).
 template <class T> __device__ __forceinline__ void mfma(v4f& acc, const bf16x8& a, const bf16x8& b)
 {
-    if constexpr (T::PER_CU == 1) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
+    if constexpr (T::LARGE) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
     else                          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, acc, 0, 0, 0);
+}
+
+// The same with copy `c` of the large tile behind it: M0 is set in front, and the MFMA is its wait state; so the copy takes two issue slots of the four
+// that an MFMA leaves.
+template <int CTO> __device__ __forceinline__ void mfma_copy(v4f& acc, const bf16x8& a, const bf16x8& b, v4i rsrc, unsigned off, unsigned soff, unsigned to)
+{
+    asm volatile("s_add_u32 m0, %6, %7\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0\n\tbuffer_load_dwordx4 %3, %4, %5 offen lds"
+                 : "+a"(acc) : "v"(a), "v"(b), "v"(off), "s"(rsrc), "s"(soff), "s"(to), "i"(CTO) : "memory", "m0", "scc");
 }
 
 // The products of a tile, stages [first, last) of the contraction, 64 elements each.
@@ -185,8 +198,8 @@ template <class T, bool TA, bool TB, class F>
 __device__ __forceinline__ void multiply(const ProductArgs& p, uint8_t* lds, int i0, int j0, int first, int last, int lane, int wave, v4f (&acc)[T::MB][T::NB], F meanwhile)
 {
     const int wm = wave / T::WGN, wn = wave % T::WGN;
-    Operand<T::TM, T::WM, TA> a;
-    Operand<T::TN, T::WN, TB> b;
+    Operand<T::TM, T::WM, TA, T::LARGE> a;
+    Operand<T::TN, T::WN, TB, T::LARGE> b;
     a.start(p.a, p.lda, i0, p.I, p.R, wm * T::WM, lane, wave);
     b.start(p.b, p.ldb, j0, p.J, p.R, wn * T::WN, lane, wave);
     const unsigned lds0 = lds_addr(lds), share_a = lds0 + wave * T::CA * 1024, share_b = lds0 + wave * T::CB * 1024;
@@ -203,76 +216,86 @@ __device__ __forceinline__ void multiply(const ProductArgs& p, uint8_t* lds, int
 #pragma unroll
         for (int n = 0; n < T::NB; ++n) acc[m][n] = v4f{0.f, 0.f, 0.f, 0.f};
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (T::PER_CU == 1) asm volatile("s_nop 7");
+    if constexpr (T::LARGE) asm volatile("s_nop 7");
     __builtin_amdgcn_sched_barrier(0);
+    // all slots but A's last: its copies are those of the first stage below.  (Copies go on past the end, with zeros that nobody reads: without tests, and the
+    // numbers of copies under way stay the same.)
 #pragma unroll
     for (int i = 0; i < T::SLOTS; ++i) {
+        if (i == 2 * (T::DA - 1)) continue;
         const int s = first + i / 2;
-        if (s < last) {
-            const unsigned slot = i / 2 * T::PAIR + i % 2 * T::SA;
-            if (i % 2 == 0) {
-                a.stage(s);
+        const unsigned slot = i / 2 * T::PAIR + i % 2 * T::SA;
+        if (i % 2 == 0) {
+            a.stage(s);
 #pragma unroll
-                for (int u = 0; u < a.UNITS; ++u) a.copy(u, s, share_a + slot);
-            } else {
-                b.stage(s);
+            for (int u = 0; u < a.UNITS; ++u) a.copy(u, s, share_a + slot);
+        } else {
+            b.stage(s);
 #pragma unroll
-                for (int u = 0; u < b.UNITS; ++u) b.copy(u, s, share_b + slot);
-            }
+            for (int u = 0; u < b.UNITS; ++u) b.copy(u, s, share_b + slot);
         }
     }
     meanwhile();
-    if (last - first >= T::DA) SNIP_WAIT_VM(T::BEHIND_FIRST);
-    else                       SNIP_WAIT_VM(0);
+    SNIP_WAIT_VM(T::BEHIND_FIRST);
     SNIP_BAR();
-    unsigned sa = 0, sb = T::SA, to_a = 0;
+    unsigned sa = 0, sb = T::SA, to_a = (T::DA - 1) * T::PAIR;
 #pragma unroll
     for (int j = 0; j < READS; ++j) read(j, 0, sa, sb);
-    bool more_a = false;                                            // A of stage s - 1 + DA belongs into slot to_a
     for (int s = first; s < last; ++s) {
         const unsigned na = ahead(sa), nb = ahead(sb);
-        const unsigned to_b = T::SLOTS % 2 ? sa : sb;
-        bool more_b = false;
-        if (more_a) a.stage(s - 1 + T::DA);
+        // A of stage s - 1 + DA goes into the slot that the stage before left, B of stage s + DB into one of this stage's
+        const int next_a = s - 1 + T::DA, next_b = s + T::DB;
+        const unsigned lds_a = share_a + to_a, lds_b = share_b + (T::SLOTS % 2 ? sa : sb), at_a = a.uniform(next_a), at_b = b.uniform(next_b);
+        a.stage(next_a);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             if (ks == 1) {
                 __builtin_amdgcn_s_waitcnt(0xC07F);                 // lgkmcnt(0)
-                if (more_a) SNIP_WAIT_VM(T::BEHIND);
-                else        SNIP_WAIT_VM(0);
+                SNIP_WAIT_VM(T::BEHIND);
                 SNIP_BAR();
                 asm volatile("" ::: "memory");                      // (no read of the next stage before the barrier)
-                more_b = s + T::DB < last;
-                if (more_b) b.stage(s + T::DB);
+                b.stage(next_b);
             }
-#pragma unroll
-            for (int i = 0; i < T::NM; ++i) {
-                mfma<T>(acc[i / T::NB][i % T::NB], fa[ks][i / T::NB], fb[ks][i % T::NB]);
+            // A's copies are spread over the first step, B's over the first half of the second
+            constexpr int EVERY_A = T::NM / a.UNITS, EVERY_B = T::NM / 2 / b.UNITS;
+            unroll_for<T::NM>([&](auto index) {
+                constexpr int i = decltype(index)::value;
+                v4f& c = acc[i / T::NB][i % T::NB];
+                if constexpr (T::LARGE) {
+                    constexpr int ua = i % EVERY_A == EVERY_A / 2 ? i / EVERY_A : -1, ub = i % EVERY_B == EVERY_B / 2 && i < T::NM / 2 ? i / EVERY_B : -1;
+                    if (ks == 0 && ua >= 0)      mfma_copy<(ua < 0 ? 0 : ua) * 1024>(c, fa[ks][i / T::NB], fb[ks][i % T::NB], a.rsrc, a.off[ua < 0 ? 0 : ua], at_a, lds_a);
+                    else if (ks == 1 && ub >= 0) mfma_copy<(ub < 0 ? 0 : ub) * 1024>(c, fa[ks][i / T::NB], fb[ks][i % T::NB], b.rsrc, b.off[ub < 0 ? 0 : ub], at_b, lds_b);
+                    else                         mfma<T>(c, fa[ks][i / T::NB], fb[ks][i % T::NB]);
+                } else {
+                    mfma<T>(c, fa[ks][i / T::NB], fb[ks][i % T::NB]);
+                }
                 __builtin_amdgcn_sched_barrier(0);
-                // the reads behind the first three quarters of the MFMAs, B's copies behind the first half
+                // the reads behind the first three quarters of the MFMAs
 #pragma unroll
                 for (int j = reads_by(i); j < reads_by(i + 1); ++j) { if (ks == 0) read(j, 1, sa, sb); else read(j, 0, na, nb); }
-                if (ks == 1 && more_b) {
-#pragma unroll
-                    for (int u = 0; u < b.UNITS; ++u)
-                        if ((2 * u + 1) * T::NM / 4 / b.UNITS == i) b.copy(u, s + T::DB, share_b + to_b);
-                }
-                if (ks == 0 && more_a) {
+                if constexpr (!T::LARGE) {
 #pragma unroll
                     for (int u = 0; u < a.UNITS; ++u)
-                        if ((2 * u + 1) * T::NM / 2 / a.UNITS == i) a.copy(u, s - 1 + T::DA, share_a + to_a);
+                        if (ks == 0 && (2 * u + 1) * T::NM / 2 / a.UNITS == i) a.copy(u, next_a, lds_a);
+#pragma unroll
+                    for (int u = 0; u < b.UNITS; ++u)
+                        if (ks == 1 && (2 * u + 1) * T::NM / 4 / b.UNITS == i) b.copy(u, next_b, lds_b);
                 }
                 __builtin_amdgcn_sched_barrier(0);
-            }
+            });
         }
         to_a = T::SLOTS % 2 ? sb : sa;
-        more_a = s + T::DA < last;
         sa = na;
         sb = nb;
     }
+    // the last copies have to be there before LDS holds something else, and before the workgroup's end
+    SNIP_WAIT_VM(0);
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    SNIP_BAR();
+    asm volatile("" ::: "memory");
     // (a result is there 18 wait states behind its MFMA)
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (T::PER_CU == 1) asm volatile("s_nop 15\n\ts_nop 15");
+    if constexpr (T::LARGE) asm volatile("s_nop 15\n\ts_nop 15");
     __builtin_amdgcn_sched_barrier(0);
 }
 
@@ -358,7 +381,7 @@ __device__ __forceinline__ v4u packed(const float (&f)[8]) { return v4u{pack2(f[
 // Accumulators of the large tile come out of their registers here, not sooner: 256 of them would not fit beside.
 template <class T> __device__ __forceinline__ v4f held(v4f& acc)
 {
-    if constexpr (T::PER_CU == 1) asm volatile("" : "+a"(acc));
+    if constexpr (T::LARGE) asm volatile("" : "+a"(acc));
     return acc;
 }
 

@@ -793,12 +793,24 @@ size_t to256(size_t n) { return (n + 255) / 256 * 256; }
 enum class Shape { kLarge, kMiddle, kFew64, kFew32 };
 constexpr int tile_rows(Shape s) { return s == Shape::kLarge ? 256 : 128; }
 constexpr int tile_cols(Shape s) { return s == Shape::kLarge ? 256 : s == Shape::kMiddle ? 128 : s == Shape::kFew64 ? 64 : 32; }
-// The tile for I x J outputs, J of them tokens.
-Shape shape_for(int64_t I, int64_t J)
+constexpr int64_t stages_of(int64_t n) { return (n + 63) / 64; }
+constexpr int64_t tiles_of(Shape s, int64_t I, int64_t J) { return up(I, tile_rows(s)) / tile_rows(s) * (up(J, tile_cols(s)) / tile_cols(s)); }
+// About how long `units` tiles of so many stages take, us: a stage and what comes before and behind them, for as many at a time as the chip holds.  Measured: 256 x
+// 256 1.45-1.6 us a stage and 8 (8192 x 4096 against 128000: 64 stages, 100 us a tile; dw of 250 tokens: 4 stages, 14.4), 128 x 128 by two workgroups of a
+// compute unit 1.1-1.4 and 2.5 (515 x 1024 against 8191: 16 stages, 21; dw of 250 tokens: 7.1).
+constexpr int64_t kUnits = 256;
+double tile_time(Shape s, int64_t units, int64_t stages)
 {
-    if (J <= 32) return Shape::kFew32;
-    if (J <= 64) return Shape::kFew64;
-    return J <= 128 || up(I, 256) / 256 * (up(J, 256) / 256) < 256 ? Shape::kMiddle : Shape::kLarge;
+    return s == Shape::kLarge ? (double)((units + kUnits - 1) / kUnits) * (1.5 * stages + 8.4) : (double)((units + 2 * kUnits - 1) / (2 * kUnits)) * (1.2 * stages + 2.5);
+}
+Shape faster(int64_t I, int64_t J, int64_t R)
+{
+    return tile_time(Shape::kLarge, tiles_of(Shape::kLarge, I, J), stages_of(R)) < tile_time(Shape::kMiddle, tiles_of(Shape::kMiddle, I, J), stages_of(R)) ? Shape::kLarge : Shape::kMiddle;
+}
+// The tile for I x J outputs of a contraction of R, J of them tokens: as narrow as they are few.
+Shape shape_for(int64_t I, int64_t J, int64_t R)
+{
+    return J <= 32 ? Shape::kFew32 : J <= 64 ? Shape::kFew64 : J <= 128 ? Shape::kMiddle : faster(I, J, R);
 }
 
 template <class T, int OUT> hipError_t launch_product(ProductArgs p, int splits, hipStream_t s)
@@ -818,17 +830,37 @@ template <int OUT> hipError_t launch_product(const ProductArgs& p, Shape shape, 
     return launch_product<Middle, OUT>(p, splits, s);
 }
 
-// The backward call's pieces of the vocabulary and splits of dx.
-struct Plan { int64_t piece, splits; };
+// The backward call's pieces of the vocabulary, and the tiles and splits of dx.
+struct Plan { int64_t piece, splits; Shape dx; };
 constexpr int64_t kPieceElements = 1 << 27, kLeastPiece = 4096, kMostPiece = 1 << 17, kSplitElements = 1 << 25;
+// Splits of `here` entries, none of them empty, that are no more than `most`.
+int64_t splits_of(int64_t here, int64_t most)
+{
+    const int64_t per = (stages_of(here) + most - 1) / most;
+    return (stages_of(here) + per - 1) / per;
+}
 Plan plan_of(const VocabLossArgs& a)
 {
     Plan r;
     r.piece = std::min(up(a.vocab, 256), std::min(kMostPiece, std::max(kLeastPiece, kPieceElements / a.tokens / 256 * 256)));
-    // splits of dx: as many workgroups as there are at a time, of 512 entries at least, and partial sums within kSplitElements
-    const int64_t tn = a.tokens <= 32 ? 32 : a.tokens <= 64 ? 64 : a.tokens <= 128 ? 128 : 256, tm = tn == 256 ? 256 : 128;
-    const int64_t tiles = up(a.cols, tm) / tm * (up(a.tokens, tn) / tn);
-    r.splits = std::max<int64_t>(1, std::min({kSplitElements / (a.tokens * a.cols), r.piece / 512, (tm == 256 ? 256 : 512) / tiles}));
+    // splits of dx: those of 512 entries at least whose products and partial sums (written, read: 4 TB/s) take least, within kSplitElements
+    const int64_t first = std::min(r.piece, a.vocab), most = std::max<int64_t>(1, std::min({kSplitElements / (a.tokens * a.cols), r.piece / 512, (int64_t)256}));
+    double least = 0;
+    r.splits = 0;
+    auto consider = [&](Shape s) {
+        const int64_t tiles = tiles_of(s, a.cols, a.tokens), at_a_time = s == Shape::kLarge ? kUnits : 2 * kUnits;
+        for (int64_t halves : {0, 1, 2, 4, 6}) {                     // rounds of workgroups, in halves
+            const int64_t splits = splits_of(first, std::max<int64_t>(1, std::min(most, halves * at_a_time / (2 * tiles))));
+            const double t = tile_time(s, tiles * splits, (stages_of(first) + splits - 1) / splits) + (double)(a.tokens * a.cols * splits) * 8 / 4e6;
+            if (r.splits == 0 || t < least) { least = t; r.splits = splits; r.dx = s; }
+        }
+    };
+    if (a.tokens <= 128) {
+        consider(shape_for(0, a.tokens, 0));
+    } else {
+        consider(Shape::kLarge);
+        consider(Shape::kMiddle);
+    }
     return r;
 }
 
@@ -863,7 +895,7 @@ Forward forward_space(const VocabLossArgs& a)
 {
     Space s{(uint8_t*)a.workspace};
     Forward f;
-    f.shape = shape_for(a.vocab, a.tokens);
+    f.shape = shape_for(a.vocab, a.tokens, a.cols);
     f.l = lists_space(a, f.shape, s);
     f.z = s.take<float>((size_t)a.tokens * a.k); f.entropy = s.take<float>(a.tokens);
     f.stats = s.take<float2>((size_t)(up(a.vocab, tile_rows(f.shape)) / tile_rows(f.shape)) * a.tokens);
@@ -875,7 +907,7 @@ Backward backward_space(const VocabLossArgs& a, const Plan& pl)
 {
     Space s{(uint8_t*)a.workspace};
     Backward b;
-    b.shape = shape_for(pl.piece, a.tokens);
+    b.shape = shape_for(std::min(pl.piece, a.vocab), a.tokens, a.cols);
     b.l = lists_space(a, b.shape, s);
     b.coef = s.take<float>(a.distill ? a.tokens : 0); b.part = s.take<float>(a.tokens); b.unit = s.take<float>(1);
     b.x = s.take<uint16_t>(a.tokens * a.cols);
@@ -967,14 +999,14 @@ hipError_t launch_vocab_loss_backward(const VocabLossArgs& a, hipStream_t s)
             d.a = w; d.lda = a.ldw; d.I = (int)a.cols; d.b = b.dz; d.ldb = pl.piece; d.J = (int)a.tokens; d.R = (int)here;
             d.split = (int)((up(here, 64) / 64 + pl.splits - 1) / pl.splits);
             d.c = b.sums; d.ldc = a.cols; d.split_stride = a.tokens * a.cols; d.add = v0 > 0;
-            e = launch_product<kDx>(d, shape_for(a.cols * pl.splits, a.tokens), (int)pl.splits, s);
+            e = launch_product<kDx>(d, pl.dx, (int)pl.splits, s);
         }
         if (e == hipSuccess && a.dw) {
             ProductArgs d = {};
             d.a = b.x; d.lda = a.cols; d.I = (int)a.cols; d.b = b.dz; d.ldb = pl.piece; d.J = (int)here; d.R = (int)a.tokens;
             d.c = a.dw_fp32 ? (void*)((float*)a.dw + v0 * a.lddw) : (void*)((uint16_t*)a.dw + v0 * a.lddw);
             d.ldc = a.lddw; d.c_fp32 = a.dw_fp32; d.add = a.add; d.unit = b.unit;
-            e = launch_product<kDw>(d, a.tokens <= 512 ? Shape::kMiddle : shape_for(a.cols, std::max<int64_t>(here, 129)), 1, s);
+            e = launch_product<kDw>(d, faster(a.cols, here, a.tokens), 1, s);
         }
         if (e != hipSuccess) return e;
     }

@@ -455,7 +455,7 @@ snip_status snip_embed(const void* w, snip_out_dtype w_dtype, int64_t vocab, int
 
 /* Its gradient: dw[v] = scale * (sum of dy[t] over the t with ids[t] == v), or, with `accumulate`, that added to what dw holds (a second
  * micro-batch; a table that is the head's weight too).
- *   dy  : device, bf16 [tokens][ld_dy], 16-byte aligned, ld_dy >= cols, a multiple of 8; tokens < 2^30.
+ *   dy  : device, bf16 [tokens][ld_dy], 16-byte aligned, ld_dy >= cols, a multiple of 8; tokens < 2^30, vocab <= 2^30.
  *   dw  : device, bf16 or fp32 (dw_dtype) [vocab][ld_dw], 16-byte aligned, ld_dw a multiple of 8.  Rows that no token names become
  *         zero, or with `accumulate` are not touched.
  *   workspace: device, >= snip_embed_workspace_bytes(tokens, cols, vocab) bytes, 16-byte aligned.  The size never falls as an extent grows.
@@ -468,7 +468,7 @@ snip_status snip_embed_backward(const void* dy, int64_t tokens, int64_t cols, in
 /* Softmax cross entropy of x [tokens][cols] against the head's weight w [vocab][cols], z = x w^T never being stored:
  *     lse[t] = log(sum over v of exp(z[t][v])),   loss[t] = lse[t] - z[t][targets[t]],   0 where targets[t] is no token.
  *   x, w   : device, bf16 [rows][ld], 16-byte aligned; cols and both ld >= cols multiples of 8; cols < 2^20, ld < 2^22; up to 2^21 tokens;
- *            0 < vocab <= 2^21.
+ *            0 < vocab <= 2^21; tokens * vocab and tokens * cols up to 2^37.
  *   targets: device, [tokens].
  *   loss, lse: device, fp32 [tokens]; lse is what the backward call needs.  Either may be NULL.
  *   workspace: device, >= snip_vocab_loss_workspace_bytes(tokens, cols, vocab, 1) bytes, 16-byte aligned.  The size never falls as an extent grows;
@@ -487,7 +487,9 @@ snip_status snip_cross_entropy(const void* x, int64_t tokens, int64_t cols, int6
  *   dw   : device, bf16 or fp32 (dw_dtype) [vocab][ld_dw], 16-byte aligned, ld_dw a multiple of 8, or NULL (a frozen head); with
  *          `accumulate` the gradient is added to what dw holds.
  *   workspace: as above, >= snip_vocab_loss_backward_workspace_bytes(tokens, cols, vocab, 1) bytes.
- * dz is rounded to bf16 once, before the products with w and x (relative 2^-8 of each, also of an fp32 dw); sums are fp32, in a fixed order. */
+ * dz is rounded to bf16 once, before the products with w and x (relative 2^-8 of each, also of an fp32 dw), in units of the largest finite |dloss|
+ * (distillation: dloss * temperature): of equal weights the entry that is wanted loses least, and what is below 2^-126 of that unit may
+ * become zero.  Sums are fp32, in a fixed order. */
 size_t snip_vocab_loss_backward_workspace_bytes(int64_t tokens, int64_t cols, int64_t vocab, int64_t k);
 snip_status snip_cross_entropy_backward(const void* x, int64_t tokens, int64_t cols, int64_t ld_x, const void* w, int64_t vocab,
                                         int64_t ld_w, const void* targets, snip_index_dtype index_dtype, const float* lse,

@@ -107,6 +107,8 @@ snip_status check_out(const snip_qtensor* o, int64_t stored_rows, int64_t stored
 
 // Operands of the calls at both ends of a model: rows of a table or of tokens, whole pieces of 16 bytes.
 constexpr int64_t kMostTokens = 1 << 21, kMostLd = 1 << 22, kMostVocab = (int64_t)1 << 31, kMostHead = 1 << 21, kMostWidth = 1 << 20;
+// what their grids hold: 2^32 threads
+constexpr int64_t kMostTable = (int64_t)1 << 30, kMostLogits = (int64_t)1 << 37;
 bool valid_type(int t) { return t == SNIP_OUT_BF16 || t == SNIP_OUT_FP32; }
 snip_status check_index(const void* p, int type, int64_t n)
 {
@@ -117,7 +119,7 @@ snip_status check_index(const void* p, int type, int64_t n)
 snip_status check_vocab_loss(const VocabLossArgs& a, int index_type)
 {
     if (a.tokens < 0 || a.tokens > kMostTokens || a.vocab <= 0 || a.vocab > kMostHead || a.cols <= 0 || a.cols >= kMostWidth || a.cols % 8 != 0) return SNIP_ERR_SHAPE;
-    if (a.ldx >= kMostLd || a.ldw >= kMostLd) return SNIP_ERR_SHAPE;
+    if (a.ldx >= kMostLd || a.ldw >= kMostLd || a.tokens * std::max(a.vocab, (int64_t)a.cols) > kMostLogits) return SNIP_ERR_SHAPE;
     if (a.k < 1 || a.k > 1024 || a.tokens * a.k >= (int64_t)1 << 31) return SNIP_ERR_SHAPE;
     if (!std::isfinite(a.tau) || !(a.tau > 0.f) || !std::isfinite(1.f / a.tau)) return SNIP_ERR_FORMAT;
     snip_status st = check_rows(a.x, a.tokens, a.cols, a.ldx);
@@ -657,7 +659,7 @@ snip_status snip_embed_backward(const void* dy, int64_t tokens, int64_t cols, in
                                 int64_t ld_dw, int32_t accumulate, void* workspace, size_t workspace_bytes_, void* stream)
 {
     if (!valid_type(dw_dtype) || !std::isfinite(scale)) return SNIP_ERR_FORMAT;
-    if (tokens < 0 || tokens >= (int64_t)1 << 30 || vocab <= 0 || vocab >= kMostVocab || cols <= 0 || cols >= kMostWidth || cols % 8 != 0) return SNIP_ERR_SHAPE;
+    if (tokens < 0 || tokens >= (int64_t)1 << 30 || vocab <= 0 || vocab > kMostTable || cols <= 0 || cols >= kMostWidth || cols % 8 != 0) return SNIP_ERR_SHAPE;
     snip_status st = check_rows(dy, tokens, cols, ld_dy);
     if (st == SNIP_OK) st = check_rows(dw, vocab, cols, ld_dw);
     if (st == SNIP_OK) st = check_index(ids, id_dtype, tokens);

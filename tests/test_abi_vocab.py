@@ -33,7 +33,7 @@ def test_embed_backward(S):
         return S._lib().snip_embed_backward(dy, tokens, cols, ld, ids, it, vocab, scale, dw, dt, ldw, add, ws, n, None)
     assert back(dy=None) == NULL and back(ids=None) == NULL and back(dw=None) == NULL
     assert back(dt=2) == FORMAT and back(it=2) == FORMAT and back(scale=float("nan")) == FORMAT
-    assert back(tokens=-1) == SHAPE and back(tokens=1 << 30) == SHAPE and back(vocab=0) == SHAPE and back(cols=12) == SHAPE and back(ld=32) == SHAPE and back(ldw=32) == SHAPE
+    assert back(tokens=-1) == SHAPE and back(tokens=1 << 30) == SHAPE and back(vocab=0) == SHAPE and back(vocab=(1 << 30) + 1) == SHAPE and back(cols=12) == SHAPE and back(ld=32) == SHAPE and back(ldw=32) == SHAPE
     assert back(ld=68) == LAYOUT and back(ldw=68) == LAYOUT and back(dw=at(0x10008)) == LAYOUT and back(ids=at(0x10004)) == LAYOUT and back(ws=at(0x10008)) == LAYOUT
     size = S.embed_workspace_bytes(100, 64, 50)
     assert back(ws=None) == WORKSPACE and back(n=size - 1) == WORKSPACE
@@ -76,6 +76,9 @@ def test_losses(S):
         assert call(tokens=-1) == SHAPE and call(tokens=(1 << 21) + 1) == SHAPE and call(vocab=0) == SHAPE and call(vocab=1 << 31) == SHAPE and call(cols=60) == SHAPE
         assert call(cols=0) == SHAPE and call(cols=1 << 20, ldx=1 << 20, ldw=1 << 20) == SHAPE and call(ldx=56) == SHAPE and call(ldw=56) == SHAPE and call(ldx=1 << 22) == SHAPE
         assert call(ldw=1 << 22) == SHAPE
+        # logits and inputs beyond what a grid of tiles holds
+        assert call(tokens=1 << 21, vocab=(1 << 16) + 1, k=1) == SHAPE and call(tokens=1 << 21, vocab=1 << 16, k=1, ws=None) == WORKSPACE
+        assert call(tokens=1 << 20, cols=(1 << 17) + 8, ldx=1 << 18, ldw=1 << 18, lddx=1 << 18, lddw=1 << 18, k=1) == SHAPE
         assert call(ldx=68) == LAYOUT and call(ldw=68) == LAYOUT and call(x=at(0x10008)) == LAYOUT and call(w=at(0x10008)) == LAYOUT and call(index=at(0x10004)) == LAYOUT
         assert call(lse=at(0x10002)) == LAYOUT and call(ws=at(0x10008)) == LAYOUT
         assert call(ws=None) == WORKSPACE and call(n=1000) == WORKSPACE

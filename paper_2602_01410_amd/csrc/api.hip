@@ -1,6 +1,7 @@
 // C-ABI layer: argument validation and dispatch.  No kernel code here.
 #include "../../include/snip.h"
 #include "snip_internal.h"
+#include <algorithm>
 #include <cmath>
 #include <mutex>
 

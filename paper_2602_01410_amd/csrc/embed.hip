@@ -22,6 +22,9 @@ constexpr int kMostRange = 512;          // token numbers of a workgroup of the 
 constexpr int kLong = 64;                // tokens of a row from which on it is summed in parts, and the tokens of a part
 constexpr int kHeld = 16;                // loads of 64 ids that a wave of the sort has under way; up to 64 of them for each wave ids are read once
 constexpr int kSegment = 512;            // columns of a wave: 8 per lane
+// Up to so many tokens a workgroup of every token looks for the others itself.  Added to 32000 x 4096, us, here and sorted: 16 tokens 2.9 and 11, 1003 8.3 and 17
+// (all of one number 9.5 and 18), 2048 18 and 25 (11 and 22); 4096 (without the list's limit) 93 and 38.
+constexpr int kFewTokens = 2048;
 
 template <bool I64> __device__ __forceinline__ int token(const void* ids, int64_t t, int vocab)      // -1: none
 {
@@ -189,16 +192,15 @@ __device__ __forceinline__ void sum_rows(const uint16_t* __restrict__ dy, int64_
     if (n & 1) sum_batch<1>(dy, ld, rows, i, c, sum);
 }
 
-// Block j: the places [j kLong, (j + 1) kLong) of the order.  Of the rows with more than kLong tokens two at most have tokens there: that of the first
+// Sum of the places [j kLong, (j + 1) kLong) of the order, for the rows with more than kLong tokens: two of them at most have tokens there, that of the first
 // place (partial sum 0) and, if it is another one, that of the last (1).
 template <bool I64>
-__global__ __launch_bounds__(64) void embed_partials_kernel(const uint16_t* __restrict__ dy, int64_t ld, int cols, int vocab, const void* __restrict__ ids,
-                                                            const int* __restrict__ start, const int* __restrict__ order, float* __restrict__ partials)
+__device__ __forceinline__ void sum_part(const uint16_t* __restrict__ dy, int64_t ld, int cols, int vocab, const void* __restrict__ ids, const int* __restrict__ start,
+                                         const int* __restrict__ order, int j, int c, float* __restrict__ partials)
 {
-    const int all = start[vocab], p0 = blockIdx.x * kLong;
+    const int all = start[vocab], p0 = j * kLong, at = c < cols ? c : 0;      // (every lane holds a row's number)
     if (p0 >= all) return;
     const int p1 = all - p0 < kLong ? all : p0 + kLong;
-    const int c = blockIdx.y * kSegment + threadIdx.x * 8, at = c < cols ? c : 0;      // (every lane holds a row's number)
     const int v0 = token<I64>(ids, order[p0], vocab), v1 = token<I64>(ids, order[p1 - 1], vocab);
 #pragma unroll
     for (int slot = 0; slot < 2; ++slot) {
@@ -208,21 +210,31 @@ __global__ __launch_bounds__(64) void embed_partials_kernel(const uint16_t* __re
         if (e - s <= kLong) continue;
         float sum[8] = {};
         sum_rows(dy, ld, order, s > p0 ? s : p0, e < p1 ? e : p1, at, sum);
-        if (c < cols) store8(partials + ((int64_t)blockIdx.x * 2 + slot) * cols + c, sum);
+        if (c < cols) store8(partials + ((int64_t)j * 2 + slot) * cols + c, sum);
     }
 }
+template <class T> __device__ __forceinline__ void store_row(T* p, float (&sum)[8], float scale, bool add)
+{
+    float old[8] = {};
+    if (add) load8(p, old);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = fmaf(sum[i], scale, old[i]);
+    store8(p, sum);
+}
 
-// BY_TOKEN (a gradient that is added to): a wave for each place in the order and 512 columns, which has something to do where a number's tokens begin;
-// otherwise for each row of the table.
+// A wave for each 512 columns of `parts` parts of long rows and of, behind them, each row of the table or (BY_TOKEN, a gradient that is added to) each
+// place in the order, which has something to do where a number's tokens begin.
 template <class T, bool BY_TOKEN, bool I64>
 __global__ __launch_bounds__(256) void embed_rows_kernel(const uint16_t* __restrict__ dy, int64_t ld, int cols, int vocab, int tokens, const void* __restrict__ ids, float scale,
-                                                         const int* __restrict__ start, const int* __restrict__ order, const float* __restrict__ partials,
+                                                         const int* __restrict__ start, const int* __restrict__ order, float* __restrict__ partials, int parts,
                                                          T* __restrict__ dw, int64_t lddw, int segments)
 {
-    const int64_t units = (int64_t)(BY_TOKEN ? tokens : vocab) * segments;
+    const int64_t units = ((int64_t)parts + (BY_TOKEN ? tokens : vocab)) * segments;
     for (int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); u < units; u += (int64_t)gridDim.x * 4) {
         int v = __builtin_amdgcn_readfirstlane((int)(u / segments));
         const int c = (int)(u % segments) * kSegment + (threadIdx.x & 63) * 8, at = c < cols ? c : 0;
+        if (v < parts) { sum_part<I64>(dy, ld, cols, vocab, ids, start, order, v, c, partials); continue; }
+        v -= parts;
         if (BY_TOKEN) {
             const int place = v;
             if (place >= start[vocab]) continue;
@@ -230,27 +242,121 @@ __global__ __launch_bounds__(256) void embed_rows_kernel(const uint16_t* __restr
             if (start[v] != place) continue;
         }
         const int s = __builtin_amdgcn_readfirstlane(start[v]), e = __builtin_amdgcn_readfirstlane(start[v + 1]);
+        if (e - s > kLong) continue;
         float sum[8] = {};
-        if (e - s <= kLong) {
-            sum_rows(dy, ld, order, s, e, at, sum);
-        } else {
-            const int last = (e - 1) / kLong;
-#pragma unroll 4
-            for (int j = s / kLong; j <= last; ++j) {
-                float f[8];
-                load8(partials + ((int64_t)j * 2 + (j * kLong < s)) * cols + at, f);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) sum[i] += f[i];
-            }
-        }
-        if (c >= cols) continue;
-        T* p = dw + (int64_t)v * lddw + c;
-        float old[8] = {};
-        if (BY_TOKEN) load8(p, old);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum[i] = fmaf(sum[i], scale, old[i]);
-        store8(p, sum);
+        sum_rows(dy, ld, order, s, e, at, sum);
+        if (c < cols) store_row(dw + (int64_t)v * lddw + c, sum, scale, BY_TOKEN);
     }
+}
+
+// The long rows from their partial sums: that which begins among the places of block j, if there is one; it goes on behind them.
+template <class T, bool I64>
+__global__ __launch_bounds__(64) void embed_long_kernel(int cols, int vocab, const void* __restrict__ ids, float scale, const int* __restrict__ start, const int* __restrict__ order,
+                                                        const float* __restrict__ partials, T* __restrict__ dw, int64_t lddw, bool add)
+{
+    const int all = start[vocab], p0 = blockIdx.x * kLong, p1 = p0 + kLong, c = blockIdx.y * kSegment + threadIdx.x * 8;
+    if (p1 >= all || c >= cols) return;
+    const int v = token<I64>(ids, order[p1 - 1], vocab), s = start[v], e = start[v + 1], last = (e - 1) / kLong;
+    if (s < p0 || e - s <= kLong) return;
+    float sum[8] = {};
+#pragma unroll 4
+    for (int j = blockIdx.x; j <= last; ++j) {
+        float f[8];
+        load8(partials + ((int64_t)j * 2 + (j * kLong < s)) * cols + c, f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += f[i];
+    }
+    store_row(dw + (int64_t)v * lddw + c, sum, scale, add);
+}
+
+// Few tokens: a workgroup for each token and 2048 columns looks through all ids itself and lists the tokens of its number in their order.  Up to kLong of
+// them are summed by the first one's workgroup, a wave for each 512 columns.  Of more, every one's workgroup takes SLICE columns, and SLICE / 8 threads each
+// kLong of the tokens, whose sums are added in turn.  The table is zero before, or added to.
+template <class T, bool I64, int FEW>
+__global__ __launch_bounds__(256) void embed_few_kernel(const uint16_t* __restrict__ dy, int64_t ld, int cols, int vocab, int tokens, const void* __restrict__ ids, float scale,
+                                                        T* __restrict__ dw, int64_t lddw, bool add)
+{
+    constexpr int HELD = FEW / 256, GROUPS = FEW / kLong, SLICE = 256 / GROUPS * 8;
+    __shared__ int list[FEW];
+    __shared__ int counts[4], befores[4];
+    __shared__ float sums[GROUPS][SLICE];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), me = blockIdx.x;
+    const int v = token<I64>(ids, me, vocab);
+    const unsigned long long lower = (1ull << lane) - 1;
+    int held[HELD];
+    auto place = [&](int i) { return wave * (FEW / 4) + i * 64 + lane; };
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) held[i] = place(i) < tokens ? token<I64>(ids, place(i), vocab) : -1;
+    if (v < 0) return;
+    unsigned long long same[HELD];
+    int n = 0, before = 0;
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+        same[i] = __builtin_amdgcn_ballot_w64(held[i] == v);
+        n += __builtin_popcountll(same[i]);
+        before += __builtin_popcountll(__builtin_amdgcn_ballot_w64(held[i] == v && place(i) < me));
+    }
+    if (lane == 0) { counts[wave] = n; befores[wave] = before; }
+    __syncthreads();
+    int at = 0, all = 0, rank = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        at += w < wave ? counts[w] : 0;
+        all += counts[w];
+        rank += befores[w];
+    }
+    if (all <= kLong ? rank != 0 : blockIdx.y != 0) return;
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+        if (same[i] >> lane & 1) list[at + __builtin_popcountll(same[i] & lower)] = place(i);
+        at += __builtin_popcountll(same[i]);
+    }
+    __syncthreads();
+    T* row = dw + (int64_t)v * lddw;
+    if (all <= kLong) {
+        const int c = (blockIdx.y * 4 + wave) * kSegment + lane * 8;
+        float sum[8] = {};
+        sum_rows(dy, ld, list, 0, all, c < cols ? c : 0, sum);
+        if (c < cols) store_row(row + c, sum, scale, add);
+        return;
+    }
+    const int group = threadIdx.x / (SLICE / 8), mine = threadIdx.x % (SLICE / 8) * 8, many = all - group * kLong < kLong ? all - group * kLong : kLong;
+    for (int64_t c0 = (int64_t)rank * SLICE; c0 < cols; c0 += (int64_t)all * SLICE) {
+        const int c = (int)c0 + mine;
+        float sum[8] = {};
+        if (c < cols)
+            for (int i = 0; i < many; i += 16) {
+                uint4 raw[16];
+#pragma unroll
+                for (int b = 0; b < 16; ++b) raw[b] = *(const uint4*)(dy + list[group * kLong + (i + b < many ? i + b : many - 1)] * ld + c);
+#pragma unroll
+                for (int b = 0; b < 16; ++b) {
+                    float f[8];
+                    unpack2(raw[b].x, f[0], f[1]); unpack2(raw[b].y, f[2], f[3]); unpack2(raw[b].z, f[4], f[5]); unpack2(raw[b].w, f[6], f[7]);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) sum[k] += i + b < many ? f[k] : 0.f;
+                }
+            }
+        store8(&sums[group][mine], sum);
+        __syncthreads();
+        if (group == 0 && c < cols) {
+            for (int g = 1; g < GROUPS && g * kLong < all; ++g) {
+                float f[8];
+                load8(&sums[g][mine], f);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) sum[k] += f[k];
+            }
+            store_row(row + c, sum, scale, add);
+        }
+        __syncthreads();
+    }
+}
+
+template <class T> __global__ __launch_bounds__(256) void embed_zero_kernel(T* __restrict__ dw, int64_t rows, int cols, int64_t ld)
+{
+    const float zero[8] = {};
+    const int chunks = cols / 8;
+    for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < rows * chunks; u += (int64_t)gridDim.x * 256) store8(dw + u / chunks * ld + u % chunks * 8, zero);
 }
 
 int sort_range(int64_t vocab)
@@ -260,6 +366,35 @@ int sort_range(int64_t vocab)
     return r;
 }
 size_t to256(size_t n) { return (n + 255) / 256 * 256; }
+dim3 blocks_of(int64_t n) { return dim3((unsigned)(n < kMostBlocks ? n : kMostBlocks)); }
+
+template <class T> hipError_t launch_grad(const EmbedGradArgs& a, T* dw, hipStream_t s)
+{
+    const int segments = (a.cols + kSegment - 1) / kSegment, parts = (int)((a.tokens + kLong - 1) / kLong);
+    const int vocab = (int)a.vocab, tokens = (int)a.tokens;
+    if (a.tokens <= kFewTokens) {
+        if (!a.add) hipLaunchKernelGGL(embed_zero_kernel<T>, blocks_of((a.vocab * (a.cols / 8) + 255) / 256), dim3(256), 0, s, dw, a.vocab, a.cols, a.lddw);
+        if (tokens > 0)
+            hipLaunchKernelGGL((tokens <= kFewTokens / 2 ? a.ids64 ? embed_few_kernel<T, true, kFewTokens / 2> : embed_few_kernel<T, false, kFewTokens / 2>
+                                                         : a.ids64 ? embed_few_kernel<T, true, kFewTokens> : embed_few_kernel<T, false, kFewTokens>),
+                               dim3((unsigned)tokens, (unsigned)((segments + 3) / 4)), dim3(256), 0, s, a.dy, a.ld, a.cols, vocab, tokens, a.ids, a.scale, dw, a.lddw, a.add);
+        return hipGetLastError();
+    }
+    uint8_t* ws = (uint8_t*)a.workspace;
+    int* start = (int*)ws;
+    int* order = (int*)(ws + to256((size_t)(a.vocab + 1) * 4));
+    float* partials = (float*)(ws + to256((size_t)(a.vocab + 1) * 4) + to256((size_t)a.tokens * 4));
+    const int range = sort_range(a.vocab);
+    hipLaunchKernelGGL(a.ids64 ? embed_sort_kernel<true> : embed_sort_kernel<false>, dim3((unsigned)((a.vocab + range - 1) / range)), dim3(kSortThreads), 0, s,
+                       a.ids, tokens, vocab, range, start, order);
+    const dim3 grid = blocks_of(((parts + (a.add ? a.tokens : a.vocab)) * segments + 3) / 4);
+    auto rows = [&](auto* kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a.dy, a.ld, a.cols, vocab, tokens, a.ids, a.scale, start, order, partials, parts, dw, a.lddw, segments); };
+    if (a.add) a.ids64 ? rows(embed_rows_kernel<T, true, true>) : rows(embed_rows_kernel<T, true, false>);
+    else       a.ids64 ? rows(embed_rows_kernel<T, false, true>) : rows(embed_rows_kernel<T, false, false>);
+    hipLaunchKernelGGL((a.ids64 ? embed_long_kernel<T, true> : embed_long_kernel<T, false>), dim3((unsigned)parts, (unsigned)segments), dim3(64), 0, s, a.cols, vocab, a.ids, a.scale, start,
+                       order, partials, dw, a.lddw, a.add);
+    return hipGetLastError();
+}
 
 }  // namespace
 
@@ -283,31 +418,8 @@ hipError_t launch_embed(const EmbedArgs& a, hipStream_t s)
 
 hipError_t launch_embed_backward(const EmbedGradArgs& a, hipStream_t s)
 {
-    uint8_t* ws = (uint8_t*)a.workspace;
-    int* start = (int*)ws;
-    int* order = (int*)(ws + to256((size_t)(a.vocab + 1) * 4));
-    float* partials = (float*)(ws + to256((size_t)(a.vocab + 1) * 4) + to256((size_t)a.tokens * 4));
-    const int range = sort_range(a.vocab), segments = (a.cols + kSegment - 1) / kSegment;
-    hipLaunchKernelGGL(a.ids64 ? embed_sort_kernel<true> : embed_sort_kernel<false>, dim3((unsigned)((a.vocab + range - 1) / range)), dim3(kSortThreads), 0, s,
-                       a.ids, (int)a.tokens, (int)a.vocab, range, start, order);
-    if (a.tokens > kLong)
-        hipLaunchKernelGGL(a.ids64 ? embed_partials_kernel<true> : embed_partials_kernel<false>, dim3((unsigned)((a.tokens + kLong - 1) / kLong), (unsigned)segments),
-                           dim3(64), 0, s, a.dy, a.ld, a.cols, (int)a.vocab, a.ids, start, order, partials);
-    const int64_t blocks = ((a.add ? a.tokens : a.vocab) * segments + 3) / 4;
-    if (blocks == 0) return hipGetLastError();
-    const dim3 grid((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks));
-    auto rows = [&](auto* dw, auto* kernel) {
-        hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a.dy, a.ld, a.cols, (int)a.vocab, (int)a.tokens, a.ids, a.scale, start, order, partials, dw, a.lddw, segments);
-    };
-    auto typed = [&](auto* dw) {
-        using T = std::remove_pointer_t<decltype(dw)>;
-        if (!a.add)       rows(dw, embed_rows_kernel<T, false, false>);
-        else if (a.ids64) rows(dw, embed_rows_kernel<T, true, true>);
-        else              rows(dw, embed_rows_kernel<T, true, false>);
-    };
-    if (a.dw_fp32) typed((float*)a.dw);
-    else           typed((uint16_t*)a.dw);
-    return hipGetLastError();
+    if (a.dw_fp32) return launch_grad(a, (float*)a.dw, s);
+    return launch_grad(a, (uint16_t*)a.dw, s);
 }
 
 }  // namespace snip

@@ -45,7 +45,13 @@ GRADS = [  # tokens, cols, vocab, pad, out, index, scale, accumulate, what the n
     (129, 64, 9, 0, torch.float32, torch.int64, 1.0, False, "one"), (4096, 136, 700, 0, torch.bfloat16, torch.int64, 0.5, True, "text"),
     (5000, 64, 130000, 0, torch.float32, torch.int64, 1.0, False, "text"), (3000, 512, 515, 0, torch.float32, torch.int32, 1.0, False, "runs"),
     (500, 64, 40, 0, torch.float32, torch.int64, 1.0, False, "none"), (0, 64, 40, 0, torch.float32, torch.int64, 1.0, False, "any"),
-    (0, 64, 40, 0, torch.float32, torch.int64, 1.0, True, "any")]
+    (0, 64, 40, 0, torch.float32, torch.int64, 1.0, True, "any"),
+    # on both sides of what a workgroup of every token looks through
+    (1023, 2056, 3, 0, torch.float32, torch.int32, 1.0, True, "any"), (1024, 4104, 900, 8, torch.bfloat16, torch.int64, 0.7, False, "text"),
+    (1024, 520, 9, 0, torch.bfloat16, torch.int64, 1.0, True, "one"), (70, 9000, 9, 0, torch.float32, torch.int64, 1.0, False, "one"), (1025, 520, 9, 0, torch.float32, torch.int64, 1.0, True, "one"),
+    (1025, 2056, 3, 24, torch.float32, torch.int32, 1.0, True, "any"), (2500, 1032, 900, 8, torch.bfloat16, torch.int32, 0.7, False, "text"), (2048, 264, 1500, 0, torch.float32, torch.int64, 1.0, True, "text"),
+    (2048, 264, 15, 8, torch.bfloat16, torch.int32, 1.0, False, "one"), (2049, 264, 15, 0, torch.float32, torch.int64, 1.0, True, "one"),
+    (1025, 72, 4000, 0, torch.float32, torch.int64, 1.0, False, "none")]
 
 
 @pytest.mark.parametrize("tokens, cols, vocab, pad, out, index, scale, add, kind", GRADS)
@@ -85,18 +91,18 @@ def test_gradient(tokens, cols, vocab, pad, out, index, scale, add, kind):
         assert torch.equal(again, got)                      # one order of the sums
 
 
-def test_order_of_tokens():
+@pytest.mark.parametrize("tokens, add", [(5000, False), (1000, False), (1000, True), (2000, True), (5000, True)])
+def test_order_of_tokens(tokens, add):
     """Tokens of a number are added in their order, also where many waves look through the numbers: a sum that depends on it."""
     snip = require_gpu()
-    tokens = 5000
     dy = torch.zeros(tokens, 8, dtype=torch.bfloat16, device="cuda")
-    ids = torch.arange(tokens, device="cuda") % 1000 + 3
-    picked = (ids == 500).nonzero()[:, 0]
+    ids = torch.arange(tokens, device="cuda") % (tokens // 5) + 3
+    picked = (ids == tokens // 10).nonzero()[:, 0]
     assert len(picked) == 5
     for t, v in zip(picked.tolist(), [2.0 ** 30, 1.0, 1.0, -2.0 ** 30, 3.0]):
         dy[t] = v                            # in order, in fp32: 2^30 takes up the ones
-    got = snip.snip_embed_backward(dy, ids, 1200)
-    assert torch.all(got[500] == 3.0) and torch.count_nonzero(got) == 8
+    got = snip.snip_embed_backward(dy, ids, 1200, dw=torch.zeros(1200, 8, device="cuda"), accumulate=add)
+    assert torch.all(got[tokens // 10] == 3.0) and torch.count_nonzero(got) == 8
 
 
 def test_streams_and_graph():

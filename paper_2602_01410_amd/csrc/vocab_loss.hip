@@ -38,7 +38,7 @@ struct ProductArgs {
     const int* starts; const int2* items; int64_t items_pitch; int vocab_tiles;
     int v0, vocab;               // entry of A's first row
     float2* tile_stats;          // stats: [tiles_i][J], (largest s log2 e, sum of 2^(s log2 e - that))
-    float* z;                    // stats: of every named entry
+    float* z;                    // stats: of every named entry, by its place
     const float* lse;            // dz
     const float* part;           // dz: dloss tau of every token in units of *unit, zero for those that take no part
     const float* unit;           // dw
@@ -533,15 +533,82 @@ __global__ __launch_bounds__(T::NT, T::PER_CU) void product_kernel(const Product
     }
 }
 
-// What a distillation names, a wave per token: entries (-1 where there is nothing: outside the vocabulary, q = 0, or one named before, which has its q
-// added), q, the entropy term sum q log q, and for the gradient dloss tau, zero where no entry counts.
+__device__ __forceinline__ float logit(const void* teacher, bool fp32, int64_t at)
+{
+    return fp32 ? ((const float*)teacher)[at] : __uint_as_float((unsigned)((const uint16_t*)teacher)[at] << 16);
+}
+__device__ __forceinline__ float over_wave(float v) { for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d); return v; }
+__device__ __forceinline__ float top_of_wave(float v) { for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d)); return v; }
+
+// dloss tau of a token, zero where it has no target.
+struct Weights {
+    const void* targets; int target64, vocab;
+    const float* dloss;
+    float tau;
+    __device__ __forceinline__ float operator()(int t) const
+    {
+        if (targets) {
+            const int64_t at = target64 ? ((const int64_t*)targets)[t] : (int64_t)((const int*)targets)[t];
+            if (at < 0 || at >= vocab) return 0.f;
+        }
+        return dloss ? dloss[t] * tau : tau;
+    }
+};
+// The largest of them that is finite, or 1: the unit that dz is held in.  dz is rounded to bf16, and at the entry that is wanted it is near -1 times the
+// token's weight: exact in this unit where all weights are equal (a mean), and otherwise with the largest ones where bf16's relative steps are smallest.
+// Relative error of dw in bf16, its own rounding included, weights from 0.5 to 1.5: 0.0025 -> 0.0022; equal ones 0.0024 -> 0.0017.
+template <int NT> __device__ __forceinline__ float unit_of(const Weights& w, int tokens, float* shared)
+{
+    float top = 0.f;
+#pragma unroll 4
+    for (int t = threadIdx.x; t < tokens; t += NT) {
+        const float v = fabsf(w(t));
+        top = v < INFINITY ? fmaxf(top, v) : top;
+    }
+    top = top_of_wave(top);
+    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = top;
+    __syncthreads();
+    for (int i = 0; i < NT / 64; ++i) top = fmaxf(top, shared[i]);
+    return top > 0.f ? top : 1.f;
+}
+__global__ __launch_bounds__(1024) void unit_kernel(const Weights w, int tokens, float* __restrict__ unit)
+{
+    __shared__ float shared[16];
+    const float u = unit_of<1024>(w, tokens, shared);
+    if (threadIdx.x == 0) *unit = u;
+}
+// Every token's weight in that unit, and x without the rows of tokens that take no part (it may hold anything there), by a wave.
+__device__ __forceinline__ void take_part(int t, float weight, float unit, const uint16_t* __restrict__ x, int64_t ld, int cols, float* __restrict__ part, uint16_t* __restrict__ out)
+{
+    const int lane = threadIdx.x & 63;
+    const float g = __fdiv_rn(weight, unit);
+    if (lane == 0) part[t] = g;
+    if (out)
+        for (int c = lane * 8; c < cols; c += 512)
+            *reinterpret_cast<uint4*>(out + (int64_t)t * cols + c) = g == 0.f ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4*>(x + t * ld + c);
+}
+// `find`: every workgroup finds the unit itself (a launch less).
+__global__ __launch_bounds__(256) void part_kernel(const uint16_t* __restrict__ x, int64_t ld, int tokens, int cols, const Weights w, bool find, float* __restrict__ unit,
+                                                   float* __restrict__ part, uint16_t* __restrict__ out)
+{
+    __shared__ float shared[4];
+    const float u = find ? unit_of<256>(w, tokens, shared) : *unit;
+    if (find && blockIdx.x == 0 && threadIdx.x == 0) *unit = u;
+    for (int t = blockIdx.x * 4 + (threadIdx.x >> 6); t < tokens; t += gridDim.x * 4) take_part(t, w(t), u, x, ld, cols, part, out);
+}
+
+// What a distillation's gradient needs of every token, a wave for each: entries (-1 where there is nothing: outside the vocabulary, q = 0, or one named
+// before, which has its q added) and q, and what part_kernel forms for targets; no entry that counts, no part.
 template <bool I64>
 __global__ __launch_bounds__(256) void entries_kernel(const void* __restrict__ indices, const void* __restrict__ teacher, bool teacher_fp32, int tokens, int vocab,
-                                                      int k, float tau, const float* __restrict__ dloss, int* __restrict__ index, float* __restrict__ q,
-                                                      float* __restrict__ entropy, float* __restrict__ coef)
+                                                      int k, float tau, int* __restrict__ index, float* __restrict__ q, const uint16_t* __restrict__ x, int64_t ld, int cols,
+                                                      const Weights weights, bool find, float* __restrict__ unit, float* __restrict__ part, uint16_t* __restrict__ out)
 {
     __shared__ int numbers[4][1024];
     __shared__ float wants[4][1024];
+    __shared__ float shared[4];
+    const float unit_ = find ? unit_of<256>(weights, tokens, shared) : *unit;
+    if (find && blockIdx.x == 0 && threadIdx.x == 0) *unit = unit_;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const float alpha = 1.f / tau;
     for (int t = blockIdx.x * 4 + wave; t < tokens; t += gridDim.x * 4) {
@@ -550,33 +617,27 @@ __global__ __launch_bounds__(256) void entries_kernel(const void* __restrict__ i
         bool any = false;
         for (int j = lane; j < k; j += 64) {
             const int64_t v = I64 ? ((const int64_t*)indices)[row + j] : ((const int*)indices)[row + j];
-            const float u = (teacher_fp32 ? ((const float*)teacher)[row + j] : __uint_as_float((unsigned)((const uint16_t*)teacher)[row + j] << 16)) * alpha;
+            const float u = logit(teacher, teacher_fp32, row + j) * alpha;
             const bool is = v >= 0 && v < vocab;
             numbers[wave][j] = is ? (int)v : -1;
             wants[wave][j] = u;
             any = any || (is && !(u == -INFINITY));
             if (is) top = fmaxf(top, u);
         }
-        for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+        top = top_of_wave(top);
         any = __builtin_amdgcn_ballot_w64(any) != 0;
         const float base = top == -INFINITY ? 0.f : top;
         float sum = 0.f;
         for (int j = lane; j < k; j += 64)
             if (numbers[wave][j] >= 0) sum += expf(wants[wave][j] - base);
-        for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+        sum = over_wave(sum);
         const float log_sum = logf(sum);
-        float ent = 0.f;
         for (int j = lane; j < k; j += 64) {
             float w = 0.f;
-            if (any && numbers[wave][j] >= 0) {
-                const float l = wants[wave][j] - base - log_sum;
-                w = expf(l);
-                if (w != 0.f) ent += w * l;
-            }
+            if (any && numbers[wave][j] >= 0) w = expf(wants[wave][j] - base - log_sum);
             if (w == 0.f) numbers[wave][j] = -1;
             wants[wave][j] = w;
         }
-        for (int d = 32; d > 0; d >>= 1) ent += __shfl_xor(ent, d);
         for (int j = lane; j < k; j += 64) {
             const int v = numbers[wave][j];
             float w = 0.f;
@@ -590,29 +651,31 @@ __global__ __launch_bounds__(256) void entries_kernel(const void* __restrict__ i
             index[row + j] = before ? -1 : v;
             q[row + j] = before ? 0.f : w;
         }
-        if (lane == 0) {
-            if (entropy) entropy[t] = ent;
-            if (coef) coef[t] = any ? (dloss ? dloss[t] : 1.f) * tau : 0.f;
-        }
+        take_part(t, any ? weights(t) : 0.f, unit_, x, ld, cols, part, out);
     }
 }
 
 // Lists of the entries by tile: a workgroup for each `tn` tokens counts the entries of every vocabulary tile (1 << log_tm entries), forms their places
-// and writes them.  The order within a tile's run varies; no two items of a run are of one element.
+// and writes them, with q or, without, with their place among all.  The order within a tile's run varies; two items of one element have places of their own.
 constexpr int kMostTiles = 1 << 14;
-__global__ __launch_bounds__(1024) void lists_kernel(const int* __restrict__ index, const float* __restrict__ q, int tokens, int k, int tn, int log_tm, int tiles,
-                                                     bool want_q, int* __restrict__ starts, int2* __restrict__ items)
+template <bool I64>
+__global__ __launch_bounds__(1024) void lists_kernel(const void* __restrict__ index, const float* __restrict__ q, int tokens, int vocab, int k, int tn, int log_tm, int tiles,
+                                                     int* __restrict__ starts, int2* __restrict__ items)
 {
     __shared__ int counts[kMostTiles];
     __shared__ int sums[16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int t0 = blockIdx.x * tn, here = min(tn, tokens - t0) * k;
     const int64_t base = (int64_t)t0 * k;
+    auto number = [&](int i) {
+        const int64_t v = I64 ? ((const int64_t*)index)[base + i] : (int64_t)((const int*)index)[base + i];
+        return v >= 0 && v < vocab ? (int)v : -1;
+    };
     for (int i = threadIdx.x; i < tiles; i += 1024) counts[i] = 0;
     __syncthreads();
 #pragma unroll 4
     for (int i = threadIdx.x; i < here; i += 1024) {
-        const int v = index[base + i];
+        const int v = number(i);
         if (v >= 0) atomicAdd(&counts[v >> log_tm], 1);
     }
     __syncthreads();
@@ -639,18 +702,18 @@ __global__ __launch_bounds__(1024) void lists_kernel(const int* __restrict__ ind
     }
     if (threadIdx.x == 0) out[tiles] = before;
     for (int i = threadIdx.x; i < here; i += 1024) {
-        const int v = index[base + i];
+        const int v = number(i);
         if (v < 0) continue;
         const int at = atomicAdd(&counts[v >> log_tm], 1);
-        items[base + at] = make_int2((v & ((1 << log_tm) - 1)) << 16 | i / k, want_q ? __float_as_int(q[base + i]) : (int)(base + i));
+        items[base + at] = make_int2((v & ((1 << log_tm) - 1)) << 16 | i / k, q ? __float_as_int(q[base + i]) : (int)(base + i));
     }
 }
 
 // The tiles' sums joined and the loss formed: TOK tokens of a workgroup, 256 / TOK threads of a token.
 template <int TOK>
 __global__ __launch_bounds__(256) void join_kernel(const float2* __restrict__ tile_stats, int tiles, int tokens, int vocab, float alpha, float tau, const void* __restrict__ targets,
-                                                   int target64, const int* __restrict__ index, const float* __restrict__ q, int k, const float* __restrict__ z,
-                                                   const float* __restrict__ entropy, float* __restrict__ loss, float* __restrict__ lse)
+                                                   int target64, const void* __restrict__ teacher, bool teacher_fp32, int k, const float* __restrict__ z, float* __restrict__ loss,
+                                                   float* __restrict__ lse)
 {
     constexpr int PARTS = 256 / TOK;
     __shared__ float2 shared[PARTS][TOK + 1];
@@ -659,7 +722,7 @@ __global__ __launch_bounds__(256) void join_kernel(const float2* __restrict__ ti
     // (what the loss names is fetched beside the sums)
     int64_t target = -1;
     float at_target = 0.f;
-    if (here && targets) {
+    if (here && !teacher) {
         target = target64 ? ((const int64_t*)targets)[t] : (int64_t)((const int*)targets)[t];
         at_target = z[t];
     }
@@ -682,76 +745,40 @@ __global__ __launch_bounds__(256) void join_kernel(const float2* __restrict__ ti
     const float l = fmaf(v.x, kLn2, logf(v.y));
     if (lse && part == 0 && here) lse[t] = l;
     if (!loss) return;
-    if (targets) {
+    if (!teacher) {
         if (part == 0 && here) loss[t] = target >= 0 && target < vocab ? l - at_target : 0.f;
         return;
     }
-    float sum = 0.f, any = 0.f;
-    if (here)
-        for (int j = part; j < k; j += PARTS) {
-            const int64_t at = (int64_t)t * k + j;
-            if (index[at] >= 0) {
-                sum = fmaf(q[at], fmaf(-z[at], alpha, l), sum);
-                any = 1.f;
+    // a wave for each token: q, and with it the loss (targets are the entries' numbers here)
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int i = wave; i < TOK; i += 4) {
+        const int token = blockIdx.x * TOK + i;
+        if (token >= tokens) break;
+        const int64_t row = (int64_t)token * k;
+        const float2 all = shared[0][i];
+        const float of_token = fmaf(all.x, kLn2, logf(all.y));
+        auto entry = [&](int j, float& u) {
+            const int64_t v = target64 ? ((const int64_t*)targets)[row + j] : (int64_t)((const int*)targets)[row + j];
+            u = logit(teacher, teacher_fp32, row + j) * alpha;
+            return v >= 0 && v < vocab && !(u == -INFINITY);
+        };
+        float top = -INFINITY, u, sum = 0.f, total = 0.f;
+        bool any = false;
+        for (int j = lane; j < k; j += 64)
+            if (entry(j, u)) { top = fmaxf(top, u); any = true; }
+        top = top_of_wave(top);
+        const float base = top == -INFINITY ? 0.f : top;
+        for (int j = lane; j < k; j += 64)
+            if (entry(j, u)) sum += expf(u - base);
+        const float log_sum = logf(over_wave(sum));
+        for (int j = lane; j < k; j += 64)
+            if (entry(j, u)) {
+                const float log_q = u - base - log_sum, q = expf(log_q);
+                // (a q that is zero has no part, whatever its logit)
+                if (q != 0.f) total = fmaf(q, log_q + fmaf(-z[row + j], alpha, of_token), total);
             }
-        }
-    __syncthreads();
-    shared[part][tok] = make_float2(sum, any);
-    __syncthreads();
-    if (part != 0 || !here) return;
-    for (int i = 1; i < PARTS; ++i) { sum += shared[i][tok].x; any += shared[i][tok].y; }
-    loss[t] = any > 0.f ? (sum + entropy[t]) * tau * tau : 0.f;
-}
-
-// dloss tau of a token, zero where it takes no part: of targets, or given.
-struct Weights {
-    const void* targets; int target64, vocab;
-    const float *dloss, *coef;
-    __device__ __forceinline__ float operator()(int t) const
-    {
-        if (!targets) return coef[t];
-        const int64_t at = target64 ? ((const int64_t*)targets)[t] : (int64_t)((const int*)targets)[t];
-        return at >= 0 && at < vocab ? (dloss ? dloss[t] : 1.f) : 0.f;
-    }
-};
-// The largest of them that is finite, or 1: the unit that dz is held in.  dz is rounded to bf16, and at the entry that is wanted it is near -1 times the
-// token's weight: exact in this unit where all weights are equal (a mean), and otherwise with the largest ones where bf16's relative steps are smallest.
-// Relative error of dw in bf16, its own rounding included, weights from 0.5 to 1.5: 0.0025 -> 0.0022; equal ones 0.0024 -> 0.0017.
-template <int NT> __device__ __forceinline__ float unit_of(const Weights& w, int tokens, float* shared)
-{
-    float top = 0.f;
-#pragma unroll 4
-    for (int t = threadIdx.x; t < tokens; t += NT) {
-        const float v = fabsf(w(t));
-        top = v < INFINITY ? fmaxf(top, v) : top;
-    }
-    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = top;
-    __syncthreads();
-    for (int i = 0; i < NT / 64; ++i) top = fmaxf(top, shared[i]);
-    return top > 0.f ? top : 1.f;
-}
-__global__ __launch_bounds__(1024) void unit_kernel(const Weights w, int tokens, float* __restrict__ unit)
-{
-    __shared__ float shared[16];
-    const float u = unit_of<1024>(w, tokens, shared);
-    if (threadIdx.x == 0) *unit = u;
-}
-// Every token's weight in that unit, and x without the rows of tokens that take no part (it may hold anything there); a wave per token.  `find`: every
-// workgroup finds the unit itself (a launch less).
-__global__ __launch_bounds__(256) void part_kernel(const uint16_t* __restrict__ x, int64_t ld, int tokens, int cols, const Weights w, bool find, float* __restrict__ unit,
-                                                   float* __restrict__ part, uint16_t* __restrict__ out)
-{
-    __shared__ float shared[4];
-    const int lane = threadIdx.x & 63;
-    const float u = find ? unit_of<256>(w, tokens, shared) : *unit;
-    if (find && blockIdx.x == 0 && threadIdx.x == 0) *unit = u;
-    for (int t = blockIdx.x * 4 + (threadIdx.x >> 6); t < tokens; t += gridDim.x * 4) {
-        const float g = __fdiv_rn(w(t), u);
-        if (lane == 0) part[t] = g;
-        if (out)
-            for (int c = lane * 8; c < cols; c += 512)
-                *reinterpret_cast<uint4*>(out + (int64_t)t * cols + c) = g == 0.f ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4*>(x + t * ld + c);
+        total = over_wave(total);
+        if (lane == 0) loss[token] = __builtin_amdgcn_ballot_w64(any) != 0 ? total * tau * tau : 0.f;
     }
 }
 
@@ -875,41 +902,40 @@ struct Space {
     }
 };
 // Lists of a distillation's entries (without a teacher there are none).
-struct Lists { int* index; float* q; int* starts; int2* items; };
+struct Lists { int* starts; int2* items; };
 Lists lists_space(const VocabLossArgs& a, Shape shape, Space& s)
 {
     Lists l = {};
     if (!a.distill) return l;
-    const size_t n = (size_t)a.tokens * a.k;
-    l.index = s.take<int>(n); l.q = s.take<float>(n); l.items = s.take<int2>(n);
+    l.items = s.take<int2>((size_t)a.tokens * a.k);
     l.starts = s.take<int>((up(a.tokens, tile_cols(shape)) / tile_cols(shape)) * (up(a.vocab, tile_rows(shape)) / tile_rows(shape) + 1));
     return l;
 }
 size_t lists_bytes(int64_t tokens, int64_t vocab, int64_t k)
 {
-    const size_t n = (size_t)tokens * k;
-    return 2 * to256(n * 4) + to256(n * 8) + to256((size_t)(up(tokens, 32) / 32) * (up(vocab, 128) / 128 + 1) * 4);
+    return to256((size_t)tokens * k * 8) + to256((size_t)(up(tokens, 32) / 32) * (up(vocab, 128) / 128 + 1) * 4);
 }
-struct Forward { Lists l; float *entropy, *z; float2* stats; Shape shape; size_t bytes; };
+struct Forward { Lists l; float* z; float2* stats; Shape shape; size_t bytes; };
 Forward forward_space(const VocabLossArgs& a)
 {
     Space s{(uint8_t*)a.workspace};
     Forward f;
     f.shape = shape_for(a.vocab, a.tokens, a.cols);
     f.l = lists_space(a, f.shape, s);
-    f.z = s.take<float>((size_t)a.tokens * a.k); f.entropy = s.take<float>(a.tokens);
+    f.z = s.take<float>((size_t)a.tokens * a.k);
     f.stats = s.take<float2>((size_t)(up(a.vocab, tile_rows(f.shape)) / tile_rows(f.shape)) * a.tokens);
     f.bytes = s.used;
     return f;
 }
-struct Backward { Lists l; float *coef, *part, *unit, *sums; uint16_t *x, *dz; Shape shape; size_t bytes; };
+struct Backward { Lists l; int* index; float *q, *part, *unit, *sums; uint16_t *x, *dz; Shape shape; size_t bytes; };
 Backward backward_space(const VocabLossArgs& a, const Plan& pl)
 {
     Space s{(uint8_t*)a.workspace};
     Backward b;
     b.shape = shape_for(std::min(pl.piece, a.vocab), a.tokens, a.cols);
     b.l = lists_space(a, b.shape, s);
-    b.coef = s.take<float>(a.distill ? a.tokens : 0); b.part = s.take<float>(a.tokens); b.unit = s.take<float>(1);
+    const size_t named = a.distill ? (size_t)a.tokens * a.k : 0;
+    b.index = s.take<int>(named); b.q = s.take<float>(named); b.part = s.take<float>(a.tokens); b.unit = s.take<float>(1);
     b.x = s.take<uint16_t>(a.tokens * a.cols);
     b.dz = s.take<uint16_t>(a.tokens * pl.piece);
     b.sums = s.take<float>((size_t)a.tokens * a.cols * pl.splits);
@@ -917,13 +943,11 @@ Backward backward_space(const VocabLossArgs& a, const Plan& pl)
     return b;
 }
 
-void launch_lists(const VocabLossArgs& a, const Lists& l, Shape shape, float* entropy, float* coef, hipStream_t s)
+template <bool I64> void launch_lists(const VocabLossArgs& a, const void* index, const float* q, const Lists& l, Shape shape, hipStream_t s)
 {
-    const int64_t blocks = (a.tokens + 3) / 4, tn = tile_cols(shape), tm = tile_rows(shape);
-    hipLaunchKernelGGL(a.index64 ? entries_kernel<true> : entries_kernel<false>, dim3((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks)), dim3(256), 0, s, a.indices, a.teacher,
-                       a.teacher_fp32 != 0, (int)a.tokens, (int)a.vocab, (int)a.k, a.tau, a.dloss, l.index, l.q, entropy, coef);
-    hipLaunchKernelGGL(lists_kernel, dim3((unsigned)((a.tokens + tn - 1) / tn)), dim3(1024), 0, s, l.index, l.q, (int)a.tokens, (int)a.k, (int)tn, tm == 256 ? 8 : 7,
-                       (int)((a.vocab + tm - 1) / tm), coef != nullptr, l.starts, l.items);
+    const int64_t tn = tile_cols(shape), tm = tile_rows(shape);
+    hipLaunchKernelGGL(lists_kernel<I64>, dim3((unsigned)((a.tokens + tn - 1) / tn)), dim3(1024), 0, s, index, q, (int)a.tokens, (int)a.vocab, (int)a.k, (int)tn, tm == 256 ? 8 : 7,
+                       (int)((a.vocab + tm - 1) / tm), l.starts, l.items);
 }
 void name_entries(ProductArgs& p, const VocabLossArgs& a, const Lists& l, Shape shape)
 {
@@ -940,20 +964,20 @@ size_t vocab_loss_backward_needed(const VocabLossArgs& a) { return backward_spac
 // Bounds of the above that grow with every extent.
 size_t vocab_loss_bytes(int64_t tokens, int64_t vocab, int64_t k)
 {
-    return lists_bytes(tokens, vocab, k) + to256((size_t)tokens * k * 4) + to256((size_t)tokens * 4) + to256((size_t)(up(vocab, 128) / 128) * tokens * 8);
+    return lists_bytes(tokens, vocab, k) + to256((size_t)tokens * k * 4) + to256((size_t)(up(vocab, 128) / 128) * tokens * 8);
 }
 size_t vocab_loss_backward_bytes(int64_t tokens, int64_t cols, int64_t vocab, int64_t k)
 {
     const int64_t piece = std::min(up(vocab, 256), kMostPiece), dz = std::min(tokens * piece, std::max(kPieceElements, tokens * kLeastPiece));
     const int64_t sums = std::min(std::max(tokens * cols, kSplitElements), tokens * cols * std::max<int64_t>(1, piece / 512));
-    return lists_bytes(tokens, vocab, k) + 2 * to256((size_t)tokens * 4) + 256 + to256((size_t)(tokens * cols) * 2) + to256((size_t)dz * 2) + to256((size_t)sums * 4);
+    return lists_bytes(tokens, vocab, k) + 2 * to256((size_t)tokens * k * 4) + to256((size_t)tokens * 4) + 256 + to256((size_t)(tokens * cols) * 2) + to256((size_t)dz * 2) + to256((size_t)sums * 4);
 }
 
 hipError_t launch_vocab_loss(const VocabLossArgs& a, hipStream_t s)
 {
     if (a.tokens == 0) return hipSuccess;
     const Forward f = forward_space(a);
-    if (a.distill) launch_lists(a, f.l, f.shape, f.entropy, nullptr, s);
+    if (a.distill) a.index64 ? launch_lists<true>(a, a.indices, nullptr, f.l, f.shape, s) : launch_lists<false>(a, a.indices, nullptr, f.l, f.shape, s);
     ProductArgs p = {};
     p.a = a.w; p.lda = a.ldw; p.I = (int)a.vocab; p.b = a.x; p.ldb = a.ldx; p.J = (int)a.tokens; p.R = (int)a.cols;
     name_entries(p, a, f.l, f.shape);
@@ -962,8 +986,8 @@ hipError_t launch_vocab_loss(const VocabLossArgs& a, hipStream_t s)
     if (e != hipSuccess) return e;
     const int tok = a.tokens >= 2048 ? 16 : 4;
     hipLaunchKernelGGL(tok == 16 ? join_kernel<16> : join_kernel<4>, dim3((unsigned)((a.tokens + tok - 1) / tok)), dim3(256), 0, s, f.stats,
-                       (int)((a.vocab + tile_rows(f.shape) - 1) / tile_rows(f.shape)), (int)a.tokens, (int)a.vocab, p.alpha, a.tau, p.targets, p.target64, f.l.index, f.l.q, (int)a.k, f.z,
-                       f.entropy, a.loss, a.lse);
+                       (int)((a.vocab + tile_rows(f.shape) - 1) / tile_rows(f.shape)), (int)a.tokens, (int)a.vocab, p.alpha, a.tau, a.indices, a.index64, a.distill ? a.teacher : nullptr,
+                       a.teacher_fp32 != 0, (int)a.k, f.z, a.loss, a.lse);
     return hipGetLastError();
 }
 
@@ -978,13 +1002,19 @@ hipError_t launch_vocab_loss_backward(const VocabLossArgs& a, hipStream_t s)
     }
     const Plan pl = plan_of(a);
     const Backward b = backward_space(a, pl);
-    if (a.distill) launch_lists(a, b.l, b.shape, nullptr, b.coef, s);
-    const Weights weights = {a.distill ? nullptr : a.indices, a.index64, (int)a.vocab, a.dloss, b.coef};
+    const Weights weights = {a.distill ? nullptr : a.indices, a.index64, (int)a.vocab, a.dloss, a.tau};
     const bool find = a.tokens <= 2048;
     if (!find) hipLaunchKernelGGL(unit_kernel, dim3(1), dim3(1024), 0, s, weights, (int)a.tokens, b.unit);
     const int64_t token_blocks = (a.tokens + 3) / 4;
-    hipLaunchKernelGGL(part_kernel, dim3((unsigned)(token_blocks < kMostBlocks ? token_blocks : kMostBlocks)), dim3(256), 0, s, a.x, a.ldx, (int)a.tokens, (int)a.cols, weights, find,
-                       b.unit, b.part, a.dw ? b.x : nullptr);
+    const dim3 grid((unsigned)(token_blocks < kMostBlocks ? token_blocks : kMostBlocks));
+    uint16_t* x = a.dw ? b.x : nullptr;
+    if (a.distill) {
+        hipLaunchKernelGGL(a.index64 ? entries_kernel<true> : entries_kernel<false>, grid, dim3(256), 0, s, a.indices, a.teacher, a.teacher_fp32 != 0, (int)a.tokens, (int)a.vocab,
+                           (int)a.k, a.tau, b.index, b.q, a.x, a.ldx, (int)a.cols, weights, find, b.unit, b.part, x);
+        launch_lists<false>(a, b.index, b.q, b.l, b.shape, s);
+    } else {
+        hipLaunchKernelGGL(part_kernel, grid, dim3(256), 0, s, a.x, a.ldx, (int)a.tokens, (int)a.cols, weights, find, b.unit, b.part, x);
+    }
     for (int64_t v0 = 0; v0 < a.vocab; v0 += pl.piece) {
         const int64_t here = std::min(pl.piece, a.vocab - v0);
         const uint16_t* w = a.w + v0 * a.ldw;

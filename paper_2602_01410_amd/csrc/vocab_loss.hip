@@ -62,6 +62,8 @@ using Large = Tile<256, 256, 128, 128, 5, 1>;
 using Middle = Tile<128, 128, 64, 64, 5, 2>;
 using Few64 = Tile<128, 64, 64, 32, 6, 2>;
 using Few32 = Tile<128, 32, 32, 32, 8, 2>;
+using Low64 = Tile<64, 64, 32, 32, 10, 2>;
+using Low32 = Tile<64, 32, 32, 16, 12, 2>;
 
 __device__ __forceinline__ unsigned pack2(float a, float b) { return __builtin_bit_cast(unsigned, bf16x2{(__bf16)a, (__bf16)b}); }
 
@@ -93,9 +95,10 @@ __device__ __forceinline__ v4i early_desc(const uint16_t* p, unsigned bytes)
 // One operand of a tile: ROWS indices from `row0` on, of which a wave multiplies W from wave_row on.  C copies of this wave and stage.
 // Not turned, a stage is ROWS rows of 128 bytes; 16-byte chunk c of row r lies at c ^ (r / 2 % 8), so that 16 lanes that read one chunk of 16 rows meet
 // all banks.  Turned it is 64 rows of ROWS elements; chunk c of row r lies at c ^ (r % 4 * 4) ^ (r / 8 % 2 * 2), so that the 16 rows that a turning
-// read takes 32 bytes of, eight apart in fours, meet all banks twice.
+// read takes 32 bytes of, eight apart in fours, meet all banks twice (of 64 elements, two rows to all banks: c ^ (r / 2 % 2 * 4) ^ (r / 8 % 2 * 2)).
 template <int ROWS, int W, bool TURNED, bool SINGLE> struct Operand {
     static constexpr int C = ROWS / 32, PAIR = !SINGLE && C % 2 == 0 ? 2 : 1, UNITS = C / PAIR, BLOCKS = W / 16, READS = BLOCKS * (TURNED ? 2 : 1);
+    static_assert(!TURNED || ROWS >= 64, "chunks enough to spread");
     const uint16_t* p;
     int64_t ld;
     int rows, R;                 // of the tile, of the contraction
@@ -134,7 +137,7 @@ template <int ROWS, int W, bool TURNED, bool SINGLE> struct Operand {
             for (int m = 0; m < BLOCKS; ++m) at[m] = row * ROWS * 2 + ((((wave_row / 16 + m) * 2 + (lane >> 1 & 1)) ^ spread(row)) * 16) + (lane & 1) * 8;
         }
     }
-    static __device__ __forceinline__ int spread(int row) { return (row & 3) * 4 ^ (row >> 3 & 1) * 2; }
+    static __device__ __forceinline__ int spread(int row) { return ROWS == 64 ? (row >> 1 & 1) * 4 ^ (row >> 3 & 1) * 2 : (row & 3) * 4 ^ (row >> 3 & 1) * 2; }
     static __device__ __forceinline__ constexpr unsigned early(int c) { return kEarly - (PAIR == 2 && c % 2 ? 1024 : 0); }
     // before the copies of stage s; past the contraction's end they bring zeros
     __device__ __forceinline__ void stage(int s)
@@ -817,15 +820,15 @@ template <bool FP32> __global__ __launch_bounds__(256) void zero_kernel(void* ou
 constexpr int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 size_t to256(size_t n) { return (n + 255) / 256 * 256; }
 
-enum class Shape { kLarge, kMiddle, kFew64, kFew32 };
-constexpr int tile_rows(Shape s) { return s == Shape::kLarge ? 256 : 128; }
-constexpr int tile_cols(Shape s) { return s == Shape::kLarge ? 256 : s == Shape::kMiddle ? 128 : s == Shape::kFew64 ? 64 : 32; }
+enum class Shape { kLarge, kMiddle, kFew64, kFew32, kLow64, kLow32 };
+constexpr int tile_rows(Shape s) { return s == Shape::kLarge ? 256 : s == Shape::kLow64 || s == Shape::kLow32 ? 64 : 128; }
+constexpr int tile_cols(Shape s) { return s == Shape::kLarge ? 256 : s == Shape::kMiddle ? 128 : s == Shape::kFew64 || s == Shape::kLow64 ? 64 : 32; }
 constexpr int64_t stages_of(int64_t n) { return (n + 63) / 64; }
 constexpr int64_t tiles_of(Shape s, int64_t I, int64_t J) { return up(I, tile_rows(s)) / tile_rows(s) * (up(J, tile_cols(s)) / tile_cols(s)); }
 // About how long `units` tiles of so many stages take, us: a stage and what comes before and behind them, for as many at a time as the chip holds.  Measured: 256 x
 // 256 1.45-1.6 us a stage and 8 (8192 x 4096 against 128000: 64 stages, 100 us a tile; dw of 250 tokens: 4 stages, 14.4), 128 x 128 by two workgroups of a
 // compute unit 1.1-1.4 and 2.5 (515 x 1024 against 8191: 16 stages, 21; dw of 250 tokens: 7.1).
-constexpr int64_t kUnits = 256;
+constexpr int64_t kUnits = 256, kLastLevelCache = 256 << 20;
 double tile_time(Shape s, int64_t units, int64_t stages)
 {
     return s == Shape::kLarge ? (double)((units + kUnits - 1) / kUnits) * (1.5 * stages + 8.4) : (double)((units + 2 * kUnits - 1) / (2 * kUnits)) * (1.2 * stages + 2.5);
@@ -834,10 +837,13 @@ Shape faster(int64_t I, int64_t J, int64_t R)
 {
     return tile_time(Shape::kLarge, tiles_of(Shape::kLarge, I, J), stages_of(R)) < tile_time(Shape::kMiddle, tiles_of(Shape::kMiddle, I, J), stages_of(R)) ? Shape::kLarge : Shape::kMiddle;
 }
-// The tile for I x J outputs of a contraction of R, J of them tokens: as narrow as they are few.
+// Tiles as narrow as tokens are few.
+Shape few(int64_t tokens, bool low) { return tokens <= 32 ? low ? Shape::kLow32 : Shape::kFew32 : tokens <= 64 ? low ? Shape::kLow64 : Shape::kFew64 : Shape::kMiddle; }
+// The tile for I x J outputs of a contraction of R, J of them tokens.  Few tokens: 64 rows where tiles of 128 are no more than one for each compute unit (16 tokens, loss of
+// 32000 x 2048: 34.0 us, 128 rows 37.3; of 50257 x 1024, 1.5 for each: 27.7 and 26.5).
 Shape shape_for(int64_t I, int64_t J, int64_t R)
 {
-    return J <= 32 ? Shape::kFew32 : J <= 64 ? Shape::kFew64 : J <= 128 ? Shape::kMiddle : faster(I, J, R);
+    return J <= 128 ? few(J, up(I, 128) / 128 <= kUnits) : faster(I, J, R);
 }
 
 template <class T, int OUT> hipError_t launch_product(ProductArgs p, int splits, hipStream_t s)
@@ -853,6 +859,8 @@ template <int OUT> hipError_t launch_product(const ProductArgs& p, Shape shape, 
     if constexpr (OUT != kDw) {
         if (shape == Shape::kFew64) return launch_product<Few64, OUT>(p, splits, s);
         if (shape == Shape::kFew32) return launch_product<Few32, OUT>(p, splits, s);
+        if (shape == Shape::kLow64) return launch_product<Low64, OUT>(p, splits, s);
+        if (shape == Shape::kLow32) return launch_product<Low32, OUT>(p, splits, s);
     }
     return launch_product<Middle, OUT>(p, splits, s);
 }
@@ -883,7 +891,9 @@ Plan plan_of(const VocabLossArgs& a)
         }
     };
     if (a.tokens <= 128) {
-        consider(shape_for(0, a.tokens, 0));
+        // (w of the piece comes from the last-level cache, where dz's pass has left it, or as it did there from memory.  16 tokens, 64 and 128 rows, us of the call:
+        // 50257 x 768 56 and 67, 128000 x 1024 124 and 132; 128000 x 2048 239 and 232, 128000 x 4096 452 and 432)
+        consider(few(a.tokens, first * a.cols * 2 <= kLastLevelCache));
     } else {
         consider(Shape::kLarge);
         consider(Shape::kMiddle);
@@ -913,7 +923,7 @@ Lists lists_space(const VocabLossArgs& a, Shape shape, Space& s)
 }
 size_t lists_bytes(int64_t tokens, int64_t vocab, int64_t k)
 {
-    return to256((size_t)tokens * k * 8) + to256((size_t)(up(tokens, 32) / 32) * (up(vocab, 128) / 128 + 1) * 4);
+    return to256((size_t)tokens * k * 8) + to256((size_t)(up(tokens, 32) / 32) * (up(vocab, 64) / 64 + 1) * 4);
 }
 struct Forward { Lists l; float* z; float2* stats; Shape shape; size_t bytes; };
 Forward forward_space(const VocabLossArgs& a)
@@ -946,7 +956,7 @@ Backward backward_space(const VocabLossArgs& a, const Plan& pl)
 template <bool I64> void launch_lists(const VocabLossArgs& a, const void* index, const float* q, const Lists& l, Shape shape, hipStream_t s)
 {
     const int64_t tn = tile_cols(shape), tm = tile_rows(shape);
-    hipLaunchKernelGGL(lists_kernel<I64>, dim3((unsigned)((a.tokens + tn - 1) / tn)), dim3(1024), 0, s, index, q, (int)a.tokens, (int)a.vocab, (int)a.k, (int)tn, tm == 256 ? 8 : 7,
+    hipLaunchKernelGGL(lists_kernel<I64>, dim3((unsigned)((a.tokens + tn - 1) / tn)), dim3(1024), 0, s, index, q, (int)a.tokens, (int)a.vocab, (int)a.k, (int)tn, tm == 256 ? 8 : tm == 128 ? 7 : 6,
                        (int)((a.vocab + tm - 1) / tm), l.starts, l.items);
 }
 void name_entries(ProductArgs& p, const VocabLossArgs& a, const Lists& l, Shape shape)
@@ -964,7 +974,7 @@ size_t vocab_loss_backward_needed(const VocabLossArgs& a) { return backward_spac
 // Bounds of the above that grow with every extent.
 size_t vocab_loss_bytes(int64_t tokens, int64_t vocab, int64_t k)
 {
-    return lists_bytes(tokens, vocab, k) + to256((size_t)tokens * k * 4) + to256((size_t)(up(vocab, 128) / 128) * tokens * 8);
+    return lists_bytes(tokens, vocab, k) + to256((size_t)tokens * k * 4) + to256((size_t)std::max(up(vocab, 128) / 128 * tokens, std::min(up(vocab, 64) / 64, 2 * kUnits) * std::min<int64_t>(tokens, 64)) * 8);
 }
 size_t vocab_loss_backward_bytes(int64_t tokens, int64_t cols, int64_t vocab, int64_t k)
 {

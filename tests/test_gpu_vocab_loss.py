@@ -136,6 +136,12 @@ def test_pieces_of_the_vocabulary(tokens, cols, vocab, k):
     check(require_gpu(), Case(tokens, cols, vocab, k, ignored=0.1))
 
 
+@pytest.mark.parametrize("tokens, cols, vocab, k", [(31, 72, 33001, 0), (31, 72, 33001, 9), (50, 136, 40001, 4), (1, 2056, 66001, 0), (20, 2056, 66001, 3), (50, 2056, 66001, 0)])
+def test_few_tokens(tokens, cols, vocab, k):
+    """Tiles of more rows, where there are many, and weights beyond the last-level cache."""
+    check(require_gpu(), Case(tokens, cols, vocab, k, index=torch.int32))
+
+
 def test_long_contraction_and_splits():
     check(require_gpu(), Case(520, 2080, 9001, 4, 2.0))
 

@@ -165,12 +165,21 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const void* __
     }
 }
 
-// Sum of dy's rows order[from ... to), kLong of them at most, at column c, in their order.
-template <int B> __device__ __forceinline__ void sum_batch(const uint16_t* __restrict__ dy, int64_t ld, int rows, int i, int c, float (&sum)[8])
+// Eight columns of a lane: from a on, or (APART) four from a and four from b on, so that a wave's stores of fp32 are whole runs.
+struct Columns { int a, b; };
+template <bool APART> __device__ __forceinline__ uint4 load_row(const uint16_t* row, Columns c)
+{
+    if (!APART) return *(const uint4*)(row + c.a);
+    const uint2 lo = *(const uint2*)(row + c.a), hi = *(const uint2*)(row + c.b);
+    return make_uint4(lo.x, lo.y, hi.x, hi.y);
+}
+
+// Sum of dy's rows order[from ... to), 64 of them at most, in their order.
+template <int B, bool APART> __device__ __forceinline__ void sum_batch(const uint16_t* __restrict__ dy, int64_t ld, int rows, int i, Columns c, float (&sum)[8])
 {
     uint4 raw[B];
 #pragma unroll
-    for (int b = 0; b < B; ++b) raw[b] = *(const uint4*)(dy + (int64_t)__builtin_amdgcn_readlane(rows, i + b) * ld + c);
+    for (int b = 0; b < B; ++b) raw[b] = load_row<APART>(dy + (int64_t)__builtin_amdgcn_readlane(rows, i + b) * ld, c);
 #pragma unroll
     for (int b = 0; b < B; ++b) {
         float f[8];
@@ -179,17 +188,18 @@ template <int B> __device__ __forceinline__ void sum_batch(const uint16_t* __res
         for (int k = 0; k < 8; ++k) sum[k] += f[k];
     }
 }
-__device__ __forceinline__ void sum_rows(const uint16_t* __restrict__ dy, int64_t ld, const int* __restrict__ order, int from, int to, int c, float (&sum)[8])
+template <bool APART = false>
+__device__ __forceinline__ void sum_rows(const uint16_t* __restrict__ dy, int64_t ld, const int* __restrict__ order, int from, int to, Columns c, float (&sum)[8])
 {
     const int n = to - from, lane = threadIdx.x & 63;
     if (n == 0) return;
     const int rows = order[from + (lane < n ? lane : n - 1)];
     int i = 0;
-    for (; i + 16 <= n; i += 16) sum_batch<16>(dy, ld, rows, i, c, sum);
-    if (n & 8) { sum_batch<8>(dy, ld, rows, i, c, sum); i += 8; }
-    if (n & 4) { sum_batch<4>(dy, ld, rows, i, c, sum); i += 4; }
-    if (n & 2) { sum_batch<2>(dy, ld, rows, i, c, sum); i += 2; }
-    if (n & 1) sum_batch<1>(dy, ld, rows, i, c, sum);
+    for (; i + 16 <= n; i += 16) sum_batch<16, APART>(dy, ld, rows, i, c, sum);
+    if (n & 8) { sum_batch<8, APART>(dy, ld, rows, i, c, sum); i += 8; }
+    if (n & 4) { sum_batch<4, APART>(dy, ld, rows, i, c, sum); i += 4; }
+    if (n & 2) { sum_batch<2, APART>(dy, ld, rows, i, c, sum); i += 2; }
+    if (n & 1) sum_batch<1, APART>(dy, ld, rows, i, c, sum);
 }
 
 // Sum of the places [j kLong, (j + 1) kLong) of the order, for the rows with more than kLong tokens: two of them at most have tokens there, that of the first
@@ -209,7 +219,7 @@ __device__ __forceinline__ void sum_part(const uint16_t* __restrict__ dy, int64_
         const int s = start[v], e = start[v + 1];
         if (e - s <= kLong) continue;
         float sum[8] = {};
-        sum_rows(dy, ld, order, s > p0 ? s : p0, e < p1 ? e : p1, at, sum);
+        sum_rows(dy, ld, order, s > p0 ? s : p0, e < p1 ? e : p1, Columns{at, 0}, sum);
         if (c < cols) store8(partials + ((int64_t)j * 2 + slot) * cols + c, sum);
     }
 }
@@ -221,6 +231,11 @@ template <class T> __device__ __forceinline__ void store_row(T* p, float (&sum)[
     for (int i = 0; i < 8; ++i) sum[i] = fmaf(sum[i], scale, old[i]);
     store8(p, sum);
 }
+__device__ __forceinline__ void store_half(float* p, const float* sum, float scale, bool add)
+{
+    const float4 old = add ? *(const float4*)p : make_float4(0.f, 0.f, 0.f, 0.f);
+    *(float4*)p = make_float4(fmaf(sum[0], scale, old.x), fmaf(sum[1], scale, old.y), fmaf(sum[2], scale, old.z), fmaf(sum[3], scale, old.w));
+}
 
 // A wave for each 512 columns of `parts` parts of long rows and of, behind them, each row of the table or (BY_TOKEN, a gradient that is added to) each
 // place in the order, which has something to do where a number's tokens begin.
@@ -229,11 +244,12 @@ __global__ __launch_bounds__(256) void embed_rows_kernel(const uint16_t* __restr
                                                          const int* __restrict__ start, const int* __restrict__ order, float* __restrict__ partials, int parts,
                                                          T* __restrict__ dw, int64_t lddw, int segments)
 {
+    constexpr bool APART = sizeof(T) == 4;
     const int64_t units = ((int64_t)parts + (BY_TOKEN ? tokens : vocab)) * segments;
     for (int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); u < units; u += (int64_t)gridDim.x * 4) {
         int v = __builtin_amdgcn_readfirstlane((int)(u / segments));
-        const int c = (int)(u % segments) * kSegment + (threadIdx.x & 63) * 8, at = c < cols ? c : 0;
-        if (v < parts) { sum_part<I64>(dy, ld, cols, vocab, ids, start, order, v, c, partials); continue; }
+        const int segment = (int)(u % segments) * kSegment, lane = threadIdx.x & 63;
+        if (v < parts) { sum_part<I64>(dy, ld, cols, vocab, ids, start, order, v, segment + lane * 8, partials); continue; }
         v -= parts;
         if (BY_TOKEN) {
             const int place = v;
@@ -244,8 +260,15 @@ __global__ __launch_bounds__(256) void embed_rows_kernel(const uint16_t* __restr
         const int s = __builtin_amdgcn_readfirstlane(start[v]), e = __builtin_amdgcn_readfirstlane(start[v + 1]);
         if (e - s > kLong) continue;
         float sum[8] = {};
-        sum_rows(dy, ld, order, s, e, at, sum);
-        if (c < cols) store_row(dw + (int64_t)v * lddw + c, sum, scale, BY_TOKEN);
+        T* row = dw + (int64_t)v * lddw;
+        const int a = segment + lane * (APART ? 4 : 8), b = a + kSegment / 2;
+        sum_rows<APART>(dy, ld, order, s, e, Columns{a < cols ? a : 0, b < cols ? b : 0}, sum);
+        if constexpr (!APART) {
+            if (a < cols) store_row(row + a, sum, scale, BY_TOKEN);
+        } else {
+            if (a < cols) store_half(row + a, sum, scale, BY_TOKEN);
+            if (b < cols) store_half(row + b, sum + 4, scale, BY_TOKEN);
+        }
     }
 }
 
@@ -316,7 +339,7 @@ __global__ __launch_bounds__(256) void embed_few_kernel(const uint16_t* __restri
     if (all <= kLong) {
         const int c = (blockIdx.y * 4 + wave) * kSegment + lane * 8;
         float sum[8] = {};
-        sum_rows(dy, ld, list, 0, all, c < cols ? c : 0, sum);
+        sum_rows(dy, ld, list, 0, all, Columns{c < cols ? c : 0, 0}, sum);
         if (c < cols) store_row(row + c, sum, scale, add);
         return;
     }

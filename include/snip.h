@@ -459,7 +459,7 @@ snip_status snip_embed(const void* w, snip_out_dtype w_dtype, int64_t vocab, int
  *   dw  : device, bf16 or fp32 (dw_dtype) [vocab][ld_dw], 16-byte aligned, ld_dw a multiple of 8.  Rows that no token names become
  *         zero, or with `accumulate` are not touched.
  *   workspace: device, >= snip_embed_workspace_bytes(tokens, cols, vocab) bytes, 16-byte aligned.  The size never falls as an extent grows.
- * Sums are fp32, of the tokens in their order (64 at a time where a row has more), and rounded once: results are the same from run to run. */
+ * Sums are fp32, of the tokens in their order (in parts of up to 64 where a row has more), and rounded once: results are the same from run to run. */
 size_t snip_embed_workspace_bytes(int64_t tokens, int64_t cols, int64_t vocab);
 snip_status snip_embed_backward(const void* dy, int64_t tokens, int64_t cols, int64_t ld_dy, const void* ids,
                                 snip_index_dtype id_dtype, int64_t vocab, float scale, void* dw, snip_out_dtype dw_dtype,

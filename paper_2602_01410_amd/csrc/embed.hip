@@ -2,14 +2,17 @@
 //     y[t] = scale w[ids[t]]            dw[v] = scale sum over t with ids[t] = v of dy[t]   (+ what dw holds)
 // Both move bytes and do nothing else: T rows read and written; T rows of dy read and the table's gradient written.
 //
-// The gradient takes three launches without atomics on memory, so that its sums have one order:
+// The gradient is formed without atomics on memory, so that its sums have one order.  Few tokens find each other themselves (embed_few_kernel); more take three
+// launches (16384 tokens of 4096 columns into fp32 [32000]: 17 + 136 + 9 us; 658 MB, of which a fill alone would store the 524 of the table in 76 us):
 //   sort      a workgroup for each range of token numbers looks through all of ids twice: it counts its numbers (and those below its
 //             range, which gives its place in the order), then puts the places of its tokens in order.  A wave takes a stretch of ids, so
-//             tokens of one number stay in their order.  T * ranges reads, from L2: 16384 ids of 8 bytes and 250 ranges are 65 MB.
-//   partials  rows with more than kLong tokens (the most frequent words, a tenth of a text each) are summed kLong tokens at a time
-//             by as many workgroups; for most blocks there is nothing to do.
-//   rows      a wave for each 512 columns of a row of the table: zeros, or the sum of its tokens, or of its partial sums; where the gradient is added to,
-//             of the rows that have tokens.
+//             tokens of one number stay in their order.  T * ranges reads, from L2: 16384 ids of 8 bytes and 250 ranges are 65 MB.  Latency bounds it: one read of
+//             the ids, counts in LDS, sums over waves and numbers, places.
+//   rows      parts of the rows with more than kLong tokens (the most frequent words, a tenth of a text each), kLong tokens at a time and first, so that they run
+//             beside the rest (launched before it they took 20 us of their own); and a wave for each 512 columns of every other row of the table: zeros, or the sum of
+//             its tokens; where the gradient is added to, of the rows that have tokens.  Memory bounds it: 4.8 TB/s.  A wave that takes 2 to 8 segments of its row one
+//             after the other: 148 to 196 us instead of 144, stores past the caches 205.
+//   long      long rows from their parts: a chain of five loads.
 #include "snip_internal.h"
 #include "quant_common.h"
 #include <type_traits>
@@ -57,7 +60,8 @@ __device__ __forceinline__ void store8(uint16_t* p, const float (&f)[8])
     *(uint4*)p = make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
 }
 
-// `lanes` (64 or 256) threads share a row.
+// `lanes` (64 or 256) threads share a row.  Bound by memory: 16384 rows of 4096 in fp32 52 us, 403 MB with rows that come again from caches; one row 2.1 us, a launch
+// and two loads in turn.
 template <class T, bool I64>
 __global__ __launch_bounds__(256) void embed_kernel(const T* __restrict__ w, int vocab, int cols, int64_t ldw, const void* __restrict__ ids,
                                                     int64_t tokens, float scale, uint16_t* __restrict__ y, int64_t ldy, int lanes)
@@ -165,7 +169,8 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const void* __
     }
 }
 
-// Eight columns of a lane: from a on, or (APART) four from a and four from b on, so that a wave's stores of fp32 are whole runs.
+// Eight columns of a lane: from a on, or (APART) four from a and four from b on, so that a wave's stores of fp32 are whole runs (136 us
+// instead of 144).
 struct Columns { int a, b; };
 template <bool APART> __device__ __forceinline__ uint4 load_row(const uint16_t* row, Columns c)
 {

@@ -482,7 +482,7 @@ snip_status snip_cross_entropy(const void* x, int64_t tokens, int64_t cols, int6
 /* Its gradients, from the same x, w and targets and the forward call's lse.  The logits are formed anew, a piece of the vocabulary at a time:
  *     dz[t][v] = dloss[t] * (exp(z[t][v] - lse[t]) - [v == targets[t]]),   dx = dz w,   dw = dz^T x.
  *   dloss: device, fp32 [tokens], the loss's gradient of every token (1 / count for a mean), or NULL for 1.  A token without a target, or
- *          whose dloss is zero, takes no part, whatever its x holds: its dx is zero and dw has nothing of it.
+ *          whose dloss is zero, takes no part, whatever its x holds: its dx is zero, dw has nothing of it, and no product is formed for it.
  *   dx   : device, bf16 [tokens][ld_dx], 16-byte aligned, ld_dx a multiple of 8, or NULL.
  *   dw   : device, bf16 or fp32 (dw_dtype) [vocab][ld_dw], 16-byte aligned, ld_dw a multiple of 8, or NULL (a frozen head); with
  *          `accumulate` the gradient is added to what dw holds.

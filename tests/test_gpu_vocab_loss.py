@@ -142,6 +142,17 @@ def test_few_tokens(tokens, cols, vocab, k):
     check(require_gpu(), Case(tokens, cols, vocab, k, index=torch.int32))
 
 
+@pytest.mark.parametrize("tokens, cols, vocab, k, ignored", [
+    (2048, 72, 300, 0, 0.5), (2049, 72, 300, 3, 0.5), (8192, 64, 130, 0, 0.9), (16390, 64, 33, 2, 0.4), (2100, 64, 257, 0, 1.1), (600, 264, 5000, 5, 0.6), (130, 520, 1003, 0, 0.99)])
+def test_tokens_that_are_not_learned(tokens, cols, vocab, k, ignored):
+    """Products over the tokens that take part alone, found by every workgroup or by a kernel of its own."""
+    c = Case(tokens, cols, vocab, k, ignored=ignored)
+    c.dloss[::5] = 0.0
+    if ignored < 1:
+        c.at[tokens // 3:tokens // 2] = -1                       # a prompt
+    check(require_gpu(), c)
+
+
 def test_long_contraction_and_splits():
     check(require_gpu(), Case(520, 2080, 9001, 4, 2.0))
 

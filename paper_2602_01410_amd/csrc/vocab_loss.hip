@@ -663,7 +663,7 @@ __global__ __launch_bounds__(256) void part_kernel(const uint16_t* __restrict__ 
 }
 
 // What a distillation's gradient needs of every token, a wave for each: entries (-1 where there is nothing: outside the vocabulary, q = 0, or one named
-// before, which has its q added) and q, and dloss tau, zero where no entry counts.
+// before, which has its q added) and q, and dloss tau, zero where no entry counts.  Bound by latency: 515 x 16 entries 5 us, 4096 x 32 9.
 template <bool I64>
 __global__ __launch_bounds__(256) void entries_kernel(const void* __restrict__ indices, const void* __restrict__ teacher, bool teacher_fp32, int tokens, int vocab,
                                                       int k, float tau, const float* __restrict__ dloss, int* __restrict__ index, float* __restrict__ q, float* __restrict__ weight)
@@ -718,8 +718,8 @@ __global__ __launch_bounds__(256) void entries_kernel(const void* __restrict__ i
 
 // Lists of the entries by tile: a workgroup for each `tn` tokens counts the entries of every vocabulary tile (1 << log_tm entries), forms their places
 // and writes them, with q or, without, with their place among all.  The order within a tile's run varies; two items of
-// one element do not meet: without q they have places of their own, with q entries_kernel has left one.  Latency bounds it: 37 x 8 entries 5 us, 4096 x 64 by 16 workgroups 23.
-constexpr int kMostTiles = 1 << 14;
+// one element do not meet: without q they have places of their own, with q entries_kernel has left one.  Latency bounds it: 37 x 8 entries 5 us, 4096 x 64 by 16 workgroups 20.
+constexpr int kMostTiles = 1 << 14, kHeldEntries = 16;      // loads of 1024 entries under way; as many of a workgroup are read once
 template <bool I64>
 __global__ __launch_bounds__(1024) void lists_kernel(const void* __restrict__ index, const float* __restrict__ q, const int* __restrict__ from, const int* __restrict__ count,
                                                      int tokens, int vocab, int k, int tn, int log_tm, int tiles, int* __restrict__ starts, int2* __restrict__ items)
@@ -731,17 +731,36 @@ __global__ __launch_bounds__(1024) void lists_kernel(const void* __restrict__ in
     const int t0 = blockIdx.x * tn, here = min(tn, tokens - t0) * k;
     if (here <= 0) return;
     const int64_t base = (int64_t)t0 * k;
-    auto source = [&](int i) { return from ? (int64_t)from[t0 + i / k] * k + i % k : base + i; };
-    auto number = [&](int i) {
-        const int64_t at = source(i), v = I64 ? ((const int64_t*)index)[at] : (int64_t)((const int*)index)[at];
-        return v >= 0 && v < vocab ? (int)v : -1;
+    // entries c0 + 1024 j + thread: -1 for those that name nothing, their tokens of the tile, and where they lie
+    int held[kHeldEntries], token[kHeldEntries];
+    unsigned source[kHeldEntries];
+    const int step = 1024 / k, step_rest = 1024 % k;               // (one division, not one for each entry)
+    auto fetch = [&](int c0) {
+        int t = (c0 + (int)threadIdx.x) / k, rest = (c0 + (int)threadIdx.x) % k;
+#pragma unroll
+        for (int j = 0; j < kHeldEntries; ++j) {
+            const bool is = c0 + j * 1024 + (int)threadIdx.x < here;
+            held[j] = -1;
+            token[j] = t;
+            if (c0 + j * 1024 < here) source[j] = is ? from ? (unsigned)from[t0 + t] * k + rest : (unsigned)(base + t * k + rest) : 0u;
+            t += step;
+            rest += step_rest;
+            if (rest >= k) { rest -= k; ++t; }
+        }
+#pragma unroll
+        for (int j = 0; j < kHeldEntries; ++j)
+            if (c0 + j * 1024 < here) {
+                const int64_t v = I64 ? ((const int64_t*)index)[source[j]] : (int64_t)((const int*)index)[source[j]];
+                held[j] = c0 + j * 1024 + (int)threadIdx.x < here && v >= 0 && v < vocab ? (int)v : -1;
+            }
     };
     for (int i = threadIdx.x; i < tiles; i += 1024) counts[i] = 0;
     __syncthreads();
-#pragma unroll 4
-    for (int i = threadIdx.x; i < here; i += 1024) {
-        const int v = number(i);
-        if (v >= 0) atomicAdd(&counts[v >> log_tm], 1);
+    for (int c0 = 0; c0 < here; c0 += kHeldEntries * 1024) {
+        fetch(c0);
+#pragma unroll
+        for (int j = 0; j < kHeldEntries; ++j)
+            if (held[j] >= 0) atomicAdd(&counts[held[j] >> log_tm], 1);
     }
     __syncthreads();
     int* out = starts + (int64_t)blockIdx.x * (tiles + 1);
@@ -766,11 +785,21 @@ __global__ __launch_bounds__(1024) void lists_kernel(const void* __restrict__ in
         __syncthreads();
     }
     if (threadIdx.x == 0) out[tiles] = before;
-    for (int i = threadIdx.x; i < here; i += 1024) {
-        const int v = number(i);
-        if (v < 0) continue;
-        const int at = atomicAdd(&counts[v >> log_tm], 1);
-        items[base + at] = make_int2((v & ((1 << log_tm) - 1)) << 16 | i / k, q ? __float_as_int(q[source(i)]) : (int)(base + i));
+    for (int c0 = 0; c0 < here; c0 += kHeldEntries * 1024) {
+        if (here > kHeldEntries * 1024) fetch(c0);
+        float wanted[kHeldEntries];
+        if (q) {
+#pragma unroll
+            for (int j = 0; j < kHeldEntries; ++j)
+                if (c0 + j * 1024 < here) wanted[j] = q[source[j]];
+        }
+#pragma unroll
+        for (int j = 0; j < kHeldEntries; ++j) {
+            const int v = held[j];
+            if (v < 0) continue;
+            const int at = atomicAdd(&counts[v >> log_tm], 1);
+            items[base + at] = make_int2((v & ((1 << log_tm) - 1)) << 16 | token[j], q ? __float_as_int(wanted[j]) : (int)source[j]);
+        }
     }
 }
 

@@ -876,7 +876,7 @@ __global__ __launch_bounds__(256) void join_kernel(const float2* __restrict__ ti
     }
 }
 
-// dx: the partial sums of the splits, rounded; zeros for tokens that take no part.  Bound by memory: 250 x 2080 of 28 splits, 58 MB, 19 us; 8192 x 4096 of one, 33.
+// dx: the partial sums of the splits, rounded; zeros for tokens that take no part.  Bound by memory: 150 of 250 x 2080 in 28 splits, 35 MB, 18 us; 8192 x 4096 in one, 33.
 __global__ __launch_bounds__(256) void dx_kernel(const float* __restrict__ sums, int splits, int64_t stride, int tokens, int cols, const int* __restrict__ place,
                                                  const float* __restrict__ unit, uint16_t* __restrict__ dx, int64_t ld)
 {

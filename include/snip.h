@@ -504,7 +504,7 @@ snip_status snip_cross_entropy_backward(const void* x, int64_t tokens, int64_t c
  *   indices: device, [tokens][k], contiguous.  An index may come twice: both entries count.
  *   teacher: device, fp32 or bf16 (teacher_dtype) [tokens][k], contiguous.  An entry of minus infinity has q = 0; a row of nothing else is
  *            one without a token.
- *   k      : 1 to 1024, tokens * k < 2^31.   temperature: finite, > 0, as is its inverse.
+ *   k      : 1 to 1024, tokens * k < 2^31.   temperature: > 0; its square, which is normal, is an fp32 number too (1.1e-19 to 1.8e19).
  * Other arguments as for snip_cross_entropy; workspace for this k. */
 snip_status snip_distill(const void* x, int64_t tokens, int64_t cols, int64_t ld_x, const void* w, int64_t vocab, int64_t ld_w,
                          const void* indices, snip_index_dtype index_dtype, const void* teacher, snip_out_dtype teacher_dtype, int64_t k,

@@ -122,7 +122,7 @@ snip_status check_vocab_loss(const VocabLossArgs& a, int index_type)
     if (a.tokens < 0 || a.tokens > kMostTokens || a.vocab <= 0 || a.vocab > kMostHead || a.cols <= 0 || a.cols >= kMostWidth || a.cols % 8 != 0) return SNIP_ERR_SHAPE;
     if (a.ldx >= kMostLd || a.ldw >= kMostLd || a.tokens * std::max(a.vocab, (int64_t)a.cols) > kMostLogits) return SNIP_ERR_SHAPE;
     if (a.k < 1 || a.k > 1024 || a.tokens * a.k >= (int64_t)1 << 31) return SNIP_ERR_SHAPE;
-    if (!std::isfinite(a.tau) || !(a.tau > 0.f) || !std::isfinite(1.f / a.tau)) return SNIP_ERR_FORMAT;
+    if (!(a.tau > 0.f) || !std::isfinite(1.f / a.tau) || !std::isnormal(a.tau * a.tau)) return SNIP_ERR_FORMAT;
     snip_status st = check_rows(a.x, a.tokens, a.cols, a.ldx);
     if (st == SNIP_OK) st = check_rows(a.w, a.vocab, a.cols, a.ldw);
     if (st == SNIP_OK) st = check_index(a.indices, index_type, a.tokens);

@@ -92,8 +92,9 @@ def test_losses(S):
     for call in (distill, distill_back):
         assert call(teacher=None) == NULL and call(tt=2) == FORMAT and call(teacher=at(0x10002)) == LAYOUT and call(teacher=at(0x10001), tt=0) == LAYOUT
         assert call(k=0) == SHAPE and call(k=1025) == SHAPE and call(tokens=1 << 21, k=1024) == SHAPE
-        for tau in (0.0, -1.0, float("nan"), float("inf"), 1e-39):
+        for tau in (0.0, -1.0, float("nan"), float("inf"), 1e-39, 1e-19, 1.9e19, -2.0):
             assert call(tau=tau) == FORMAT
+        assert call(tau=1.1e-19, ws=None) == WORKSPACE and call(tau=1.8e19, ws=None) == WORKSPACE
 
 
 @pytest.mark.parametrize("name, extents", [

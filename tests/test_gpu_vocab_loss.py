@@ -324,3 +324,52 @@ def test_no_tokens():
     dw = torch.ones(50, 64, device="cuda")
     c.backward(snip, lse, dw=dw, accumulate=True)
     assert torch.all(dw == 1)
+
+
+def test_weights_of_more_than_2_31_elements():
+    """The head's last rows lie behind 2^31 elements, in w and in its gradient: each token's target, and a teacher's entries, are there."""
+    snip = require_gpu()
+    tokens, cols, vocab = 5, 2056, 1048801
+    assert vocab * cols > 2 ** 31
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    w = torch.empty(vocab, cols, dtype=torch.bfloat16, device="cuda")
+    for r in range(0, vocab, 1 << 17):
+        w[r:r + (1 << 17)] = torch.randn(min(1 << 17, vocab - r), cols, generator=gen, device="cuda") * 0.05
+    x = torch.randn(tokens, cols, generator=gen, device="cuda").bfloat16()
+    at = torch.tensor([vocab - 1, 7, vocab - 2, vocab - 70000, 1 << 20], device="cuda")
+    pieces = [(r, min(r + (1 << 17), vocab)) for r in range(0, vocab, 1 << 17)]
+    z = torch.cat([x.double() @ w[a:b].double().t() for a, b in pieces], 1)
+    slack = (x.double().abs() @ w[at].double().abs().t()).amax() * ((cols + 2) * HALF32) * 2 + (300 + vocab / 128 + 60) * HALF32
+    for k in (0, 3):                     # (token 2 names one entry twice: each counts, with a third)
+        index = at if not k else torch.stack((at, at.flip(0), torch.arange(tokens, device="cuda")), 1)
+        teacher = torch.zeros(tokens, 3, device="cuda")
+        q = torch.zeros(tokens, vocab, dtype=torch.float64, device="cuda").scatter_add_(1, index.view(tokens, -1), torch.full((tokens, max(k, 1)), 1.0 / max(k, 1), dtype=torch.float64, device="cuda"))
+        loss, lse = snip.snip_distill(x, w, index, teacher) if k else snip.snip_cross_entropy(x, w, at)
+        want = torch.logsumexp(z, 1)
+        assert torch.all((lse.double() - want).abs() <= slack)
+        assert torch.all((loss.double() - (want - math.log(max(k, 1)) - (q * z).sum(1))).abs() <= 2 * slack + 30 * 8 * HALF32)
+        dx, dw = snip.snip_distill_backward(x, w, index, teacher, lse) if k else snip.snip_cross_entropy_backward(x, w, at, lse)
+        dz = torch.exp(z - lse.double()[:, None]) - q
+        err = dz.abs() * HALF16 * 1.01 + (torch.exp(z - lse.double()[:, None]) + q) * slack + 2.0 ** -125
+        wx, bx = 0, 0
+        for a, b in pieces:
+            wx, bx = wx + dz[:, a:b] @ w[a:b].double(), bx + (err[:, a:b] + dz[:, a:b].abs() * (vocab + 64) * HALF32) @ w[a:b].double().abs()
+        close(dx, wx, bx)
+        # dw in its first, middle and last rows, and those that are named
+        for rows in (slice(0, 300), slice(vocab // 2, vocab // 2 + 300), slice(vocab - 300, vocab), index.flatten()):
+            close(dw[rows], dz[:, rows].t() @ x.double(), err[:, rows].t() @ x.double().abs() + dz[:, rows].abs().t() @ x.double().abs() * 80 * HALF32)
+
+
+def test_widest_pitch():
+    """Rows almost 2^22 elements apart: places within a tile just below 2^31 bytes."""
+    snip = require_gpu()
+    c = Case(260, 72, 300, 2)
+    ld = (1 << 22) - 8
+    wide = [torch.empty(n * ld, dtype=torch.bfloat16, device="cuda").as_strided((n, 72), (ld, 1)) for n in (260, 300)]
+    wide[0].copy_(c.x), wide[1].copy_(c.w)
+    a = c.forward(snip)
+    a += c.backward(snip, a[1])
+    c.x, c.w = wide
+    b = c.forward(snip)
+    b += c.backward(snip, b[1])
+    assert all(torch.equal(p, q) for p, q in zip(a, b))

@@ -128,3 +128,29 @@ def test_streams_and_graph():
         dy.mul_(-0.5)
         a, b = snip.snip_embed(w, ids, 2.0), snip.snip_embed_backward(dy, ids, 900, 2.0)
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("tokens", [40, 2500])
+def test_tables_of_more_than_2_31_elements(tokens):
+    """Rows behind 2^31 elements, and a workspace with bytes in it that mean "not a number"."""
+    snip = require_gpu()
+    vocab, cols = 1048801, 2056
+    assert vocab * cols > 2 ** 31
+    gen = torch.Generator(device="cuda").manual_seed(tokens)
+    table = torch.zeros(vocab, cols, dtype=torch.bfloat16, device="cuda")
+    ids = torch.cat((torch.randint(vocab - 500, vocab, (tokens - 3,), generator=gen, device="cuda"), torch.tensor([0, 1 << 20, vocab - 1], device="cuda")))
+    rows = torch.unique(ids)
+    table[rows] = torch.randn(len(rows), cols, generator=gen, device="cuda").bfloat16()
+    assert torch.equal(snip.snip_embed(table, ids), table[ids])
+    dy = torch.randn(tokens, cols, generator=gen, device="cuda").bfloat16()
+    ws = torch.full((snip.embed_workspace_bytes(tokens, cols, vocab),), 255, dtype=torch.uint8, device="cuda")
+    want, size = (torch.zeros(len(rows), cols, dtype=torch.float64, device="cuda").index_add_(0, torch.searchsorted(rows, ids), t) for t in (dy.double(), dy.double().abs()))
+    for dtype in (torch.float32, torch.bfloat16):
+        dw = torch.full((vocab, cols), float("nan"), dtype=dtype, device="cuda")
+        snip.snip_embed_backward(dy, ids, vocab, dw=dw, workspace=ws)
+        tol = size * ((tokens + 1) * HALF32) * 1.01 + (want.abs() * HALF16 * 1.01 if dtype == torch.bfloat16 else 0)
+        assert torch.all((dw[rows].double() - want).abs() <= tol)
+        dw[rows] = 0
+        assert not dw.any()
+        snip.snip_embed_backward(dy, ids, vocab, dw=dw, accumulate=True, workspace=ws)
+        assert torch.all((dw[rows].double() - want).abs() <= tol)

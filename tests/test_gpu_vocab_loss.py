@@ -315,6 +315,35 @@ def test_streams_and_graph():
         torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("tokens, cols, vocab, k", [(1, 72, 300, 0), (33, 136, 1003, 3), (100, 64, 257, 0), (300, 520, 5003, 6), (600, 2056, 33001, 0), (2100, 72, 515, 2)])
+def test_workspace_may_hold_anything(tokens, cols, vocab, k):
+    """One workspace for calls of other sizes, captured ones among them, with bytes in it that mean "not a number"."""
+    snip = require_gpu()
+    c = Case(tokens, cols, vocab, k, ignored=0.3)
+    n = max(k, 1)
+    want = c.forward(snip)
+    want += c.backward(snip, want[1])
+    ws = torch.empty(max(snip.vocab_loss_workspace_bytes(tokens, cols, vocab, n), snip.vocab_loss_backward_workspace_bytes(tokens, cols, vocab, n)), dtype=torch.uint8, device="cuda")
+    bufs = [torch.empty_like(t) for t in want]
+
+    def calls():
+        c.forward(snip, loss=bufs[0], lse=bufs[1], workspace=ws)
+        c.backward(snip, bufs[1], dx=bufs[2], dw=bufs[3], workspace=ws)
+    graphs = []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            calls()
+        graphs.append(g)
+    for run in (calls, graphs[0].replay, graphs[1].replay, graphs[0].replay):
+        ws.fill_(255)
+        for t in bufs:
+            t.fill_(float("nan"))
+        run()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(bufs, want))
+
+
 def test_no_tokens():
     snip = require_gpu()
     c = Case(0, 64, 50)

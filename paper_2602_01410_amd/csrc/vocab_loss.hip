@@ -310,6 +310,23 @@ __device__ __forceinline__ void multiply(const ProductArgs& p, uint8_t* lds, int
 
 // In registers, lane 16 g + r of block (m, n) holds C[16 m + 4 g + t][16 n + r] in acc[m][n][t].
 
+// Stored from there: fp32 as it lies, 64 bytes of a row of the result by four lanes; bf16 of two blocks (m, m + 1), where lanes 16 apart swap halves so
+// that each has eight numbers in a row, again 64 bytes by four lanes.  (Through LDS in whole lines, before: 5.6 us of a tile of 256 x 256 behind its last product.)
+__device__ __forceinline__ void swap_rows(unsigned& a, unsigned& b)          // lanes 16 ... 31 and 48 ... 63 of a with those 16 before of b
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+    a = r[0];
+    b = r[1];
+}
+__device__ __forceinline__ v4u eight(v4f v, v4f w)
+{
+    v4u u = {pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(w[0], w[1]), pack2(w[2], w[3])};
+    { unsigned a = u[0], b = u[2]; swap_rows(a, b); u[0] = a; u[2] = b; }
+    { unsigned a = u[1], b = u[3]; swap_rows(a, b); u[1] = a; u[3] = b; }
+    return u;
+}
+__device__ __forceinline__ int eight_at(int m, int g) { return (m + (g & 1)) * 16 + (g >> 1) * 8; }
+
 // A wave's result leaves through its own part of LDS, 16 columns (rows of the result in memory) of WM numbers at a time: stores are whole runs then, and
 // an element that the loss names is found by its place.  16-byte chunk c of column r lies at c ^ r.
 template <class T> struct Stage {
@@ -359,6 +376,13 @@ template <class T> struct Names {
         from = __builtin_amdgcn_readfirstlane(run[0]); to = __builtin_amdgcn_readfirstlane(run[1]);
         items = p.items + tj * p.items_pitch;
         if (from < to) mine = items[min(from + lane, to - 1)];
+    }
+    // Whether there are some in columns 16 n ... 16 n + 15.
+    __device__ __forceinline__ bool some(int n, int tj) const
+    {
+        bool found = false;
+        of(n, tj, [&]() { found = true; }, [](int, int, int) {});
+        return found;
     }
     // Those of columns 16 n ... 16 n + 15: calls f(column, row, item), a lane for each, with the item of a list or, of targets, the token; `any` before, if there are some.
     template <class G, class F> __device__ __forceinline__ void of(int n, int tj, G any, F f) const
@@ -496,55 +520,104 @@ __global__ __launch_bounds__(T::NT, T::PER_CU) void product_kernel(const Product
 #pragma unroll
         for (int n = 0; n < T::NB; ++n) {
             const float base = lse[n] * kLog2e, mine = jw + n * 16 + r16 < p.J ? part[n] : 0.f;
-            stage.turn(n);
-#pragma unroll
-            for (int m = 0; m < T::MB; ++m) {
+            auto powers = [&](int m) {
                 v4f v = held<T>(acc[m][n]);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) v[k] = __builtin_amdgcn_exp2f(fmaf(v[k], c, -base));
-                stage.put(m, v);
+                return v;
+            };
+            // (the pitch covers whole tiles)
+            if (!names.some(n, tj)) {
+                uint16_t* to = (uint16_t*)p.c + (jw + n * 16 + r16) * p.ldc + iw;
+#pragma unroll
+                for (int m = 0; m < T::MB; m += 2) {
+                    auto weighted = [&](int m) {
+                        v4f v = powers(m);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) v[k] = mine == 0.f || iw + m * 16 + g * 4 + k >= p.I ? 0.f : v[k] * mine;
+                        return v;
+                    };
+                    const v4u u = eight(weighted(m), weighted(m + 1));
+                    if (jw + n * 16 + r16 < p.J) *reinterpret_cast<v4u*>(to + eight_at(m, g)) = u;
+                }
+                continue;
             }
+            stage.turn(n);
+#pragma unroll
+            for (int m = 0; m < T::MB; ++m) stage.put(m, powers(m));
             names.of(n, tj, []() {}, [&](int col, int row, int q) { *stage.at(col, row) -= p.targets ? 1.f : __int_as_float(q); });
             stage.take([&](int col, int row, const float (&f)[8]) {
                 const float coef = __shfl(mine, col);
                 float v[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = coef == 0.f || iw + row + e >= p.I ? 0.f : f[e] * coef;
-                // (the pitch covers whole tiles)
                 if (jw + n * 16 + col < p.J) *reinterpret_cast<v4u*>((uint16_t*)p.c + (jw + n * 16 + col) * p.ldc + iw + row) = packed(v);
             });
         }
     }
     if constexpr (OUT == kDx || OUT == kDw) {
+        // (I is a multiple of 8)
+        auto whole = [&](auto fp32, auto add) {
 #pragma unroll
-        for (int n = 0; n < T::NB; ++n) {
-            stage.turn(n);
+            for (int n = 0; n < T::NB; ++n) {
+                const int j = jw + n * 16 + r16;
+                auto scaled = [&](int m) {
+                    v4f v = held<T>(acc[m][n]);
 #pragma unroll
-            for (int m = 0; m < T::MB; ++m) stage.put(m, held<T>(acc[m][n]));
-            stage.take([&](int col, int row, const float (&f)[8]) {
-                const int j = jw + n * 16 + col, i = iw + row;
-                if (j >= p.J || i >= p.I) return;                   // (I is a multiple of 8)
-                float v[8];
+                    for (int k = 0; k < 4; ++k) v[k] = OUT == kDw ? v[k] * unit : v[k];
+                    return v;
+                };
+                if constexpr (decltype(fp32)::value) {
+                    float* to = (float*)p.c + (OUT == kDx ? blockIdx.y * p.split_stride : 0) + j * p.ldc + iw + g * 4;
+                    v4f old[T::MB];
+                    auto is = [&](int m) { return j < p.J && iw + m * 16 + g * 4 < p.I; };
+                    if constexpr (decltype(add)::value) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = OUT == kDw ? f[e] * unit : f[e];
-                if (OUT == kDx || p.c_fp32) {
-                    float4* to = reinterpret_cast<float4*>((float*)p.c + (OUT == kDx ? blockIdx.y * p.split_stride : 0) + j * p.ldc + i);
-                    if (p.add) {
-                        const float4 o = to[0], q = to[1];
-                        v[0] += o.x; v[1] += o.y; v[2] += o.z; v[3] += o.w; v[4] += q.x; v[5] += q.y; v[6] += q.z; v[7] += q.w;
+                        for (int m = 0; m < T::MB; ++m) old[m] = is(m) ? *reinterpret_cast<const v4f*>(to + m * 16) : v4f{0.f, 0.f, 0.f, 0.f};
                     }
-                    to[0] = make_float4(v[0], v[1], v[2], v[3]);
-                    to[1] = make_float4(v[4], v[5], v[6], v[7]);
+#pragma unroll
+                    for (int m = 0; m < T::MB; ++m) {
+                        v4f v = scaled(m);
+                        if constexpr (decltype(add)::value) v += old[m];
+                        if (is(m)) *reinterpret_cast<v4f*>(to + m * 16) = v;
+                    }
                 } else {
-                    v4u* to = reinterpret_cast<v4u*>((uint16_t*)p.c + j * p.ldc + i);
-                    if (p.add) {
-                        const v4u o = *to;
+                    uint16_t* to = (uint16_t*)p.c + j * p.ldc + iw;
+                    v4u old[T::MB / 2];
+                    auto is = [&](int m) { return j < p.J && iw + eight_at(m, g) < p.I; };
+                    if constexpr (decltype(add)::value) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) { v[2 * e] += __uint_as_float(o[e] << 16); v[2 * e + 1] += __uint_as_float(o[e] & 0xFFFF0000u); }
+                        for (int m = 0; m < T::MB; m += 2) old[m / 2] = is(m) ? *reinterpret_cast<const v4u*>(to + eight_at(m, g)) : v4u{0u, 0u, 0u, 0u};
                     }
-                    *to = packed(v);
+#pragma unroll
+                    for (int m = 0; m < T::MB; m += 2) {
+                        v4f v = scaled(m), w = scaled(m + 1);
+                        if constexpr (decltype(add)::value) {
+                            // (one rounding: the old numbers come to the products' places first)
+                            v4u o = old[m / 2];
+                            { unsigned a = o[0], b = o[2]; swap_rows(a, b); o[0] = a; o[2] = b; }
+                            { unsigned a = o[1], b = o[3]; swap_rows(a, b); o[1] = a; o[3] = b; }
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                v[2 * k] += __uint_as_float(o[k] << 16); v[2 * k + 1] += __uint_as_float(o[k] & 0xFFFF0000u);
+                                w[2 * k] += __uint_as_float(o[2 + k] << 16); w[2 * k + 1] += __uint_as_float(o[2 + k] & 0xFFFF0000u);
+                            }
+                        }
+                        const v4u u = eight(v, w);
+                        if (is(m)) *reinterpret_cast<v4u*>(to + eight_at(m, g)) = u;
+                    }
                 }
-            });
+            }
+        };
+        if constexpr (OUT == kDx) {
+            if (p.add) whole(std::true_type(), std::true_type());
+            else       whole(std::true_type(), std::false_type());
+        } else if (p.c_fp32) {
+            if (p.add) whole(std::true_type(), std::true_type());
+            else       whole(std::true_type(), std::false_type());
+        } else {
+            if (p.add) whole(std::false_type(), std::true_type());
+            else       whole(std::false_type(), std::false_type());
         }
     }
 }

@@ -202,10 +202,13 @@ template <int CTO> __device__ __forceinline__ void mfma_copy(v4f& acc, const bf1
 // next stage's first) and issues copies.  A barrier a stage, in front of its second step: every wave has the whole stage in registers
 // then, so its two slots are free, and the next stage has arrived.  With five slots B of stage s + 2 follows A of stage s in the ring and A of
 // stage s + 3 follows B: the copies have 1 to 1.5 stages (A) and 0.75 to 1 (B) to arrive.
-// `meanwhile` is called behind the first copies: loads for later.
-template <class T, bool TA, bool TB, class F>
-__device__ __forceinline__ void multiply(const ProductArgs& p, uint8_t* lds, int i0, int j0, int first, int last, int lane, int wave, v4f (&acc)[T::MB][T::NB], F meanwhile)
+// `before` and `behind` are called before and behind the first copies: loads for later.  (What waits for a copy waits for every load before it, and behind copies a load
+// makes the wait for the first stage one for later copies.)
+template <class T, bool TA, bool TB, class F, class G>
+__device__ __forceinline__ void multiply(const ProductArgs& p, uint8_t* lds, int i0, int j0, int first, int last, int lane, int wave, v4f (&acc)[T::MB][T::NB], F before, G behind)
 {
+    before();
+    __builtin_amdgcn_sched_barrier(0);
     const int wm = wave / T::WGN, wn = wave % T::WGN;
     Operand<T::TM, T::WM, TA, T::LARGE> a;
     Operand<T::TN, T::WN, TB, T::LARGE> b;
@@ -244,7 +247,7 @@ __device__ __forceinline__ void multiply(const ProductArgs& p, uint8_t* lds, int
             for (int u = 0; u < b.UNITS; ++u) b.copy(u, s, share_b + slot);
         }
     }
-    meanwhile();
+    behind();
     SNIP_WAIT_VM(T::BEHIND_FIRST);
     SNIP_BAR();
     unsigned sa = 0, sb = T::SA, to_a = (T::DA - 1) * T::PAIR;
@@ -372,8 +375,13 @@ template <class T> struct Names {
             }
             return;
         }
-        const int* run = p.starts + (int64_t)tj * (p.vocab_tiles + 1) + p.v0 / T::TM + ti;
-        from = __builtin_amdgcn_readfirstlane(run[0]); to = __builtin_amdgcn_readfirstlane(run[1]);
+        // (scalar loads, which the copies behind them do not hold up)
+        const auto* run = (const __attribute__((address_space(4))) int*)(p.starts + (int64_t)tj * (p.vocab_tiles + 1) + p.v0 / T::TM + ti);
+        from = run[0]; to = run[1];
+    }
+    __device__ __forceinline__ void load_items(int tj)
+    {
+        if (p.targets) return;
         items = p.items + tj * p.items_pitch;
         if (from < to) mine = items[min(from + lane, to - 1)];
     }
@@ -448,7 +456,7 @@ __global__ __launch_bounds__(T::NT, T::PER_CU) void product_kernel(const Product
     Names<T> names(p, lane);
     float lse[T::NB], part[T::NB];                                  // dz, of the lane's columns
     multiply<T, (OUT == kDx || OUT == kDw), OUT == kDw>(p, lds, i0, j0, first, last, lane, wave, acc, [&]() {
-        if constexpr (OUT == kStats || OUT == kDz) names.load(ti, tj, wm, wn);
+        if constexpr (OUT == kDz) names.load(ti, tj, wm, wn);
         if constexpr (OUT == kDz) {
 #pragma unroll
             for (int n = 0; n < T::NB; ++n) {
@@ -457,6 +465,9 @@ __global__ __launch_bounds__(T::NT, T::PER_CU) void product_kernel(const Product
                 part[n] = p.part[j];
             }
         }
+    }, [&]() {
+        if constexpr (OUT == kStats) names.load(ti, tj, wm, wn);
+        if constexpr (OUT == kStats || OUT == kDz) names.load_items(tj);
     });
 
     Stage<T> stage(lds, wave, lane);
@@ -519,7 +530,8 @@ __global__ __launch_bounds__(T::NT, T::PER_CU) void product_kernel(const Product
         const float c = p.alpha * kLog2e;
 #pragma unroll
         for (int n = 0; n < T::NB; ++n) {
-            const float base = lse[n] * kLog2e, mine = jw + n * 16 + r16 < p.J ? part[n] : 0.f;
+            // (a weight that is zero makes dz zero, whatever lse holds)
+            const float mine = jw + n * 16 + r16 < p.J ? part[n] : 0.f, base = mine == 0.f ? INFINITY : lse[n] * kLog2e;
             auto powers = [&](int m) {
                 v4f v = held<T>(acc[m][n]);
 #pragma unroll
@@ -529,17 +541,21 @@ __global__ __launch_bounds__(T::NT, T::PER_CU) void product_kernel(const Product
             // (the pitch covers whole tiles)
             if (!names.some(n, tj)) {
                 uint16_t* to = (uint16_t*)p.c + (jw + n * 16 + r16) * p.ldc + iw;
+                auto direct = [&](auto cut) {                        // cut: rows past the piece's end are zero
 #pragma unroll
-                for (int m = 0; m < T::MB; m += 2) {
-                    auto weighted = [&](int m) {
-                        v4f v = powers(m);
+                    for (int m = 0; m < T::MB; m += 2) {
+                        auto weighted = [&](int m) {
+                            v4f v = powers(m);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) v[k] = mine == 0.f || iw + m * 16 + g * 4 + k >= p.I ? 0.f : v[k] * mine;
-                        return v;
-                    };
-                    const v4u u = eight(weighted(m), weighted(m + 1));
-                    if (jw + n * 16 + r16 < p.J) *reinterpret_cast<v4u*>(to + eight_at(m, g)) = u;
-                }
+                            for (int k = 0; k < 4; ++k) v[k] = decltype(cut)::value && iw + m * 16 + g * 4 + k >= p.I ? 0.f : v[k] * mine;
+                            return v;
+                        };
+                        const v4u u = eight(weighted(m), weighted(m + 1));
+                        if (jw + n * 16 + r16 < p.J) *reinterpret_cast<v4u*>(to + eight_at(m, g)) = u;
+                    }
+                };
+                if (iw + T::WM > p.I) direct(std::true_type());
+                else                  direct(std::false_type());
                 continue;
             }
             stage.turn(n);
@@ -550,7 +566,7 @@ __global__ __launch_bounds__(T::NT, T::PER_CU) void product_kernel(const Product
                 const float coef = __shfl(mine, col);
                 float v[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = coef == 0.f || iw + row + e >= p.I ? 0.f : f[e] * coef;
+                for (int e = 0; e < 8; ++e) v[e] = iw + row + e >= p.I ? 0.f : f[e] * coef;
                 if (jw + n * 16 + col < p.J) *reinterpret_cast<v4u*>((uint16_t*)p.c + (jw + n * 16 + col) * p.ldc + iw + row) = packed(v);
             });
         }
@@ -1032,7 +1048,7 @@ template <int OUT> hipError_t launch_product(const ProductArgs& p, Shape shape, 
 
 // The backward call's pieces of the vocabulary, and the tiles and splits of dx.
 struct Plan { int64_t piece, splits; Shape dx; };
-constexpr int64_t kPieceElements = 1 << 27, kLeastPiece = 4096, kMostPiece = 1 << 17, kSplitElements = 1 << 25;
+constexpr int64_t kPieceElements = 1 << 28, kLeastPiece = 4096, kMostPiece = 1 << 17, kSplitElements = 1 << 25;
 // Splits of `here` entries, none of them empty, that are no more than `most`.
 int64_t splits_of(int64_t here, int64_t most)
 {

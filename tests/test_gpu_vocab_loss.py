@@ -131,7 +131,8 @@ def test_distillation(tokens, cols, vocab, k, tau, teacher):
     check(require_gpu(), Case(tokens, cols, vocab, k, tau, torch.int32 if k % 2 else torch.int64, teacher, ignored=0.2))
 
 
-@pytest.mark.parametrize("tokens, cols, vocab, k", [(40, 64, 20001, 0), (300, 72, 33000, 3), (64, 64, 16384, 0), (129, 64, 16385, 5)])
+@pytest.mark.parametrize("tokens, cols, vocab, k", [(40, 64, 20001, 0), (300, 72, 33000, 3), (64, 64, 16384, 0), (129, 64, 16385, 5),
+                                                     (70, 72, 140001, 3), (129, 64, 262145, 0), (2500, 72, 140001, 2), (20, 520, 131073, 4)])
 def test_pieces_of_the_vocabulary(tokens, cols, vocab, k):
     check(require_gpu(), Case(tokens, cols, vocab, k, ignored=0.1))
 

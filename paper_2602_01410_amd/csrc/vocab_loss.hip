@@ -360,7 +360,7 @@ template <class T> struct Names {
     const ProductArgs& p;
     const int2* items;
     int from, to, lane, row0, col0;          // the run of the tile's list; of the wave's block
-    int2 mine;                               // of the first 64 items of the run
+    int mine, mine_place;                    // of the first 64 items of the run (apart: a pair would live in scratch memory)
     int64_t target[T::NB];                   // of the lane's columns, as they are
     __device__ __forceinline__ Names(const ProductArgs& p_, int lane_) : p(p_), lane(lane_) {}
     __device__ __forceinline__ void load(int ti, int tj, int wm, int wn)
@@ -383,7 +383,9 @@ template <class T> struct Names {
     {
         if (p.targets) return;
         items = p.items + tj * p.items_pitch;
-        if (from < to) mine = items[min(from + lane, to - 1)];
+        if (from >= to) return;
+        const int2 item = items[min(from + lane, to - 1)];
+        mine = item.x; mine_place = item.y;
     }
     // Whether there are some in columns 16 n ... 16 n + 15.
     __device__ __forceinline__ bool some(int n, int tj) const
@@ -406,13 +408,17 @@ template <class T> struct Names {
         }
         bool first = true;
         for (int e = from; e < to; e += 64) {
-            const int2 item = e == from ? mine : items[min(e + lane, to - 1)];
-            const int row = (item.x >> 16) - row0, col = (item.x & 0xFFFF) - col0 - n * 16;
+            int at = mine, place = mine_place;
+            if (e != from) {
+                const int2 item = items[min(e + lane, to - 1)];
+                at = item.x; place = item.y;
+            }
+            const int row = (at >> 16) - row0, col = (at & 0xFFFF) - col0 - n * 16;
             const bool is = e + lane < to && row >= 0 && row < T::WM && col >= 0 && col < 16;
             if (__builtin_amdgcn_ballot_w64(is) == 0) continue;
             if (first) any();
             first = false;
-            if (is) f(col, row, item.y);
+            if (is) f(col, row, place);
         }
     }
 };
@@ -488,27 +494,29 @@ __global__ __launch_bounds__(T::NT, T::PER_CU) void product_kernel(const Product
             for (int n = 0; n < T::NB; ++n) {
                 int rows = p.I - iw - 4 * g;
                 auto counts = [&](int m, int k) { return !decltype(cut)::value || m * 16 + k < rows; };
-                float top = -INFINITY, sum = 0.f;
+                v4f v[T::MB];
+                float top = -INFINITY, tops[2] = {-INFINITY, -INFINITY}, part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int m = 0; m < T::MB; ++m) {
-                    const v4f v = held<T>(acc[m][n]);
+                    v[m] = held<T>(acc[m][n]);
                     if (decltype(cut)::value) asm volatile("" : "+v"(rows));      // (kept for all blocks, the comparisons would spill)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) top = fmaxf(top, counts(m, k) ? v[k] : -INFINITY);
+                    for (int k = 0; k < 4; ++k) tops[k & 1] = fmaxf(tops[k & 1], counts(m, k) ? v[m][k] : -INFINITY);
                 }
+                top = fmaxf(tops[0], tops[1]);
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32)) * c;
                 const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
                 for (int m = 0; m < T::MB; ++m) {
-                    const v4f v = held<T>(acc[m][n]);
                     if (decltype(cut)::value) asm volatile("" : "+v"(rows));
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        const float e = __builtin_amdgcn_exp2f(fmaf(v[k], c, -base));
-                        sum += counts(m, k) ? e : 0.f;
+                        const float e = __builtin_amdgcn_exp2f(fmaf(v[m][k], c, -base));
+                        part[k] += counts(m, k) ? e : 0.f;
                     }
                 }
+                float sum = (part[0] + part[1]) + (part[2] + part[3]);
                 sum += __shfl_xor(sum, 16);
                 sum += __shfl_xor(sum, 32);
                 if (g == 0) shared[wm * T::TN + wn * T::WN + n * 16 + r16] = make_float2(top, sum);

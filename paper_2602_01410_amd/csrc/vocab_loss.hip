@@ -49,7 +49,7 @@ struct ProductArgs {
 // TM x TN outputs of a workgroup of four waves, WM x WN of a wave.  LDS is a ring of SLOTS slots, a stage (64 contraction elements) of A and B
 // in turn; an odd number needs slots of one size.
 //   Large    bound by the matrix cores and the clock that the power leaves: a wave reads 32 KB from LDS a stage, for 128 MFMAs.  8192 x 4096 against
-//            128000 5.9 ms, 1.45 PFLOP/s (the product alone, by the vendor's library, 5.8 ms); its gradient, 32000, 4.7 ms, 1.37.  Matrix cores busy 64 to 67 % of the
+//            128000 5.9 ms, 1.45 PFLOP/s (the product alone, by the vendor's library, 5.8 ms); its gradient, 32000, 4.55 ms, 1.42.  Matrix cores busy 69 to 75 % of the
 //            cycles, at 1.9 GHz; no bank conflicts.
 //   Middle   two workgroups of a compute unit, for problems with too few large tiles and for 65 to 128 tokens: bound by the copies' latency, 1.1 us a stage.
 //   Few, Low up to 64 tokens: bound by w, which is read once; 64 tokens of 4096 against 128000 197 us, 5.3 TB/s, 37 of 2048 against 32000 21 us in the last-level cache.
@@ -667,7 +667,7 @@ struct Weights {
 };
 
 // The gradients' products run over the tokens that take part alone, in their order: of a dialogue whose prompt is not learned they are half.  `place`: of a
-// token among them, or -1.  8192 x 4096 against 32000: 4.73 ms with all, 3.27 without 40 % of them, 1.35 without 80 %.
+// token among them, or -1.  8192 x 4096 against 32000: 4.60 ms with all, 3.23 without 40 % of them, 1.38 without 80 %.
 // The largest weight that is finite, or 1, is the unit that dz is held in.  dz is rounded to bf16, and at the entry that is wanted it is near -1 times the
 // token's weight: exact in this unit where all weights are equal (a mean), and otherwise with the largest ones where bf16's relative steps are smallest.
 // Relative error of dw in bf16, its own rounding included, weights from 0.5 to 1.5: 0.0025 -> 0.0022; equal ones 0.0024 -> 0.0017.

@@ -439,23 +439,23 @@ __device__ __forceinline__ float2 join2(float2 v, float2 o)
     return make_float2(top, v.y * __builtin_amdgcn_exp2f(v.x - base) + o.y * __builtin_amdgcn_exp2f(o.x - base));
 }
 
+// Tile `tile` of split `split`.
 template <class T, int OUT>
-__global__ __launch_bounds__(T::NT, T::PER_CU) void product_kernel(const ProductArgs given)
+__device__ __forceinline__ void product(const ProductArgs& given, uint8_t* lds, int tile, int split)
 {
     ProductArgs p = given;
     if constexpr (OUT == kDz || OUT == kDx) {
-        p.J = *p.count;
+        p.J = __builtin_amdgcn_readfirstlane(*p.count);
         p.tiles_j = (p.J + T::TN - 1) / T::TN;
-        if (blockIdx.x >= p.tiles_i * p.tiles_j) return;
+        if (tile >= p.tiles_i * p.tiles_j) return;
     }
-    if constexpr (OUT == kDw) p.R = *p.count;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[T::LDS];
+    if constexpr (OUT == kDw) p.R = __builtin_amdgcn_readfirstlane(*p.count);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / T::WGN, wn = wave % T::WGN, r16 = lane & 15, g = lane >> 4;
     int ti, tj;
-    tile_of(blockIdx.x, p.tiles_i * p.tiles_j, p.tiles_i, p.tiles_j, ti, tj);
+    tile_of(tile, p.tiles_i * p.tiles_j, p.tiles_i, p.tiles_j, ti, tj);
     const int i0 = ti * T::TM, j0 = tj * T::TN;
-    const int all = (p.R + 63) / 64, first = OUT == kDx ? blockIdx.y * p.split : 0, last = OUT == kDx ? min(all, first + p.split) : all;
+    const int all = (p.R + 63) / 64, first = OUT == kDx ? split * p.split : 0, last = OUT == kDx ? min(all, first + p.split) : all;
     const float unit = OUT == kDw ? *p.unit : 1.f;
     v4f acc[T::MB][T::NB];
     const int iw = i0 + wm * T::WM, jw = j0 + wn * T::WN;
@@ -592,7 +592,7 @@ __global__ __launch_bounds__(T::NT, T::PER_CU) void product_kernel(const Product
                     return v;
                 };
                 if constexpr (decltype(fp32)::value) {
-                    float* to = (float*)p.c + (OUT == kDx ? blockIdx.y * p.split_stride : 0) + j * p.ldc + iw + g * 4;
+                    float* to = (float*)p.c + (OUT == kDx ? split * p.split_stride : 0) + j * p.ldc + iw + g * 4;
                     v4f old[T::MB];
                     auto is = [&](int m) { return j < p.J && iw + m * 16 + g * 4 < p.I; };
                     if constexpr (decltype(add)::value) {
@@ -644,6 +644,22 @@ __global__ __launch_bounds__(T::NT, T::PER_CU) void product_kernel(const Product
             else       whole(std::false_type(), std::false_type());
         }
     }
+}
+
+template <class T, int OUT>
+__global__ __launch_bounds__(T::NT, T::PER_CU) void product_kernel(const ProductArgs p)
+{
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[T::LDS];
+    product<T, OUT>(p, lds, blockIdx.x, blockIdx.y);
+}
+// dx (tiles x splits) and dw, which need dz alone, in one launch where neither has large tiles: what one leaves idle the other takes.
+template <class X, class W>
+__global__ __launch_bounds__(256, 2) void pair_kernel(const ProductArgs dx, int splits, const ProductArgs dw)
+{
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[X::LDS > W::LDS ? X::LDS : W::LDS];
+    const int tiles = dx.tiles_i * dx.tiles_j, b = blockIdx.x, split = __builtin_amdgcn_readfirstlane(b / tiles);
+    if (split < splits) product<X, kDx>(dx, lds, b - split * tiles, split);
+    else                product<W, kDw>(dw, lds, b - splits * tiles, 0);
 }
 
 __device__ __forceinline__ float logit(const void* teacher, bool fp32, int64_t at)
@@ -1042,6 +1058,26 @@ template <class T, int OUT> hipError_t launch_product(ProductArgs p, int splits,
     hipLaunchKernelGGL((product_kernel<T, OUT>), dim3((unsigned)(p.tiles_i * p.tiles_j), (unsigned)splits), dim3(T::NT), 0, s, p);
     return hipGetLastError();
 }
+// Stages of dw's tiles up to which it shares a launch with dx.  us of a call, shared and not: 515 x 1024 against 8191 (4608) 65.6 and 73, 16 x 2048 against 32000 (4000)
+// 113 and 118, 250 x 1024 against 50257 (12576) 153 and 158; 500 x 1024 against 50257 (25152) 244 and 240.
+constexpr int64_t kPairStages = 1 << 14;
+template <class X> hipError_t launch_pair(ProductArgs dx, int splits, ProductArgs dw, hipStream_t s)
+{
+    dx.tiles_i = (dx.I + X::TM - 1) / X::TM; dx.tiles_j = (dx.J + X::TN - 1) / X::TN;
+    dw.tiles_i = (dw.I + Middle::TM - 1) / Middle::TM; dw.tiles_j = (dw.J + Middle::TN - 1) / Middle::TN;
+    hipLaunchKernelGGL((pair_kernel<X, Middle>), dim3((unsigned)(dx.tiles_i * dx.tiles_j * splits + dw.tiles_i * dw.tiles_j)), dim3(256), 0, s, dx, splits, dw);
+    return hipGetLastError();
+}
+hipError_t launch_pair(const ProductArgs& dx, Shape shape, int splits, const ProductArgs& dw, hipStream_t s)
+{
+    switch (shape) {
+    case Shape::kFew64: return launch_pair<Few64>(dx, splits, dw, s);
+    case Shape::kFew32: return launch_pair<Few32>(dx, splits, dw, s);
+    case Shape::kLow64: return launch_pair<Low64>(dx, splits, dw, s);
+    case Shape::kLow32: return launch_pair<Low32>(dx, splits, dw, s);
+    default:            return launch_pair<Middle>(dx, splits, dw, s);
+    }
+}
 template <int OUT> hipError_t launch_product(const ProductArgs& p, Shape shape, int splits, hipStream_t s)
 {
     if (shape == Shape::kLarge) return launch_product<Large, OUT>(p, splits, s);
@@ -1222,20 +1258,25 @@ hipError_t launch_vocab_loss_backward(const VocabLossArgs& a, hipStream_t s)
         if (!a.distill) { p.targets = b.at; p.target64 = 0; }
         p.lse = b.lse; p.part = b.part; p.c = b.dz; p.ldc = pl.piece;
         hipError_t e = launch_product<kDz>(p, b.shape, 1, s);
-        if (e == hipSuccess && a.dx) {
+        if (e != hipSuccess) return e;
+        ProductArgs x = {}, d = {};
+        if (a.dx) {
             // dz is zero up to a whole tile, w has no row past the piece
-            ProductArgs d = {};
-            d.a = w; d.lda = a.ldw; d.I = (int)a.cols; d.b = b.dz; d.ldb = pl.piece; d.J = (int)a.tokens; d.R = (int)here;
-            d.split = (int)((up(here, 64) / 64 + pl.splits - 1) / pl.splits);
-            d.c = b.sums; d.ldc = a.cols; d.split_stride = a.tokens * a.cols; d.add = v0 > 0; d.count = b.count;
-            e = launch_product<kDx>(d, pl.dx, (int)pl.splits, s);
+            x.a = w; x.lda = a.ldw; x.I = (int)a.cols; x.b = b.dz; x.ldb = pl.piece; x.J = (int)a.tokens; x.R = (int)here;
+            x.split = (int)((up(here, 64) / 64 + pl.splits - 1) / pl.splits);
+            x.c = b.sums; x.ldc = a.cols; x.split_stride = a.tokens * a.cols; x.add = v0 > 0; x.count = b.count;
         }
-        if (e == hipSuccess && a.dw) {
-            ProductArgs d = {};
+        if (a.dw) {
             d.a = b.x; d.lda = a.cols; d.I = (int)a.cols; d.b = b.dz; d.ldb = pl.piece; d.J = (int)here; d.R = (int)a.tokens;
             d.c = a.dw_fp32 ? (void*)((float*)a.dw + v0 * a.lddw) : (void*)((uint16_t*)a.dw + v0 * a.lddw);
             d.ldc = a.lddw; d.c_fp32 = a.dw_fp32; d.add = a.add; d.unit = b.unit; d.count = b.count;
-            e = launch_product<kDw>(d, faster(a.cols, here, a.tokens), 1, s);
+        }
+        const Shape of_dw = faster(a.cols, here, a.tokens);
+        if (a.dx && a.dw && pl.dx != Shape::kLarge && of_dw == Shape::kMiddle && tiles_of(of_dw, a.cols, here) * stages_of(a.tokens) <= kPairStages) {
+            e = launch_pair(x, pl.dx, (int)pl.splits, d, s);
+        } else {
+            if (a.dx) e = launch_product<kDx>(x, pl.dx, (int)pl.splits, s);
+            if (e == hipSuccess && a.dw) e = launch_product<kDw>(d, of_dw, 1, s);
         }
         if (e != hipSuccess) return e;
     }

@@ -933,6 +933,25 @@ __global__ __launch_bounds__(256) void join_kernel(const float2* __restrict__ ti
         target = target64 ? ((const int64_t*)targets)[t] : (int64_t)((const int*)targets)[t];
         at_target = z[t];
     }
+    // of a distillation the first 64 entries of the tokens that this wave will take (`targets` are the entries' numbers)
+    constexpr int OWN = TOK / 4;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    auto entry = [&](int64_t at, float& u) {
+        const int64_t v = target64 ? ((const int64_t*)targets)[at] : (int64_t)((const int*)targets)[at];
+        u = logit(teacher, teacher_fp32, at) * alpha;
+        return v >= 0 && v < vocab && !(u == -INFINITY);
+    };
+    bool named[OWN];
+    float u_of[OWN], z_of[OWN];
+#pragma unroll
+    for (int o = 0; o < OWN; ++o) {
+        const int token = blockIdx.x * TOK + wave + o * 4;
+        named[o] = false;
+        u_of[o] = z_of[o] = 0.f;
+        if (!teacher || token >= tokens || lane >= k) continue;
+        named[o] = entry((int64_t)token * k + lane, u_of[o]);
+        z_of[o] = z[(int64_t)token * k + lane];
+    }
     float2 v = make_float2(-INFINITY, 0.f);
     for (int i0 = part; i0 < tiles; i0 += 8 * PARTS) {
         float2 o[8];
@@ -956,34 +975,32 @@ __global__ __launch_bounds__(256) void join_kernel(const float2* __restrict__ ti
         if (part == 0 && here) loss[t] = target >= 0 && target < vocab ? l - at_target : 0.f;
         return;
     }
-    // a wave for each token: q, and with it the loss (targets are the entries' numbers here)
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int i = wave; i < TOK; i += 4) {
-        const int token = blockIdx.x * TOK + i;
+    // a wave for each token: q, and with it the loss
+#pragma unroll
+    for (int o = 0; o < OWN; ++o) {
+        const int token = blockIdx.x * TOK + wave + o * 4;
         if (token >= tokens) break;
         const int64_t row = (int64_t)token * k;
-        const float2 all = shared[0][i];
+        const float2 all = shared[0][wave + o * 4];
         const float of_token = fmaf(all.x, kLn2, logf(all.y));
-        auto entry = [&](int j, float& u) {
-            const int64_t v = target64 ? ((const int64_t*)targets)[row + j] : (int64_t)((const int*)targets)[row + j];
-            u = logit(teacher, teacher_fp32, row + j) * alpha;
-            return v >= 0 && v < vocab && !(u == -INFINITY);
-        };
-        float top = -INFINITY, u, sum = 0.f, total = 0.f;
-        bool any = false;
-        for (int j = lane; j < k; j += 64)
-            if (entry(j, u)) { top = fmaxf(top, u); any = true; }
+        float top = fmaxf(-INFINITY, named[o] ? u_of[o] : -INFINITY), u, total = 0.f;
+        bool any = named[o];
+        for (int j = lane + 64; j < k; j += 64)
+            if (entry(row + j, u)) { top = fmaxf(top, u); any = true; }
         top = top_of_wave(top);
         const float base = top == -INFINITY ? 0.f : top;
-        for (int j = lane; j < k; j += 64)
-            if (entry(j, u)) sum += expf(u - base);
+        float sum = named[o] ? expf(u_of[o] - base) : 0.f;
+        for (int j = lane + 64; j < k; j += 64)
+            if (entry(row + j, u)) sum += expf(u - base);
         const float log_sum = logf(over_wave(sum));
-        for (int j = lane; j < k; j += 64)
-            if (entry(j, u)) {
-                const float log_q = u - base - log_sum, q = expf(log_q);
-                // (a q that is zero has no part, whatever its logit)
-                if (q != 0.f) total = fmaf(q, log_q + fmaf(-z[row + j], alpha, of_token), total);
-            }
+        auto add = [&](float u, float at) {
+            const float log_q = u - base - log_sum, q = expf(log_q);
+            // (a q that is zero has no part, whatever its logit)
+            if (q != 0.f) total = fmaf(q, log_q + fmaf(-at, alpha, of_token), total);
+        };
+        if (named[o]) add(u_of[o], z_of[o]);
+        for (int j = lane + 64; j < k; j += 64)
+            if (entry(row + j, u)) add(u, z[row + j]);
         total = over_wave(total);
         if (lane == 0) loss[token] = __builtin_amdgcn_ballot_w64(any) != 0 ? total * tau * tau : 0.f;
     }

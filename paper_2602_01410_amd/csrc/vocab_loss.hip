@@ -25,6 +25,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 enum Out { kStats, kDz, kDx, kDw };
+constexpr int kGroup = 16;       // tokens of a list of named entries: those of a block's columns
 
 struct ProductArgs {
     const uint16_t *a, *b;
@@ -33,8 +34,8 @@ struct ProductArgs {
     const int* count;            // gradients: tokens that take part, J of dz and dx and R of dw
     int tiles_i, tiles_j, split; // stages of a split (blockIdx.y)
     float alpha;                 // 1 / tau
-    // What the loss names: a target of every token, or lists, a run of each tile (vocabulary tiles of a token tile in turn): token and entry within
-    // the tile (16 bits each), and the place in `z` or q itself
+    // What the loss names: a target of every token, or lists of kGroup tokens each, a run for each tile of the vocabulary in turn: token of the group and entry
+    // of the tile (16 bits each), and the place in `z` or q itself
     const void* targets; int target64;
     const int* starts; const int2* items; int64_t items_pitch; int vocab_tiles;
     int v0, vocab;               // entry of A's first row
@@ -358,14 +359,15 @@ template <class T> struct Stage {
 // The elements of this wave's block that the loss names.
 template <class T> struct Names {
     const ProductArgs& p;
-    const int2* items;
-    int from, to, lane, row0, col0;          // the run of the tile's list; of the wave's block
-    int mine, mine_place;                    // of the first 64 items of the run (apart: a pair would live in scratch memory)
+    int lane, row0, col0, group0;            // of the wave's block; its first group of tokens
+    int from[T::NB], to[T::NB];              // runs of the groups' lists, and of each the first 64 items
+    int mine[T::NB], mine_place[T::NB];
     int64_t target[T::NB];                   // of the lane's columns, as they are
     __device__ __forceinline__ Names(const ProductArgs& p_, int lane_) : p(p_), lane(lane_) {}
+    __device__ __forceinline__ const int2* items(int n) const { return p.items + (group0 + n) * p.items_pitch; }
     __device__ __forceinline__ void load(int ti, int tj, int wm, int wn)
     {
-        row0 = wm * T::WM; col0 = wn * T::WN;
+        row0 = wm * T::WM; col0 = wn * T::WN; group0 = (tj * T::TN + col0) / kGroup;
         if (p.targets) {
             row0 += p.v0 + ti * T::TM;
 #pragma unroll
@@ -376,16 +378,22 @@ template <class T> struct Names {
             return;
         }
         // (scalar loads, which the copies behind them do not hold up)
-        const auto* run = (const __attribute__((address_space(4))) int*)(p.starts + (int64_t)tj * (p.vocab_tiles + 1) + p.v0 / T::TM + ti);
-        from = run[0]; to = run[1];
+#pragma unroll
+        for (int n = 0; n < T::NB; ++n) {
+            const bool is = (group0 + n) * kGroup < p.J;
+            const auto* run = (const __attribute__((address_space(4))) int*)(p.starts + (int64_t)(is ? group0 + n : 0) * (p.vocab_tiles + 1) + p.v0 / T::TM + ti);
+            from[n] = run[0]; to[n] = is ? run[1] : from[n];
+        }
     }
-    __device__ __forceinline__ void load_items(int tj)
+    __device__ __forceinline__ void load_items()
     {
         if (p.targets) return;
-        items = p.items + tj * p.items_pitch;
-        if (from >= to) return;
-        const int2 item = items[min(from + lane, to - 1)];
-        mine = item.x; mine_place = item.y;
+#pragma unroll
+        for (int n = 0; n < T::NB; ++n) {
+            if (from[n] >= to[n]) continue;
+            const int2 item = items(n)[min(from[n] + lane, to[n] - 1)];
+            mine[n] = item.x; mine_place[n] = item.y;
+        }
     }
     // Whether there are some in columns 16 n ... 16 n + 15.
     __device__ __forceinline__ bool some(int n, int tj) const
@@ -407,18 +415,19 @@ template <class T> struct Names {
             return;
         }
         bool first = true;
-        for (int e = from; e < to; e += 64) {
-            int at = mine, place = mine_place;
-            if (e != from) {
-                const int2 item = items[min(e + lane, to - 1)];
+        for (int e = from[n]; e < to[n]; e += 64) {
+            int at = mine[n], place = mine_place[n];
+            asm volatile("" : "+v"(at), "+v"(place));               // (numbers, not places in scratch memory)
+            if (e != from[n]) {
+                const int2 item = items(n)[min(e + lane, to[n] - 1)];
                 at = item.x; place = item.y;
             }
-            const int row = (at >> 16) - row0, col = (at & 0xFFFF) - col0 - n * 16;
-            const bool is = e + lane < to && row >= 0 && row < T::WM && col >= 0 && col < 16;
+            const int row = (at >> 16) - row0;
+            const bool is = e + lane < to[n] && row >= 0 && row < T::WM;
             if (__builtin_amdgcn_ballot_w64(is) == 0) continue;
             if (first) any();
             first = false;
-            if (is) f(col, row, place);
+            if (is) f(at & 0xFFFF, row, place);
         }
     }
 };
@@ -473,7 +482,7 @@ __device__ __forceinline__ void product(const ProductArgs& given, uint8_t* lds, 
         }
     }, [&]() {
         if constexpr (OUT == kStats) names.load(ti, tj, wm, wn);
-        if constexpr (OUT == kStats || OUT == kDz) names.load_items(tj);
+        if constexpr (OUT == kStats || OUT == kDz) names.load_items();
     });
 
     Stage<T> stage(lds, wave, lane);
@@ -775,16 +784,22 @@ __global__ __launch_bounds__(256) void part_kernel(const uint16_t* __restrict__ 
     }
 }
 
+constexpr unsigned kFree = 0xFFFFFFFFu, kTwice = 0x80000000u;
+__device__ __forceinline__ int place_in_table(int v, int mask) { return (int)((unsigned)v * 2654435761u >> 16) & mask; }
 // What a distillation's gradient needs of every token, a wave for each: entries (-1 where there is nothing: outside the vocabulary, q = 0, or one named
-// before, which has its q added) and q, and dloss tau, zero where no entry counts.  Bound by latency: 515 x 16 entries 5 us, 4096 x 32 9.
+// before, which has its q added) and q, and dloss tau, zero where no entry counts.  Bound by latency: 515 x 16 entries 5 us, 4096 x 32 9-12,
+// 4096 x 1024 45, 209 where most tokens name something twice (all entries compared with all: 1574).
 template <bool I64>
 __global__ __launch_bounds__(256) void entries_kernel(const void* __restrict__ indices, const void* __restrict__ teacher, bool teacher_fp32, int tokens, int vocab,
                                                       int k, float tau, const float* __restrict__ dloss, int* __restrict__ index, float* __restrict__ q, float* __restrict__ weight)
 {
     __shared__ int numbers[4][1024];
     __shared__ float wants[4][1024];
+    __shared__ unsigned table[4][2048];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const float alpha = 1.f / tau;
+    int mask = 63;
+    while (mask < 2 * k - 1) mask = 2 * mask + 1;
     for (int t = blockIdx.x * 4 + wave; t < tokens; t += gridDim.x * 4) {
         const int64_t row = (int64_t)t * k;
         float top = -INFINITY;
@@ -812,69 +827,90 @@ __global__ __launch_bounds__(256) void entries_kernel(const void* __restrict__ i
             if (w == 0.f) numbers[wave][j] = -1;
             wants[wave][j] = w;
         }
+        // those named twice are found with a table (open addressing, twice as many places as entries), and the wave looks through all entries for each of them
+        for (int j = lane; j <= mask; j += 64) table[wave][j] = kFree;
         for (int j = lane; j < k; j += 64) {
             const int v = numbers[wave][j];
-            float w = 0.f;
-            bool before = false;
-            if (v >= 0)
-                for (int i = 0; i < k; ++i)
-                    if (numbers[wave][i] == v) {
-                        before = before || i < j;
-                        w += wants[wave][i];
-                    }
-            index[row + j] = before ? -1 : v;
-            q[row + j] = before ? 0.f : w;
+            if (v < 0) continue;
+            int at = place_in_table(v, mask);
+            for (;; at = (at + 1) & mask) {
+                const unsigned old = atomicCAS(&table[wave][at], kFree, (unsigned)v);
+                if (old == kFree) break;
+                if ((old & ~kTwice) != (unsigned)v) continue;
+                atomicOr(&table[wave][at], kTwice);
+                break;
+            }
+        }
+        for (int j0 = 0; j0 < k; j0 += 64) {
+            const int j = j0 + lane;
+            int v = j < k ? numbers[wave][j] : -1;
+            float w = j < k ? wants[wave][j] : 0.f;
+            bool twice = false;
+            if (v >= 0) {
+                int at = place_in_table(v, mask);
+                while ((table[wave][at] & ~kTwice) != (unsigned)v) at = (at + 1) & mask;
+                twice = (table[wave][at] & kTwice) != 0;
+            }
+            const int named = v;
+            for (unsigned long long left = __builtin_amdgcn_ballot_w64(twice); left; left &= left - 1) {
+                const int l = __builtin_ctzll(left), of = __builtin_amdgcn_readlane(named, l);
+                float all = 0.f;
+                int first = k;
+                for (int i = lane; i < k; i += 64)
+                    if (numbers[wave][i] == of) { all += wants[wave][i]; first = min(first, i); }
+                all = over_wave(all);
+                for (int d = 32; d > 0; d >>= 1) first = min(first, __shfl_xor(first, d));
+                if (lane == l) { w = first < j ? 0.f : all; v = first < j ? -1 : v; }
+            }
+            if (j < k) { index[row + j] = v; q[row + j] = w; }
         }
         if (lane == 0) weight[t] = any ? dloss ? dloss[t] * tau : tau : 0.f;
     }
 }
 
-// Lists of the entries by tile: a workgroup for each `tn` tokens counts the entries of every vocabulary tile (1 << log_tm entries), forms their places
+// Lists of the entries by tile: a workgroup for each kGroup tokens counts the entries of every vocabulary tile (1 << log_tm entries), forms their places
 // and writes them, with q or, without, with their place among all.  The order within a tile's run varies; two items of
-// one element do not meet: without q they have places of their own, with q entries_kernel has left one.  Latency bounds it: 37 x 8 entries 5 us, 4096 x 64 by 16 workgroups 20.
-constexpr int kMostTiles = 1 << 14, kHeldEntries = 16;      // loads of 1024 entries under way; as many of a workgroup are read once
+// one element do not meet: without q they have places of their own, with q entries_kernel has left one.  Latency bounds it: 37 x 8 entries 5 us, 4096 x 64 7,
+// 4096 x 1024 24 (a list for all tokens of a tile: 23 and 290, and its tiles looked through as much as sixteen times the items).
+constexpr int kMostTiles = 1 << 14, kHeldEntries = kGroup * 1024 / 1024;      // entries of a thread, of up to 1024 for each token
 template <bool I64>
 __global__ __launch_bounds__(1024) void lists_kernel(const void* __restrict__ index, const float* __restrict__ q, const int* __restrict__ from, const int* __restrict__ count,
-                                                     int tokens, int vocab, int k, int tn, int log_tm, int tiles, int* __restrict__ starts, int2* __restrict__ items)
+                                                     int tokens, int vocab, int k, int log_tm, int tiles, int* __restrict__ starts, int2* __restrict__ items)
 {
     __shared__ int counts[kMostTiles];
     __shared__ int sums[16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (count) tokens = *count;
-    const int t0 = blockIdx.x * tn, here = min(tn, tokens - t0) * k;
+    const int t0 = blockIdx.x * kGroup, here = min(kGroup, tokens - t0) * k;
     if (here <= 0) return;
     const int64_t base = (int64_t)t0 * k;
-    // entries c0 + 1024 j + thread: -1 for those that name nothing, their tokens of the tile, and where they lie
+    // entries 1024 j + thread: -1 for those that name nothing, their tokens of the group, and where they lie
     int held[kHeldEntries], token[kHeldEntries];
     unsigned source[kHeldEntries];
+    float wanted[kHeldEntries];
     const int step = 1024 / k, step_rest = 1024 % k;               // (one division, not one for each entry)
-    auto fetch = [&](int c0) {
-        int t = (c0 + (int)threadIdx.x) / k, rest = (c0 + (int)threadIdx.x) % k;
+    int t = (int)threadIdx.x / k, rest = (int)threadIdx.x % k;
 #pragma unroll
-        for (int j = 0; j < kHeldEntries; ++j) {
-            const bool is = c0 + j * 1024 + (int)threadIdx.x < here;
-            held[j] = -1;
-            token[j] = t;
-            if (c0 + j * 1024 < here) source[j] = is ? from ? (unsigned)from[t0 + t] * k + rest : (unsigned)(base + t * k + rest) : 0u;
-            t += step;
-            rest += step_rest;
-            if (rest >= k) { rest -= k; ++t; }
-        }
+    for (int j = 0; j < kHeldEntries; ++j) {
+        token[j] = t;
+        if (j * 1024 < here) source[j] = j * 1024 + (int)threadIdx.x >= here ? 0u : from ? (unsigned)from[t0 + t] * k + rest : (unsigned)(base + t * k + rest);
+        t += step;
+        rest += step_rest;
+        if (rest >= k) { rest -= k; ++t; }
+    }
 #pragma unroll
-        for (int j = 0; j < kHeldEntries; ++j)
-            if (c0 + j * 1024 < here) {
-                const int64_t v = I64 ? ((const int64_t*)index)[source[j]] : (int64_t)((const int*)index)[source[j]];
-                held[j] = c0 + j * 1024 + (int)threadIdx.x < here && v >= 0 && v < vocab ? (int)v : -1;
-            }
-    };
+    for (int j = 0; j < kHeldEntries; ++j) {
+        held[j] = -1;
+        if (j * 1024 >= here) continue;
+        const int64_t v = I64 ? ((const int64_t*)index)[source[j]] : (int64_t)((const int*)index)[source[j]];
+        held[j] = j * 1024 + (int)threadIdx.x < here && v >= 0 && v < vocab ? (int)v : -1;
+        if (q) wanted[j] = q[source[j]];
+    }
     for (int i = threadIdx.x; i < tiles; i += 1024) counts[i] = 0;
     __syncthreads();
-    for (int c0 = 0; c0 < here; c0 += kHeldEntries * 1024) {
-        fetch(c0);
 #pragma unroll
-        for (int j = 0; j < kHeldEntries; ++j)
-            if (held[j] >= 0) atomicAdd(&counts[held[j] >> log_tm], 1);
-    }
+    for (int j = 0; j < kHeldEntries; ++j)
+        if (held[j] >= 0) atomicAdd(&counts[held[j] >> log_tm], 1);
     __syncthreads();
     int* out = starts + (int64_t)blockIdx.x * (tiles + 1);
     int before = 0;
@@ -898,21 +934,12 @@ __global__ __launch_bounds__(1024) void lists_kernel(const void* __restrict__ in
         __syncthreads();
     }
     if (threadIdx.x == 0) out[tiles] = before;
-    for (int c0 = 0; c0 < here; c0 += kHeldEntries * 1024) {
-        if (here > kHeldEntries * 1024) fetch(c0);
-        float wanted[kHeldEntries];
-        if (q) {
 #pragma unroll
-            for (int j = 0; j < kHeldEntries; ++j)
-                if (c0 + j * 1024 < here) wanted[j] = q[source[j]];
-        }
-#pragma unroll
-        for (int j = 0; j < kHeldEntries; ++j) {
-            const int v = held[j];
-            if (v < 0) continue;
-            const int at = atomicAdd(&counts[v >> log_tm], 1);
-            items[base + at] = make_int2((v & ((1 << log_tm) - 1)) << 16 | token[j], q ? __float_as_int(wanted[j]) : (int)source[j]);
-        }
+    for (int j = 0; j < kHeldEntries; ++j) {
+        const int v = held[j];
+        if (v < 0) continue;
+        const int at = atomicAdd(&counts[v >> log_tm], 1);
+        items[base + at] = make_int2((v & ((1 << log_tm) - 1)) << 16 | token[j], q ? __float_as_int(wanted[j]) : (int)source[j]);
     }
 }
 
@@ -1160,12 +1187,12 @@ Lists lists_space(const VocabLossArgs& a, Shape shape, Space& s)
     Lists l = {};
     if (!a.distill) return l;
     l.items = s.take<int2>((size_t)a.tokens * a.k);
-    l.starts = s.take<int>((up(a.tokens, tile_cols(shape)) / tile_cols(shape)) * (up(a.vocab, tile_rows(shape)) / tile_rows(shape) + 1));
+    l.starts = s.take<int>((up(a.tokens, kGroup) / kGroup) * (up(a.vocab, tile_rows(shape)) / tile_rows(shape) + 1));
     return l;
 }
 size_t lists_bytes(int64_t tokens, int64_t vocab, int64_t k)
 {
-    return to256((size_t)tokens * k * 8) + to256((size_t)(up(tokens, 32) / 32) * (up(vocab, 64) / 64 + 1) * 4);
+    return to256((size_t)tokens * k * 8) + to256((size_t)(up(tokens, kGroup) / kGroup) * (up(vocab, 64) / 64 + 1) * 4);
 }
 struct Forward { Lists l; float* z; float2* stats; Shape shape; size_t bytes; };
 Forward forward_space(const VocabLossArgs& a)
@@ -1199,15 +1226,15 @@ Backward backward_space(const VocabLossArgs& a, const Plan& pl)
 
 template <bool I64> void launch_lists(const VocabLossArgs& a, const void* index, const float* q, const int* from, const int* count, const Lists& l, Shape shape, hipStream_t s)
 {
-    const int64_t tn = tile_cols(shape), tm = tile_rows(shape);
-    hipLaunchKernelGGL(lists_kernel<I64>, dim3((unsigned)((a.tokens + tn - 1) / tn)), dim3(1024), 0, s, index, q, from, count, (int)a.tokens, (int)a.vocab, (int)a.k, (int)tn, tm == 256 ? 8 : tm == 128 ? 7 : 6,
+    const int64_t tm = tile_rows(shape);
+    hipLaunchKernelGGL(lists_kernel<I64>, dim3((unsigned)(up(a.tokens, kGroup) / kGroup)), dim3(1024), 0, s, index, q, from, count, (int)a.tokens, (int)a.vocab, (int)a.k, tm == 256 ? 8 : tm == 128 ? 7 : 6,
                        (int)((a.vocab + tm - 1) / tm), l.starts, l.items);
 }
 void name_entries(ProductArgs& p, const VocabLossArgs& a, const Lists& l, Shape shape)
 {
     p.alpha = 1.f / a.tau; p.vocab = (int)a.vocab;
     if (!a.distill) { p.targets = a.indices; p.target64 = a.index64; return; }
-    p.starts = l.starts; p.items = l.items; p.items_pitch = tile_cols(shape) * a.k; p.vocab_tiles = (int)(up(a.vocab, tile_rows(shape)) / tile_rows(shape));
+    p.starts = l.starts; p.items = l.items; p.items_pitch = kGroup * a.k; p.vocab_tiles = (int)(up(a.vocab, tile_rows(shape)) / tile_rows(shape));
 }
 
 }  // namespace

@@ -126,7 +126,9 @@ def test_cross_entropy(tokens, cols, vocab):
 
 @pytest.mark.parametrize("tokens, cols, vocab, k, tau, teacher", [
     (1, 8, 3, 2, 1.0, torch.float32), (5, 64, 100, 1, 0.5, torch.bfloat16), (33, 72, 300, 16, 2.0, torch.float32), (64, 136, 513, 64, 1.0, torch.bfloat16),
-    (70, 64, 1003, 130, 4.0, torch.float32), (258, 264, 700, 7, 1.5, torch.float32), (3, 16, 1100, 1024, 1.0, torch.float32), (2050, 64, 300, 70, 2.0, torch.bfloat16)])
+    (70, 64, 1003, 130, 4.0, torch.float32), (258, 264, 700, 7, 1.5, torch.float32), (3, 16, 1100, 1024, 1.0, torch.float32), (2050, 64, 300, 70, 2.0, torch.bfloat16),
+    # more entries than the vocabulary has: most come again
+    (20, 64, 100, 1024, 1.0, torch.float32), (40, 72, 300, 400, 2.0, torch.bfloat16), (300, 64, 60, 65, 1.0, torch.float32), (17, 64, 1, 33, 1.0, torch.float32)])
 def test_distillation(tokens, cols, vocab, k, tau, teacher):
     check(require_gpu(), Case(tokens, cols, vocab, k, tau, torch.int32 if k % 2 else torch.int64, teacher, ignored=0.2))
 

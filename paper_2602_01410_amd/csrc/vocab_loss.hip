@@ -872,7 +872,7 @@ __global__ __launch_bounds__(256) void entries_kernel(const void* __restrict__ i
 // and writes them, with q or, without, with their place among all.  The order within a tile's run varies; two items of
 // one element do not meet: without q they have places of their own, with q entries_kernel has left one.  Latency bounds it: 37 x 8 entries 5 us, 4096 x 64 7,
 // 4096 x 1024 24 (a list for all tokens of a tile: 23 and 290, and its tiles looked through as much as sixteen times the items).
-constexpr int kMostTiles = 1 << 14, kHeldEntries = kGroup * 1024 / 1024;      // entries of a thread, of up to 1024 for each token
+constexpr int kMostTiles = 1 << 14, kHeldEntries = kGroup;         // entries of each of 1024 threads: a token has up to 1024
 template <bool I64>
 __global__ __launch_bounds__(1024) void lists_kernel(const void* __restrict__ index, const float* __restrict__ q, const int* __restrict__ from, const int* __restrict__ count,
                                                      int tokens, int vocab, int k, int log_tm, int tiles, int* __restrict__ starts, int2* __restrict__ items)
@@ -943,7 +943,7 @@ __global__ __launch_bounds__(1024) void lists_kernel(const void* __restrict__ in
     }
 }
 
-// The tiles' sums joined and the loss formed: TOK tokens of a workgroup, 256 / TOK threads of a token.  8192 tokens of 500 tiles 9 us (33 MB); 4096 with 64 entries 16.
+// The tiles' sums joined and the loss formed: TOK tokens of a workgroup, 256 / TOK threads of a token.  8192 tokens of 500 tiles 9 us (33 MB); 4096 with 64 entries 14.
 template <int TOK>
 __global__ __launch_bounds__(256) void join_kernel(const float2* __restrict__ tile_stats, int tiles, int tokens, int vocab, float alpha, float tau, const void* __restrict__ targets,
                                                    int target64, const void* __restrict__ teacher, bool teacher_fp32, int k, const float* __restrict__ z, float* __restrict__ loss,

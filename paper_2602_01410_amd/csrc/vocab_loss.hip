@@ -1029,7 +1029,8 @@ __global__ __launch_bounds__(256) void join_kernel(const float2* __restrict__ ti
         for (int j = lane + 64; j < k; j += 64)
             if (entry(row + j, u)) add(u, z[row + j]);
         total = over_wave(total);
-        if (lane == 0) loss[token] = __builtin_amdgcn_ballot_w64(any) != 0 ? total * tau * tau : 0.f;
+        const bool wanted = __builtin_amdgcn_ballot_w64(any) != 0;       // (of all lanes: a ballot sees those that run it)
+        if (lane == 0) loss[token] = wanted ? total * tau * tau : 0.f;
     }
 }
 

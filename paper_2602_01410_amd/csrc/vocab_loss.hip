@@ -441,10 +441,13 @@ template <class T> __device__ __forceinline__ v4f held(v4f& acc)
     return acc;
 }
 
-// Two sums of powers of two, each (reference, sum of 2^(exponent - reference)).
+// What is subtracted from the exponents of a sum of powers of two: the largest of them.  Where that is infinite, nothing: infinity less infinity is no number,
+// and the sum is 0 or infinity as it stands.
+__device__ __forceinline__ float reference(float top) { return fabsf(top) == INFINITY ? 0.f : top; }
+// Two sums of powers of two, each (largest exponent, sum of 2^(exponent - reference)).
 __device__ __forceinline__ float2 join2(float2 v, float2 o)
 {
-    const float top = fmaxf(v.x, o.x), base = top == -INFINITY ? 0.f : top;
+    const float top = fmaxf(v.x, o.x), base = reference(top);
     return make_float2(top, v.y * __builtin_amdgcn_exp2f(v.x - base) + o.y * __builtin_amdgcn_exp2f(o.x - base));
 }
 
@@ -515,7 +518,7 @@ __device__ __forceinline__ void product(const ProductArgs& given, uint8_t* lds, 
                 top = fmaxf(tops[0], tops[1]);
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32)) * c;
-                const float base = top == -INFINITY ? 0.f : top;
+                const float base = reference(top);
 #pragma unroll
                 for (int m = 0; m < T::MB; ++m) {
                     if (decltype(cut)::value) asm volatile("" : "+v"(rows));

@@ -416,7 +416,8 @@ bool table(PyObject* o, bool may_be_fp32, bool optional, Table& m)
     if (t->dim() != 2 || !(t->scalar_type() == at::kBFloat16 || (fp32 && may_be_fp32)))
         return refuse(may_be_fp32 ? "expected a 2-D tensor of bf16 or fp32" : "expected a 2-D tensor of bf16");
     if (t->stride(1) != 1 && t->size(1) > 1) return refuse("rows must be contiguous");
-    m = {t->data_ptr(), t->size(0), t->size(1), t->stride(0), fp32 ? SNIP_OUT_FP32 : SNIP_OUT_BF16};
+    // (the stride of a single row is anything, also of tensors that torch calls contiguous)
+    m = {t->data_ptr(), t->size(0), t->size(1), t->size(0) > 1 ? t->stride(0) : t->size(1), fp32 ? SNIP_OUT_FP32 : SNIP_OUT_BF16};
     return true;
 }
 bool extents(const Table& m, int64_t rows, int64_t cols)

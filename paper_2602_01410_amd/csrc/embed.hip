@@ -307,7 +307,7 @@ __global__ __launch_bounds__(256) void embed_few_kernel(const uint16_t* __restri
     constexpr int HELD = FEW / 256, GROUPS = FEW / kLong, SLICE = 256 / GROUPS * 8;
     __shared__ int list[FEW];
     __shared__ int counts[4], befores[4];
-    __shared__ float sums[GROUPS][SLICE];
+    __shared__ __attribute__((aligned(16))) float sums[GROUPS][SLICE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), me = blockIdx.x;
     const int v = token<I64>(ids, me, vocab);
     const unsigned long long lower = (1ull << lane) - 1;

@@ -474,7 +474,8 @@ snip_status snip_embed_backward(const void* dy, int64_t tokens, int64_t cols, in
  *   workspace: device, >= snip_vocab_loss_workspace_bytes(tokens, cols, vocab, 1) bytes, 16-byte aligned.  The size never falls as an extent grows;
  *            calls that overlap in time must not share it.
  * Products are exact, sums, exponentials and logarithms fp32, in a fixed order.  Infinite logits count as the formulas have it: one of minus infinity adds
- * nothing (an entry that is masked out by its weights), one of plus infinity makes lse infinite. */
+ * nothing (an entry that is masked out by its weights), one of plus infinity makes lse infinite.  lse is fp32 too: of a logit s the exponential that a gradient forms,
+ * exp(s - lse), is off by up to |s| 2^-22 of itself, so gradients want |s| below some 2^13; from 2^29 on they need not be finite (the losses are). */
 size_t snip_vocab_loss_workspace_bytes(int64_t tokens, int64_t cols, int64_t vocab, int64_t k);
 snip_status snip_cross_entropy(const void* x, int64_t tokens, int64_t cols, int64_t ld_x, const void* w, int64_t vocab, int64_t ld_w,
                                const void* targets, snip_index_dtype index_dtype, float* loss, float* lse, void* workspace,

@@ -444,6 +444,9 @@ template <class T> __device__ __forceinline__ v4f held(v4f& acc)
 // What is subtracted from the exponents of a sum of powers of two: the largest of them.  Where that is infinite, nothing: infinity less infinity is no number,
 // and the sum is 0 or infinity as it stands.
 __device__ __forceinline__ float reference(float top) { return fabsf(top) == INFINITY ? 0.f : top; }
+// From 2^30 on half a step of the largest exponent, by which its product was rounded, is 32 and more: the largest term itself, 2^that, may be anything.  A sum
+// there is worth less than a step whatever it is, 1 to the vocabulary: 1, unless it is no number or the sum of nothing.
+__device__ __forceinline__ float far_sum(float top, float sum) { return fabsf(top) >= 1073741824.f && top != -INFINITY && sum == sum ? 1.f : sum; }
 // Two sums of powers of two, each (largest exponent, sum of 2^(exponent - reference)).
 __device__ __forceinline__ float2 join2(float2 v, float2 o)
 {
@@ -531,7 +534,7 @@ __device__ __forceinline__ void product(const ProductArgs& given, uint8_t* lds, 
                 float sum = (part[0] + part[1]) + (part[2] + part[3]);
                 sum += __shfl_xor(sum, 16);
                 sum += __shfl_xor(sum, 32);
-                if (g == 0) shared[wm * T::TN + wn * T::WN + n * 16 + r16] = make_float2(top, sum);
+                if (g == 0) shared[wm * T::TN + wn * T::WN + n * 16 + r16] = make_float2(top, far_sum(top, sum));
             }
         };
         if (iw + T::WM > p.I) sums(std::true_type());

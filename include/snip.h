@@ -446,7 +446,7 @@ snip_status snip_gemv(const void* x, int64_t m, int64_t k, int64_t ld, const sni
  * [0, vocab) is no token: it has no row, no loss and no gradient (padding; a target of -100). */
 typedef enum { SNIP_INDEX_I32 = 0, SNIP_INDEX_I64 = 1 } snip_index_dtype;
 
-/* y[t] = scale * w[ids[t]], rounded once; zeros where ids[t] is no token.
+/* y[t] = scale * w[ids[t]], a product in fp32 that is rounded to bf16; zeros where ids[t] is no token.
  *   w    : device, bf16 or fp32 (w_dtype) [vocab][ld_w], 16-byte aligned; cols < 2^20 and ld_w >= cols multiples of 8; 0 < vocab < 2^31.
  *   scale: finite.
  *   y    : device, bf16 [tokens][ld_y], 16-byte aligned, ld_y >= cols, a multiple of 8.  Columns >= cols are not touched. */
@@ -459,7 +459,9 @@ snip_status snip_embed(const void* w, snip_out_dtype w_dtype, int64_t vocab, int
  *   dw  : device, bf16 or fp32 (dw_dtype) [vocab][ld_dw], 16-byte aligned, ld_dw a multiple of 8.  Rows that no token names become
  *         zero, or with `accumulate` are not touched.
  *   workspace: device, >= snip_embed_workspace_bytes(tokens, cols, vocab) bytes, 16-byte aligned.  The size never falls as an extent grows.
- * Sums are fp32, of the tokens in their order (in parts of up to 64 where a row has more), and rounded once: results are the same from run to run. */
+ * Sums are fp32, of the tokens in their order (in parts of up to 64 where a row has more), and rounded once: results are the same from run to run.
+ * More than 2048 tokens are put in order by a pass over all of them for each 512 entries of the table: 17 us for 16384 tokens and 32000 entries, 1.6 ms for
+ * 2^20 tokens and 256000 entries. */
 size_t snip_embed_workspace_bytes(int64_t tokens, int64_t cols, int64_t vocab);
 snip_status snip_embed_backward(const void* dy, int64_t tokens, int64_t cols, int64_t ld_dy, const void* ids,
                                 snip_index_dtype id_dtype, int64_t vocab, float scale, void* dw, snip_out_dtype dw_dtype,
@@ -488,7 +490,8 @@ snip_status snip_cross_entropy(const void* x, int64_t tokens, int64_t cols, int6
  *   dx   : device, bf16 [tokens][ld_dx], 16-byte aligned, ld_dx a multiple of 8, or NULL.
  *   dw   : device, bf16 or fp32 (dw_dtype) [vocab][ld_dw], 16-byte aligned, ld_dw a multiple of 8, or NULL (a frozen head); with
  *          `accumulate` the gradient is added to what dw holds.
- *   workspace: as above, >= snip_vocab_loss_backward_workspace_bytes(tokens, cols, vocab, 1) bytes.
+ *   workspace: as above, >= snip_vocab_loss_backward_workspace_bytes(tokens, cols, vocab, 1) bytes.  It holds dz of one piece, up to 2^28 elements of bf16 (all of
+ *          dz where tokens * vocab is no more), partial sums of dx in fp32 and x of the tokens that take part: 743 MB for 8192 tokens of 4096 columns and 128000 entries.
  * dz is rounded to bf16 once, before the products with w and x (relative 2^-8 of each, also of an fp32 dw), in units of the largest finite |dloss|
  * (distillation: dloss * temperature): of equal weights the entry that is wanted loses least, and what is below 2^-126 of that unit may
  * become zero.  Sums are fp32, in a fixed order. */

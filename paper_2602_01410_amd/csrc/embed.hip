@@ -3,15 +3,16 @@
 // Both move bytes and do nothing else: T rows read and written; T rows of dy read and the table's gradient written.
 //
 // The gradient is formed without atomics on memory, so that its sums have one order.  Few tokens find each other themselves (embed_few_kernel); more take three
-// launches (16384 tokens of 4096 columns into fp32 [32000]: 17 + 136 + 9 us; 658 MB, of which a fill alone would store the 524 of the table in 76 us):
+// launches (16384 tokens of 4096 columns into fp32 [32000]: 17 + 143 + 9 us; 658 MB, of which a fill alone would store the 524 of the table in 76 us):
 //   sort      a workgroup for each range of token numbers looks through all of ids twice: it counts its numbers (and those below its
 //             range, which gives its place in the order), then puts the places of its tokens in order.  A wave takes a stretch of ids, so
 //             tokens of one number stay in their order.  T * ranges reads, from L2: 16384 ids of 8 bytes and 250 ranges are 65 MB.  Latency bounds it: one read of
-//             the ids, counts in LDS, sums over waves and numbers, places.
+//             the ids, counts in LDS, sums over waves and numbers, places.  Beyond, the reads do, which grow with tokens x numbers: 65536 x 128000 46 us of 133 for rows of 512
+//             columns, 2^20 x 256000 1550 of 1950, where an order by digits, which reads them a few times in all, would be the better one.
 //   rows      parts of the rows with more than kLong tokens (the most frequent words, a tenth of a text each), kLong tokens at a time and first, so that they run
 //             beside the rest (launched before it they took 20 us of their own); and a wave for each 512 columns of every other row of the table: zeros, or the sum of
-//             its tokens; where the gradient is added to, of the rows that have tokens.  Memory bounds it: 4.8 TB/s.  A wave that takes 2 to 8 segments of its row one
-//             after the other: 148 to 196 us instead of 144, stores past the caches 205.
+//             its tokens; where the gradient is added to, of the rows that have tokens.  Memory bounds it: 4.6 TB/s.  A wave that takes 2 to 8 segments of its row one
+//             after the other: 148 to 196 us, against 144 of this form at that time, stores past the caches 205.
 //   long      long rows from their parts: a chain of five loads.
 #include "snip_internal.h"
 #include "quant_common.h"
@@ -170,7 +171,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const void* __
 }
 
 // Eight columns of a lane: from a on, or (APART) four from a and four from b on, so that a wave's stores of fp32 are whole runs (136 us
-// instead of 144).
+// and 144, in turn on one machine).
 struct Columns { int a, b; };
 template <bool APART> __device__ __forceinline__ uint4 load_row(const uint16_t* row, Columns c)
 {

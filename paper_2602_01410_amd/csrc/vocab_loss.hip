@@ -50,8 +50,8 @@ struct ProductArgs {
 // TM x TN outputs of a workgroup of four waves, WM x WN of a wave.  LDS is a ring of SLOTS slots, a stage (64 contraction elements) of A and B
 // in turn; an odd number needs slots of one size.
 //   Large    bound by the matrix cores and the clock that the power leaves: a wave reads 32 KB from LDS a stage, for 128 MFMAs.  8192 x 4096 against
-//            128000 5.9 ms, 1.45 PFLOP/s (the product alone, by the vendor's library, 5.8 ms); its gradient, 32000, 4.55 ms, 1.42.  Matrix cores busy 69 to 75 % of the
-//            cycles, at 1.9 GHz; no bank conflicts.
+//            128000 5.9 to 6.0 ms, 1.44 PFLOP/s (the product alone, by the vendor's library, 5.8 ms); its gradient, 32000, 4.5 to 4.6 ms, 1.42.  Matrix cores busy 69 to 75 %
+//            of the cycles, at 1.9 GHz; bank conflicts of 100 cycles a launch at most.
 //   Middle   two workgroups of a compute unit, for problems with too few large tiles and for 65 to 128 tokens: bound by the copies' latency, 1.1 us a stage.
 //   Few, Low up to 64 tokens: bound by w, which is read once; 64 tokens of 4096 against 128000 197 us, 5.3 TB/s, 37 of 2048 against 32000 21 us in the last-level cache.
 template <int TM_, int TN_, int WM_, int WN_, int SLOTS_, int PER_CU_> struct Tile {
@@ -700,7 +700,7 @@ struct Weights {
 // The gradients' products run over the tokens that take part alone, in their order: of a dialogue whose prompt is not learned they are half.  `place`: of a
 // token among them, or -1.  8192 x 4096 against 32000: 4.60 ms with all, 3.23 without 40 % of them, 1.38 without 80 %.
 // The largest weight that is finite, or 1, is the unit that dz is held in.  dz is rounded to bf16, and at the entry that is wanted it is near -1 times the
-// token's weight: exact in this unit where all weights are equal (a mean), and otherwise with the largest ones where bf16's relative steps are smallest.
+// token's weight.  Where all weights are equal (a mean) the weight is 1 in this unit, so that p - q itself is rounded, near -1 where bf16's relative step is smallest.
 // Relative error of dw in bf16, its own rounding included, weights from 0.5 to 1.5: 0.0025 -> 0.0022; equal ones 0.0024 -> 0.0017.
 template <int NT> struct Live { int before[NT], waves[NT / 64]; unsigned bits[NT]; float tops[NT / 64]; };
 // Of tokens t0 ... t0 + 8 NT - 1, eight of a thread: their number, and `top` raised to their largest weight.
@@ -1040,7 +1040,8 @@ __global__ __launch_bounds__(256) void join_kernel(const float2* __restrict__ ti
     }
 }
 
-// dx: the partial sums of the splits, rounded; zeros for tokens that take no part.  Bound by memory: 150 of 250 x 2080 in 28 splits, 35 MB, 18 us; 8192 x 4096 in one, 33.
+// dx: the partial sums of the splits, rounded; zeros for tokens that take no part.  8192 x 4096 in one split, 201 MB, 33 us: memory.  150 of 250 x 2080 in 28 splits, 35 MB,
+// 18 us: loads in turn, which a thread adds up, in 254 workgroups.
 __global__ __launch_bounds__(256) void dx_kernel(const float* __restrict__ sums, int splits, int64_t stride, int tokens, int cols, const int* __restrict__ place,
                                                  const float* __restrict__ unit, uint16_t* __restrict__ dx, int64_t ld)
 {
@@ -1141,7 +1142,9 @@ template <int OUT> hipError_t launch_product(const ProductArgs& p, Shape shape, 
     return launch_product<Middle, OUT>(p, splits, s);
 }
 
-// The backward call's pieces of the vocabulary, and the tiles and splits of dx.
+// The backward call's pieces of the vocabulary, and the tiles and splits of dx.  They go by all tokens: how many take part is known on the device only, so where most do not,
+// dx has fewer splits than its tiles would bear.
+// Pieces are as large as 2^28 elements of dz, 537 MB, allow: with half of that dx is read and added to once more, 1 % of a step of 8192 tokens against 128000 entries.
 struct Plan { int64_t piece, splits; Shape dx; };
 constexpr int64_t kPieceElements = 1 << 28, kLeastPiece = 4096, kMostPiece = 1 << 17, kSplitElements = 1 << 25;
 // Splits of `here` entries, none of them empty, that are no more than `most`.
